@@ -186,8 +186,7 @@ def _handles(st):
                                           c["select"], st["scale"], types[c["dtype"]], st["lengths"])
     if c["kind"] != "token":
         st["plan"] = space(mst.mst_block_plan_bytes(st["shape"]))
-    call = {"attend": mst.MST_CALL_FWD, "train": mst.MST_CALL_BWD, "token": mst.MST_CALL_DECODE}[c["kind"]]
-    st["ws"] = space(mst.mst_block_attention_workspace_bytes(st["shape"], call))
+        st["ws"] = space(mst.mst_block_attention_workspace_bytes(st["shape"], c["kind"] == "train"))
 
 
 # ---------------------------------------------------------------- one pass
@@ -221,12 +220,12 @@ def _own_attend(st):
     mst.mst_block_select(shape, q, st["sums"], st["scales"], blocks)
     out = {"sums": st["sums"], "scales": st["scales"], "blocks": blocks, "o": o, "lse": lse}
     if c["kind"] == "token":
-        mst.mst_block_attention_decode(shape, q, k, v, blocks, o, lse, st["ws"])
+        mst.mst_block_attention_decode(shape, q, k, v, blocks, o, lse)
         return out
     mst.mst_block_plan(shape, blocks, st["plan"])
-    mst.mst_block_attention_fwd(shape, q, k, v, blocks, st["plan"], o, lse, st["ws"])
+    mst.mst_block_attention_fwd(shape, q, k, v, st["plan"], o, lse, st["ws"])
     if c["kind"] == "train":
-        mst.mst_block_attention_bwd(shape, q, k, v, blocks, st["plan"], o, lse, st["do"], st["dq"], st["dk"], st["dv"], st["ws"])
+        mst.mst_block_attention_bwd(shape, q, k, v, st["plan"], o, lse, st["do"], st["dq"], st["dk"], st["dv"], st["ws"])
         out.update(dq=st["dq"], dk=st["dk"], dv=st["dv"])
     return out
 
