@@ -267,8 +267,8 @@ def _power(e):
 
 
 def _exponent(x):
-    """floor(log2 x) of fp32 x > 0"""
-    return torch.frexp(x)[1] - 1
+    """floor(log2 x) of x >= 0; far below all others for 0"""
+    return torch.where(x > 0, torch.frexp(x)[1] - 1, -1000)
 
 
 def _to_8_bits(x, dims, over):
@@ -468,7 +468,7 @@ def _exact_eight(x, members):
     """x [..., members * D] integers or numbers in 64 bits -> 8-bit sums over the members and the exponent of their unit"""
     x = torch.where(torch.isfinite(x), x, 0.0)
     top = x.abs().amax(-1, keepdim=True)
-    e = (torch.frexp(top)[1] - 1).clamp(-100, 100)
+    e = torch.where(top > 0, torch.frexp(top)[1] - 1, -100).clamp(-100, 100)
     s = torch.round(x * _two_to(6 - e)).clamp(-127, 127).unflatten(-1, (members, -1)).sum(-2)
     r = (torch.frexp(s.abs().amax(-1, keepdim=True))[1] - 7).clamp(min=0)
     return torch.round(s * _two_to(-r)).clamp(-127, 127), (e - 6 + r)[..., 0]
