@@ -473,6 +473,117 @@ int mst_strided_attention_mask(uint8_t* M_dev, int L, int stride, mst_stream_t s
  * pattern table is this count over L * L. */
 int mst_strided_attention_count(int L, int stride, int64_t* count_out);
 
+/* ------------------------------------------- queries, keys and values of a block */
+
+/* A view of head vectors: data points at the first component of vector (batch 0, token 0, head 0); the strides count
+ * elements; the head_dim components of a vector are contiguous.  data and every stride of a dimension longer than one must be
+ * multiples of 16 bytes; strides of inputs may be 0 (one vector read for several), those of outputs may not.  A fused
+ * row of queries, keys and values is three views of one buffer.  Offsets are 64-bit. */
+typedef struct {
+    void* data;
+    int64_t batch, token, head;
+} mst_heads;
+
+/* Norm of every query and key head and the rotation by its token's position, in one pass:
+ *   n = x / sqrt(mean(x^2) + eps) * weight        (mean over the head_dim components; a weight per component)
+ *   y_a = n_a cos - n_b sin,  y_b = n_a sin + n_b cos
+ * over the pairs (a, b) of the leading `rotated` components: (i, i + rotated / 2), or (2i, 2i + 1) if interleaved is
+ * not 0.  The other components are left as they are. */
+typedef struct {
+    int32_t batch, tokens;       /* >= 0 */
+    int32_t heads, kv_heads;     /* query and key heads, >= 0: with 0 that side's arguments are not looked at */
+    int32_t head_dim;            /* a multiple of 8, 8 .. 256 */
+    int32_t rotated;             /* even, 0 .. head_dim */
+    int32_t interleaved;
+    int32_t table_rows;          /* rows of the table, >= 1 if rotated > 0 */
+    float eps;                   /* >= 0 */
+    mst_dtype in_type, out_type; /* of x and its gradient, of y and its gradient */
+} mst_qk_shape;
+
+/* q_weight, k_weight: fp32 [head_dim], or NULL for ones.  table: fp32 [table_rows x rotated], row p the rotated / 2 cosines
+ * of position p and then its sines (NULL if rotated is 0).  positions: int32 [batch x tokens], NULL for 0, 1, 2, ... in every
+ * sequence; a position outside the table is taken to its first or last row.  Sums are fp32; an output is
+ * rounded once.  In-place (q_out = q, of one type) is allowed. */
+int mst_qk_norm_rotate(const mst_qk_shape* shape, const mst_heads* q, const mst_heads* k,
+                       const float* q_weight_dev, const float* k_weight_dev, const float* table_dev,
+                       const int32_t* positions_dev, const mst_heads* q_out, const mst_heads* k_out, mst_stream_t stream);
+
+/* Gradients of the above for the same inputs: dq_in, dk_in (in_type) from dq_out, dk_out (out_type), and of the weights, fp32
+ * [head_dim] (either may be NULL: not wanted; with a NULL weight it is the gradient of ones).  Nothing has to be kept
+ * from the forward call.  Workspace: mst_qk_norm_rotate_workspace_bytes, 0 on invalid arguments. */
+int mst_qk_norm_rotate_bwd(const mst_qk_shape* shape, const mst_heads* q, const mst_heads* k,
+                           const float* q_weight_dev, const float* k_weight_dev, const float* table_dev,
+                           const int32_t* positions_dev, const mst_heads* dq_out, const mst_heads* dk_out,
+                           const mst_heads* dq_in, const mst_heads* dk_in, float* dq_weight_dev, float* dk_weight_dev,
+                           void* ws_dev, size_t ws_bytes, mst_stream_t stream);
+size_t mst_qk_norm_rotate_workspace_bytes(const mst_qk_shape* shape);
+
+/* ------------------------------------------- attention over selected blocks of keys */
+
+/* Sequence b has len_b = lengths_dev[b] keys (all `keys` of them if NULL; taken into 0 .. keys).  Its query i of `queries` sits
+ * at position p = len_b - queries + i and sees the keys 0 .. p: with queries = keys = len_b this is causal
+ * training, with queries = 1 the next token over a cache of which `keys` is the capacity, in between a piece of a prompt;
+ * len_b < queries is a sequence padded on the left, whose first queries (p < 0) are rows without keys: output 0, log-sum -inf,
+ * gradient 0.  Keys and values at or past len_b are never used, whatever they hold.  Keys are cut into blocks of
+ * `block`; a query's own block is the one that holds p.  heads / kv_heads query heads share a key head and one
+ * selection of blocks. */
+typedef struct {
+    int32_t batch, queries, keys;   /* >= 0; keys <= 2048 block */
+    int32_t heads, kv_heads;        /* heads a multiple of kv_heads, at most 64 times as many */
+    int32_t head_dim;               /* a multiple of 8, 8 .. 128 */
+    int32_t block;                  /* 32, 64 or 128 */
+    int32_t n_select;               /* blocks of a query, 1 .. 64 */
+    float scale;                    /* of the products q . k, finite */
+    mst_dtype type;                 /* of q, k, v, o and their gradients; products, statistics and sums are fp32 */
+    const int32_t* lengths_dev;     /* [batch] or NULL */
+} mst_attention_shape;
+
+/* Summaries of complete blocks of keys: sums_dev int8 [batch x kv_heads x ceil(keys / block) x head_dim] and scales_dev fp32
+ * [batch x kv_heads x ceil(keys / block)], the sum of a block's keys in 8 bits a component and the value of its unit, a
+ * power of two.  With E = floor(log2 max |key|) over the block (taken into -100 .. 100; components that are not finite count
+ * as 0):  k8 = round(key 2^(6 - E)) into -127 .. 127,  s = sum over the keys,  r = max(0, floor(log2 max |s|) - 6),
+ * sums = round(s 2^-r) into -127 .. 127,  scales = 2^(E - 6 + r); rounding is to nearest even.  A block of zeros has E = -100.
+ * Only blocks that the last new_tokens keys of their sequence completed are written (new_tokens >= keys: all complete blocks), so a
+ * cache's summaries are kept up token by token; entries of other blocks stay as they are. */
+int mst_key_summary(const mst_attention_shape* shape, const mst_heads* k, int8_t* sums_dev, float* scales_dev,
+                    int new_tokens, mst_stream_t stream);
+
+/* The blocks of each query, int32 [batch x kv_heads x queries x n_select]: its own block and the n_select - 1 blocks
+ * before it with the highest scores (lowest index on ties), ascending, -1 behind them.  The score of a block is
+ * q8 . sums * scales, q8 being the query heads that share the key head, rounded and summed as the keys of a block are.  The products
+ * are whole numbers below 2^24: scores, and so the selection, do not depend on the order of a sum, and a forward
+ * pass, its repetition and a later single-token call on the same values agree on them. */
+int mst_block_select(const mst_attention_shape* shape, const mst_heads* q, const int8_t* sums_dev, const float* scales_dev,
+                     int32_t* blocks_dev, mst_stream_t stream);
+
+/* The plan of a selection: for every block of keys the list of its queries, which forward and backward walk.  blocks_dev may be any
+ * selection; an entry that is negative, past the query's own block or not above the entries before it is left out.
+ * A plan holds for the shape that it was made with, whatever the inputs.  0 bytes on invalid arguments. */
+size_t mst_block_plan_bytes(const mst_attention_shape* shape);
+int mst_block_plan(const mst_attention_shape* shape, const int32_t* blocks_dev, void* plan_dev, size_t plan_bytes,
+                   mst_stream_t stream);
+
+/* o = softmax(scale q k^T over the keys that the query sees of its blocks) v, and the natural logarithm of the sum,
+ * lse_dev fp32 [batch x heads x queries]. */
+int mst_block_attention_fwd(const mst_attention_shape* shape, const mst_heads* q, const mst_heads* k, const mst_heads* v,
+                            const void* plan_dev, const mst_heads* o, float* lse_dev,
+                            void* ws_dev, size_t ws_bytes, mst_stream_t stream);
+
+/* Gradients of the above from its o and lse and the gradient d_o; keys and values that no query reads get 0 (all `keys` rows
+ * are written).  The selection has no gradient. */
+int mst_block_attention_bwd(const mst_attention_shape* shape, const mst_heads* q, const mst_heads* k, const mst_heads* v,
+                            const void* plan_dev, const mst_heads* o, const float* lse_dev, const mst_heads* d_o,
+                            const mst_heads* dq, const mst_heads* dk, const mst_heads* dv,
+                            void* ws_dev, size_t ws_bytes, mst_stream_t stream);
+
+/* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments. */
+size_t mst_block_attention_workspace_bytes(const mst_attention_shape* shape, int backward);
+
+/* The forward for few queries (single tokens over a cache), from blocks_dev itself, without plan or workspace.  The same rules
+ * for its entries.  lse_dev may be NULL. */
+int mst_block_attention_decode(const mst_attention_shape* shape, const mst_heads* q, const mst_heads* k, const mst_heads* v,
+                               const int32_t* blocks_dev, const mst_heads* o, float* lse_dev, mst_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -58,6 +58,31 @@ class TransformerFlops(C.Structure):
         return {k: float(getattr(self, k)) for k, _ in self._fields_}
 
 
+class HeadsView(C.Structure):
+    """Strided view of head vectors [batch, token, head, head_dim]; see heads()."""
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class QKNormShape(C.Structure):
+    """batch, tokens, heads, kv_heads, head_dim, rotated, interleaved, table_rows, eps, in_type, out_type"""
+    _fields_ = [(k, C.c_int32) for k in ("batch", "tokens", "heads", "kv_heads", "head_dim", "rotated", "interleaved",
+                                         "table_rows")] + [("eps", C.c_float), ("in_type", C.c_int), ("out_type", C.c_int)]
+
+
+class _AttentionShapeC(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("batch", "queries", "keys", "heads", "kv_heads", "head_dim", "block",
+                                         "n_select")] + [("scale", C.c_float), ("type", C.c_int), ("lengths_dev", C.c_void_p)]
+
+
+class BlockAttentionShape:
+    """Shape of the attention over selected blocks; `lengths` (int32 device tensor or None) is kept alive by it."""
+
+    def __init__(self, batch, queries, keys, heads, kv_heads, head_dim, block, n_select, scale, type=MST_BF16, lengths=None):
+        self.lengths = lengths
+        self._c = _AttentionShapeC(batch, queries, keys, heads, kv_heads, head_dim, block, n_select, scale, type, _ptr(lengths))
+        self._ref = C.byref(self._c)
+
+
 def lib_path() -> str:
     return os.path.join(HERE, "libmst_hip.so")
 
@@ -121,6 +146,17 @@ def lib() -> C.CDLL:
         "mst_flops_transformer": (i32, [C.POINTER(TransformerShape), dbl, dbl, C.POINTER(TransformerFlops)]),
         "mst_strided_attention_mask": (i32, [vp, i32, i32, vp]),
         "mst_strided_attention_count": (i32, [i32, i32, C.POINTER(i64)]),
+        "mst_qk_norm_rotate": (i32, [vp] * 10),
+        "mst_qk_norm_rotate_bwd": (i32, [vp] * 14 + [sz, vp]),
+        "mst_qk_norm_rotate_workspace_bytes": (sz, [vp]),
+        "mst_key_summary": (i32, [vp, vp, vp, vp, i32, vp]),
+        "mst_block_select": (i32, [vp] * 6),
+        "mst_block_plan_bytes": (sz, [vp]),
+        "mst_block_plan": (i32, [vp, vp, vp, sz, vp]),
+        "mst_block_attention_fwd": (i32, [vp] * 8 + [sz, vp]),
+        "mst_block_attention_bwd": (i32, [vp] * 12 + [sz, vp]),
+        "mst_block_attention_workspace_bytes": (sz, [vp, i32]),
+        "mst_block_attention_decode": (i32, [vp] * 8),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -139,7 +175,10 @@ EXPORTS = ["mst_version", "mst_last_hip_error", "mst_layer_device_bytes", "mst_w
            "mst_dense_grad", "mst_update_counts", "mst_mask_update_from_scores", "mst_mask_update_from_scores_multi", "mst_mask_update",
            "mst_sparse_fc_bwd_weight_update",
            "mst_schedule_density", "mst_erdos_renyi_density", "mst_flops_fc_forward", "mst_flops_transformer",
-           "mst_strided_attention_mask", "mst_strided_attention_count"]
+           "mst_strided_attention_mask", "mst_strided_attention_count",
+           "mst_qk_norm_rotate", "mst_qk_norm_rotate_bwd", "mst_qk_norm_rotate_workspace_bytes", "mst_key_summary",
+           "mst_block_select", "mst_block_plan_bytes", "mst_block_plan", "mst_block_attention_fwd", "mst_block_attention_bwd",
+           "mst_block_attention_workspace_bytes", "mst_block_attention_decode"]
 
 
 def _check(fn: str, code: int):
@@ -454,3 +493,79 @@ def mst_strided_attention_count(L: int, stride: int) -> int:
     out = C.c_int64(0)
     _check("mst_strided_attention_count", lib().mst_strided_attention_count(int(L), int(stride), C.byref(out)))
     return int(out.value)
+
+
+# ------------------------------------------------------------------ queries, keys and values
+
+def heads(t) -> HeadsView:
+    """View of a tensor [batch, token, head, head_dim] whose last dimension is contiguous.  The calls below take either a tensor or
+    such a view; a program that calls again on the same buffers makes the view once.  A view does not keep its tensor alive."""
+    s = t.stride()
+    if len(s) != 4 or (s[3] != 1 and t.shape[3] > 1):
+        raise ValueError("heads are [batch, token, head, head_dim] with contiguous components")
+    return HeadsView(t.data_ptr(), s[0], s[1], s[2])
+
+
+def _heads(t):
+    if t is None:
+        return None
+    return C.byref(t if isinstance(t, HeadsView) else heads(t))
+
+
+def mst_qk_norm_rotate(shape: QKNormShape, q, k, q_weight, k_weight, table, positions, q_out, k_out, stream=None):
+    _check("mst_qk_norm_rotate",
+           lib().mst_qk_norm_rotate(C.byref(shape), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _ptr(table),
+                                    _ptr(positions), _heads(q_out), _heads(k_out), _stream(stream)))
+
+
+def mst_qk_norm_rotate_workspace_bytes(shape: QKNormShape) -> int:
+    return int(lib().mst_qk_norm_rotate_workspace_bytes(C.byref(shape)))
+
+
+def mst_qk_norm_rotate_bwd(shape: QKNormShape, q, k, q_weight, k_weight, table, positions, dq_out, dk_out, dq_in, dk_in,
+                           dq_weight, dk_weight, ws, stream=None):
+    _check("mst_qk_norm_rotate_bwd",
+           lib().mst_qk_norm_rotate_bwd(C.byref(shape), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _ptr(table),
+                                        _ptr(positions), _heads(dq_out), _heads(dk_out), _heads(dq_in), _heads(dk_in),
+                                        _ptr(dq_weight), _ptr(dk_weight), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def mst_key_summary(shape: BlockAttentionShape, k, sums, scales, new_tokens: int, stream=None):
+    _check("mst_key_summary",
+           lib().mst_key_summary(shape._ref, _heads(k), _ptr(sums), _ptr(scales), new_tokens, _stream(stream)))
+
+
+def mst_block_select(shape: BlockAttentionShape, q, sums, scales, blocks, stream=None):
+    _check("mst_block_select",
+           lib().mst_block_select(shape._ref, _heads(q), _ptr(sums), _ptr(scales), _ptr(blocks), _stream(stream)))
+
+
+def mst_block_plan_bytes(shape: BlockAttentionShape) -> int:
+    return int(lib().mst_block_plan_bytes(shape._ref))
+
+
+def mst_block_plan(shape: BlockAttentionShape, blocks, plan, stream=None):
+    _check("mst_block_plan", lib().mst_block_plan(shape._ref, _ptr(blocks), _ptr(plan), plan.numel(), _stream(stream)))
+
+
+def mst_block_attention_workspace_bytes(shape: BlockAttentionShape, backward: bool) -> int:
+    return int(lib().mst_block_attention_workspace_bytes(shape._ref, int(backward)))
+
+
+def mst_block_attention_fwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, ws, stream=None):
+    _check("mst_block_attention_fwd",
+           lib().mst_block_attention_fwd(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(plan), _heads(o), _ptr(lse), _ptr(ws),
+                                         ws.numel(), _stream(stream)))
+
+
+def mst_block_attention_bwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, d_o, dq, dk, dv, ws, stream=None):
+    _check("mst_block_attention_bwd",
+           lib().mst_block_attention_bwd(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(plan), _heads(o), _ptr(lse),
+                                         _heads(d_o), _heads(dq), _heads(dk), _heads(dv), _ptr(ws), ws.numel(),
+                                         _stream(stream)))
+
+
+def mst_block_attention_decode(shape: BlockAttentionShape, q, k, v, blocks, o, lse, stream=None):
+    _check("mst_block_attention_decode",
+           lib().mst_block_attention_decode(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(blocks), _heads(o), _ptr(lse),
+                                            _stream(stream)))

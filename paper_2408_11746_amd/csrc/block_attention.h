@@ -1,0 +1,83 @@
+// What the calls of the attention over selected blocks share: the shape as kernels take it, the plan and its memory.
+#pragma once
+
+#include "heads.h"
+
+namespace mst {
+
+struct AttentionArgs {
+    int B, Tq, S, H, G, R, D;            // R query heads share a key head: H = G R
+    int BK, nb, NS;                      // keys of a block, blocks of the cache, blocks of a query
+    float scale;
+    const int* lengths;
+    __device__ int length(int b) const { return lengths ? min(max(lengths[b], 0), S) : S; }
+};
+
+// Lists of the queries of each block of keys.  bg = b G + g; a pair is query * NS + place in the query's selection.
+constexpr int PLAN_TILE = 256;           // queries that a workgroup of the builders takes
+constexpr int ITEM_ROWS = 512;           // rows (query, head) of an item: one workgroup of the kernels that walk lists
+struct Plan {
+    uint64_t* valid = nullptr;           // [bg][Tq] entries of the selection that count, a bit each
+    int* list = nullptr;                 // [bg][Tq NS] pairs, block after block, ascending inside a block
+    int* start = nullptr;                // [bg][nb + 1] first pair of a block
+    int* item_start = nullptr;           // [bg][nb + 1] first item of a block
+    int2* items = nullptr;               // [bg][max_items] block and first pair
+    int* tile = nullptr;                 // [bg][tiles][nb] pairs of a block before those of this tile of queries
+    int tiles = 0, max_items = 0, item_pairs = 0;
+    size_t total = 0;
+};
+
+inline int item_pairs(int R) { return std::max(8, ITEM_ROWS / R); }
+
+inline Plan carve_plan(void* base, const AttentionArgs& a) {
+    Plan p;
+    const size_t bg = (size_t)a.B * a.G, pairs = (size_t)a.Tq * a.NS;
+    p.tiles = (int)cdiv(a.Tq, PLAN_TILE);
+    p.item_pairs = item_pairs(a.R);
+    p.max_items = a.nb + (int)cdiv((int64_t)pairs, p.item_pairs);
+    char* c = static_cast<char*>(base);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* r = c + at;
+        at = align_up(at + bytes);
+        return r;
+    };
+    p.valid = reinterpret_cast<uint64_t*>(take(bg * a.Tq * 8));
+    p.list = reinterpret_cast<int*>(take(bg * pairs * 4));
+    p.start = reinterpret_cast<int*>(take(bg * (a.nb + 1) * 4));
+    p.item_start = reinterpret_cast<int*>(take(bg * (a.nb + 1) * 4));
+    p.items = reinterpret_cast<int2*>(take(bg * p.max_items * 8));
+    p.tile = reinterpret_cast<int*>(take(bg * p.tiles * a.nb * 4));
+    p.total = std::max<size_t>(at, 256);
+    return p;
+}
+
+inline int check_attention(const mst_attention_shape* s) {
+    if (!s || !is_type(s->type) || !(s->scale > -1e30f && s->scale < 1e30f) || !aligned16(s->lengths_dev)) return MST_ERR_ARG;
+    if (s->batch < 0 || s->queries < 0 || s->keys < 0 || s->kv_heads < 1 || s->heads < 1 || s->heads > HEADS_MAX) return MST_ERR_SHAPE;
+    if (s->heads % s->kv_heads != 0 || s->heads / s->kv_heads > 64) return MST_ERR_SHAPE;
+    if (s->head_dim < 8 || s->head_dim > HEAD_DIM_MAX || s->head_dim % 8 != 0) return MST_ERR_SHAPE;
+    if (s->block != 32 && s->block != 64 && s->block != 128) return MST_ERR_SHAPE;
+    if (s->n_select < 1 || s->n_select > SELECT_MAX) return MST_ERR_SHAPE;
+    if ((int64_t)s->keys > (int64_t)KEY_BLOCKS_MAX * s->block) return MST_ERR_SHAPE;
+    // grids of (batch, key head): 65535; pairs and rows of one of them: 31 bits
+    if ((int64_t)s->batch * s->kv_heads > 65535) return MST_ERR_SHAPE;
+    if ((int64_t)s->queries * s->n_select * (s->heads / s->kv_heads) >= (int64_t(1) << 30)) return MST_ERR_SHAPE;
+    return MST_OK;
+}
+
+inline AttentionArgs attention_args(const mst_attention_shape* s) {
+    AttentionArgs a;
+    a.B = s->batch, a.Tq = s->queries, a.S = s->keys, a.H = s->heads, a.G = s->kv_heads, a.R = s->heads / s->kv_heads, a.D = s->head_dim;
+    a.BK = s->block, a.nb = (int)cdiv(s->keys, s->block), a.NS = s->n_select, a.scale = s->scale, a.lengths = s->lengths_dev;
+    return a;
+}
+
+// f(T) with the storage type of the shape
+template <typename F>
+void with_type(mst_dtype type, F&& f) {
+    if (type == MST_F32) f(float{});
+    else f(bf16{});
+}
+
+}  // namespace mst
