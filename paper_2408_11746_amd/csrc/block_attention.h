@@ -13,11 +13,13 @@ struct AttentionArgs {
     __device__ int length(int b) const { return lengths ? min(max(lengths[b], 0), S) : S; }
 };
 
-// Lists of the queries of each block of keys.  bg = b G + g; a pair is query * NS + place in the query's selection.
+// The selection as the kernels read it: rows without the entries that do not count, and the lists of the queries of each block
+// of keys.  bg = b G + g; a pair is query * NS + place in the query's row.
 constexpr int PLAN_TILE = 256;           // queries that a workgroup of the builders takes
-constexpr int ITEM_ROWS = 512;           // rows (query, head) of an item: one workgroup of the kernels that walk lists
+constexpr int ITEM_ROWS = 512, ITEM_ROWS_MOST = 4096;          // rows (query, head) of an item: a workgroup of the kernel that walks lists
+constexpr int ITEMS = 2048;              // and about so many items, where that makes none shorter
 struct Plan {
-    uint64_t* valid = nullptr;           // [bg][Tq] entries of the selection that count, a bit each
+    int* rows = nullptr;                 // [bg][Tq][NS] the entries of a selection that count, nb behind them
     int* list = nullptr;                 // [bg][Tq NS] pairs, block after block, ascending inside a block
     int* start = nullptr;                // [bg][nb + 1] first pair of a block
     int* item_start = nullptr;           // [bg][nb + 1] first item of a block
@@ -27,13 +29,16 @@ struct Plan {
     size_t total = 0;
 };
 
-inline int item_pairs(int R) { return std::max(8, ITEM_ROWS / R); }
+inline int item_pairs(const AttentionArgs& a) {
+    const int64_t rows = (int64_t)a.B * a.G * a.Tq * a.NS * a.R;
+    return (int)std::max<int64_t>(8, std::min<int64_t>(ITEM_ROWS_MOST, std::max<int64_t>(ITEM_ROWS, rows / ITEMS)) / a.R);
+}
 
 inline Plan carve_plan(void* base, const AttentionArgs& a) {
     Plan p;
     const size_t bg = (size_t)a.B * a.G, pairs = (size_t)a.Tq * a.NS;
     p.tiles = (int)cdiv(a.Tq, PLAN_TILE);
-    p.item_pairs = item_pairs(a.R);
+    p.item_pairs = item_pairs(a);
     p.max_items = a.nb + (int)cdiv((int64_t)pairs, p.item_pairs);
     char* c = static_cast<char*>(base);
     size_t at = 0;
@@ -42,7 +47,7 @@ inline Plan carve_plan(void* base, const AttentionArgs& a) {
         at = align_up(at + bytes);
         return r;
     };
-    p.valid = reinterpret_cast<uint64_t*>(take(bg * a.Tq * 8));
+    p.rows = reinterpret_cast<int*>(take(bg * pairs * 4));
     p.list = reinterpret_cast<int*>(take(bg * pairs * 4));
     p.start = reinterpret_cast<int*>(take(bg * (a.nb + 1) * 4));
     p.item_start = reinterpret_cast<int*>(take(bg * (a.nb + 1) * 4));
@@ -64,6 +69,12 @@ inline int check_attention(const mst_attention_shape* s) {
     if ((int64_t)s->batch * s->kv_heads > 65535) return MST_ERR_SHAPE;
     if ((int64_t)s->queries * s->n_select * (s->heads / s->kv_heads) >= (int64_t(1) << 30)) return MST_ERR_SHAPE;
     return MST_OK;
+}
+
+// keys and values go to LDS by 32-bit offsets from the first key of a part
+inline int check_keys(const mst_attention_shape* s, const mst_heads* v, bool written) {
+    if (int e = check_heads(v, s->batch, s->keys, s->kv_heads, s->type, written)) return e;
+    return s->batch * (int64_t)s->keys > 0 && s->keys > 1 && v->token > (int64_t(1) << 22) ? MST_ERR_SHAPE : MST_OK;
 }
 
 inline AttentionArgs attention_args(const mst_attention_shape* s) {

@@ -1,155 +1,125 @@
 // Attention over selected blocks of keys, forward (mst_block_attention_fwd) and for single tokens (mst_block_attention_decode).
 //
-// Forward, from the lists of the plan: a wavefront keeps the keys of a block and its values, turned, in registers as operands
-// of the matrix instructions and walks the rows (query, head) that selected the block, sixteen at a time.  With S^T = K Q^T
-// a lane has the scores of one row and its probabilities are at once the operand of O^T = V^T P^T: the loop needs no LDS and no
-// barrier, and its loads are the sixteen queries.  Each (row, block) leaves its sum of values, maximum and sum of
-// weights in fp32; a second launch joins a row's blocks.  Work is in proportion to the pairs, whatever the rows select.
-#include "block_attention.h"
+// Forward: rows that own their results walk the union of their blocks (block_rows.h).  With S^T = K Q^T a lane has the scores of one
+// row, half of 32 keys, and its probabilities are at once the operand of O^T = V^T P^T; keys are read from LDS along their
+// rows and values across them.
+#include "block_rows.h"
 
 namespace mst {
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int FWD_THREADS = 256;
-
-// keys that a wavefront of the forward holds: a block, or a part of one whose keys and values fit the registers
-template <typename T, int DP> constexpr int keys_held() { return sizeof(T) == 4 && DP > 64 ? 32 : 64; }
-
-// rows of the groups of (batch, key head) that one launch takes: their partial results stay near the caches
-constexpr size_t PARTIAL_BYTES = size_t(256) << 20;
-
-struct Partials {
-    float* o;                            // [row-block][D]
-    float2* ml;                          // [row-block] maximum (base 2) and sum
-};
+// The weights of a row are 2^(score - reference), the reference a maximum that is left behind until a score passes it by more than
+// this: sums of weights stay far inside fp32, and the results are seldom scaled anew.
+constexpr float SLACK = 8.f;
 
 template <typename T, int DP, int KW>
-__global__ __launch_bounds__(FWD_THREADS) void k_attention_fwd(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v, int bg0, Partials out) {
-    constexpr int KT = KW / 16, DC = DP / 32, DT = DP / 16, KS = KW / 32, ROW = TileRow<T, DP>::stride;
-    __shared__ __align__(16) T vt[KW * ROW];
-    const int bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G, parts = a.BK / KW;
-    const int item = blockIdx.x / parts, part = blockIdx.x - item * parts;
-    if (item >= plan.item_start[(int64_t)bg * (a.nb + 1) + a.nb]) return;
-    const int2 it = plan.items[(int64_t)bg * plan.max_items + item];
-    const int last = min(it.y + plan.item_pairs, plan.start[(int64_t)bg * (a.nb + 1) + it.x + 1]);
-    const int len = a.length(b), key0 = it.x * a.BK + part * KW;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, quad = lane >> 4;
-
-    Operand<T> kf[KT][DC];               // rows = keys
+__global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void k_attention_fwd(AttentionArgs a, Plan plan, UnionSpace space, int tiles, Heads<const T> q, Heads<const T> k,
+                                                                  Heads<const T> v, Heads<T> o, float* __restrict__ lse) {
+    using Tiles = KeyTiles<T, DP, KW>;
+    constexpr int QC = DP / 16, DT = DP / 32, ST = KW / 32;
+    extern __shared__ __align__(16) char lds[];
+    const RowWork work(tiles);
+    const int bg = work.bg, b = bg / a.G, g = bg % a.G, len = a.length(b), tokens = COLS / a.R, t0 = work.tile * tokens;
+    uint32_t* list = reinterpret_cast<uint32_t*>(lds + space.list);
+    uint16_t* rows = reinterpret_cast<uint16_t*>(lds + space.rows);
+    const int n = make_union(a, plan.rows + (int64_t)bg * a.Tq * a.NS, t0, tokens, reinterpret_cast<uint32_t*>(lds + space.words), list, rows);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i32 = lane & 31, half = lane >> 5;
+    const int col = wave * 32 + i32, tok = col / a.R, t = t0 + tok, h = g * a.R + col - tok * a.R;
+    const bool there = tok < tokens && t < a.Tq;
+    const int p = len - a.Tq + t;
+    // a positive factor, so that the highest product is the highest score: its sign goes to the query
+    const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, 1.17549435e-38f);
+    Operand<T> qf[QC];
+    const T* qp = q.at(b, there ? t : 0, there ? h : 0);
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int c = 0; c < DC; ++c) {
-            const int key = key0 + kt * 16 + i16, d = c * 32 + quad * 8;
-            kf[kt][c] = key < len && d < a.D ? load_operand(k.at(b, key, g) + d) : zero_operand<T>();
-        }
-    for (int u = threadIdx.x; u < KW * (DP / 8); u += FWD_THREADS) {
-        const int r = u / (DP / 8), d = (u % (DP / 8)) * 8;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (key0 + r < len && d < a.D) load8(v.at(b, key0 + r, g) + d, x);
-        store8(&vt[r * ROW + d], x);
+    for (int c = 0; c < QC; ++c) {
+        qf[c] = there && c * 16 + half * 8 < a.D ? load_operand(qp + c * 16 + half * 8) : zero_operand<T>();
+        if (a.scale < 0.f) qf[c] = negated(qf[c]);
     }
-    __syncthreads();
-    Operand<T> vf[DT][KS];               // rows = components, contraction over the keys in the order of a product's rows
+    floatx16 acc[DT];
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) vf[dt][s] = across<ROW>(&vt[s * 32 * ROW + dt * 16], lane);
-
-    const int rows = (last - it.y) * a.R;
-    const int* list = plan.list + (int64_t)bg * a.Tq * a.NS;
-    const int64_t pair0 = (int64_t)blockIdx.y * a.Tq * a.NS;
-    const float scale2 = a.scale * LOG2E;
-    for (int r0 = wave * 16; r0 < rows; r0 += FWD_THREADS / 4) {
-        const int row = r0 + i16;
-        const bool there = row < rows;
-        const int e = there ? row / a.R : 0, h = there ? row - e * a.R : 0;
-        const int pair = list[it.y + e], t = pair / a.NS;
-        const T* qp = q.at(b, t, g * a.R + h);
-        Operand<T> qf[DC];
-#pragma unroll
-        for (int c = 0; c < DC; ++c) qf[c] = c * 32 + quad * 8 < a.D ? load_operand(qp + c * 32 + quad * 8) : zero_operand<T>();
-        floatx4 s[KT];
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            s[kt] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < DC; ++c) s[kt] = product(kf[kt][c], qf[c], s[kt]);
+    for (int d = 0; d < DT; ++d) acc[d] = zero16();
+    float m = -INFINITY, l = 0.f;
+    Cursor cursor(a, rows, tok, there);
+    const Tiles tiles_in(a, k, v, b, g, wave, lds);
+    const int parts = a.BK / KW, all = n * parts;
+    auto entry_of = [&](int i) { return (uint32_t)__builtin_amdgcn_readfirstlane(list[i]); };
+    uint32_t entry = n > 0 ? entry_of(0) : 0;
+    if (n > 0) tiles_in.load((int)(entry & 0xFFFF) * a.BK, len, 0);
+    for (int x = 0, i = 0, part = 0; x < all; ++x) {
+        wait_loads<0>();
+        lds_barrier();
+        const uint32_t now = entry;
+        const int key0 = (int)(now & 0xFFFF) * a.BK + part * KW;
+        const char* tile = lds + (x & 1) * Tiles::BUFFER;
+        const bool block_ends = part + 1 == parts;
+        if (x + 1 < all) {
+            if (block_ends) entry = entry_of(i + 1);
+            tiles_in.load(block_ends ? (int)(entry & 0xFFFF) * a.BK : key0 + KW, len, (x + 1) & 1);
         }
-        const int limit = len - a.Tq + t - key0;               // the row sees the keys 0 .. limit of this part
-        float m = -INFINITY;
+        part = block_ends ? 0 : part + 1;
+        i += block_ends;
+        if ((now >> (16 + wave)) & 1) {
+            const int limit = cursor.next == (int)(now & 0xFFFF) ? p - key0 : -1;          // the row sees the keys 0 .. limit of this part
+            floatx16 s[ST];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+            for (int st = 0; st < ST; ++st) {
+                s[st] = zero16();
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[kt][r] = kt * 16 + 4 * quad + r <= limit ? s[kt][r] * scale2 : -INFINITY;
-                m = fmaxf(m, s[kt][r]);
+                for (int c = 0; c < QC; ++c) s[st] = product32(along_row<T, DP>(tile, st * 32 + i32, c * 16 + half * 8), qf[c], s[st]);
             }
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float base = m == -INFINITY ? 0.f : m;           // (a part without visible keys)
-        float l = 0.f;
+            if (__any(limit < KW - 1 && limit >= 0)) {         // some row sees some of these keys, not all
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+                for (int st = 0; st < ST; ++st)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[kt][r] = exp2f(s[kt][r] - base);
-                l += s[kt][r];
+                    for (int r = 0; r < 16; ++r)
+                        if (st * 32 + 8 * (r / 4) + 4 * half + r % 4 > limit) s[st][r] = -INFINITY;
             }
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        Operand<T> pf[KS];
+            float top = s[0][0];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const float x[8] = {s[2 * ks][0], s[2 * ks][1], s[2 * ks][2], s[2 * ks][3], s[2 * ks + 1][0], s[2 * ks + 1][1], s[2 * ks + 1][2], s[2 * ks + 1][3]};
-            set_operand(pf[ks], x);
-        }
-        const int64_t at = ((pair0 + pair) * a.R + h) * parts + part;
-        float* po = out.o + at * a.D;
+            for (int e = 1; e < ST * 16; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
+            if (limit < 0) top = -INFINITY;
+            if (__any(top > m + SLACK)) {
+                const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : exp2_fast(m - to);
+                m = to;
+                l *= f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            floatx4 o = {0.f, 0.f, 0.f, 0.f};
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) o = product(vf[dt][ks], pf[ks], o);
-            const int d = dt * 16 + 4 * quad;
-            if (there && d < a.D) store4(po + d, o[0], o[1], o[2], o[3]);
-        }
-        if (there && quad == 0) out.ml[at] = make_float2(m, l);
-    }
-}
-
-// joins the blocks of a row: LANES lanes of four components
-template <typename T, int LANES>
-__global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a, Plan plan, int parts, int bg0, Partials in, Heads<T> o, float* __restrict__ lse) {
-    const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;    // (query, head) of a key head
-    if (row >= (int64_t)a.Tq * a.R) return;
-    const int t = (int)(row / a.R), h = (int)(row - (int64_t)t * a.R), bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G;
-    const uint64_t valid = plan.valid[(int64_t)bg * a.Tq + t];
-    const int64_t pair0 = (int64_t)blockIdx.y * a.Tq * a.NS + (int64_t)t * a.NS;
-    float m = -INFINITY;
-    for (uint64_t w = valid; w; w &= w - 1) {
-        const int64_t at = ((pair0 + __ffsll((unsigned long long)w) - 1) * a.R + h) * parts;
-        for (int p = 0; p < parts; ++p) m = fmaxf(m, in.ml[at + p].x);
-    }
-    float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint64_t w = valid; w; w &= w - 1) {
-        const int64_t at = ((pair0 + __ffsll((unsigned long long)w) - 1) * a.R + h) * parts;
-        for (int p = 0; p < parts; ++p) {
-            const float2 ml = in.ml[at + p];
-            if (ml.x == -INFINITY) continue;
-            const float f = exp2f(ml.x - m);
-            l += ml.y * f;
-            if (lane * 4 < a.D) {
-                const float4 y = *reinterpret_cast<const float4*>(in.o + (at + p) * a.D + lane * 4);
-                x[0] += y.x * f; x[1] += y.y * f; x[2] += y.z * f; x[3] += y.w * f;
+                    for (int r = 0; r < 16; ++r) acc[d][r] *= f;
             }
+            const float less = limit < 0 ? INFINITY : m;       // a row that sees nothing here: weights 2^-inf
+            Operand<T> pf[2 * ST];
+#pragma unroll
+            for (int u = 0; u < 2 * ST; ++u) {
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    w[e] = exp2_fast(__builtin_fmaf(s[u / 2][(u % 2) * 8 + e], scale2, -less));
+                    l += w[e];
+                }
+                set_operand(pf[u], w);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int u = 0; u < 2 * ST; ++u) acc[d] = product32(across_rows<T, DP>(tile + Tiles::TILE, u * 16, d * 32, lane), pf[u], acc[d]);
         }
+        if (block_ends) cursor.pass(a, (int)(now & 0xFFFF));
     }
-    const float n = l == 0.f ? 0.f : 1.f / l;                  // (a row without keys; not one whose sum is no number)
-    if (lane * 4 < a.D) store4(o.at(b, t, g * a.R + h) + lane * 4, x[0] * n, x[1] * n, x[2] * n, x[3] * n);
-    if (lane == 0) lse[((int64_t)b * a.H + g * a.R + h) * a.Tq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    if (!there) return;
+    l += __shfl_xor(l, 32);
+    const float scale = l == 0.f ? 0.f : 1.f / l;              // (a row without keys; not one whose sum is no number)
+    T* po = o.at(b, t, h);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int c = d * 32 + 2 * r + 4 * half;
+            if (c < a.D) store4(po + c, acc[d][r] * scale, acc[d][r + 1] * scale, acc[d][r + 2] * scale, acc[d][r + 3] * scale);
+        }
+    if (half == 0) lse[((int64_t)b * a.H + h) * a.Tq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
 // ---- single tokens: a workgroup per (query, key head, RT of its heads), a wavefront per selected block at a time.  A key is LANES
@@ -270,28 +240,7 @@ __global__ __launch_bounds__(DEC_THREADS) void k_attention_decode(AttentionArgs 
     }
 }
 
-size_t partial_bytes(const AttentionArgs& a, int parts, int n) {
-    return align_up((size_t)n * a.Tq * a.NS * a.R * parts * a.D * 4) + align_up((size_t)n * a.Tq * a.NS * a.R * parts * 8);
-}
-
-int parts_of(const mst_attention_shape* s) {
-    const int held = s->type == MST_F32 && s->head_dim > 64 ? 32 : 64;
-    return s->block <= held ? 1 : s->block / held;
-}
-
-// (batch, key head) that a launch takes
-int group_of(const AttentionArgs& a, int parts) {
-    const size_t one = partial_bytes(a, parts, 1);
-    return (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(one, 1)));
-}
-
 }  // namespace
-
-size_t attention_fwd_bytes(const mst_attention_shape* s) {
-    const AttentionArgs a = attention_args(s);
-    return std::max<size_t>(256, partial_bytes(a, parts_of(s), group_of(a, parts_of(s))));
-}
-
 }  // namespace mst
 
 extern "C" int mst_block_attention_fwd(const mst_attention_shape* s, const mst_heads* q, const mst_heads* k, const mst_heads* v, const void* plan_dev,
@@ -299,45 +248,38 @@ extern "C" int mst_block_attention_fwd(const mst_attention_shape* s, const mst_h
     using namespace mst;
     if (int e = check_attention(s)) return e;
     if (int e = check_heads(q, s->batch, s->queries, s->heads, s->type, false)) return e;
-    if (int e = check_heads(k, s->batch, s->keys, s->kv_heads, s->type, false)) return e;
-    if (int e = check_heads(v, s->batch, s->keys, s->kv_heads, s->type, false)) return e;
+    if (int e = check_keys(s, k, false)) return e;
+    if (int e = check_keys(s, v, false)) return e;
     if (int e = check_heads(o, s->batch, s->queries, s->heads, s->type, true)) return e;
     if (!plan_dev || !lse || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
-    if (ws_bytes < attention_fwd_bytes(s)) return MST_ERR_WORKSPACE;
+    if (ws_bytes < mst_block_attention_workspace_bytes(s, 0)) return MST_ERR_WORKSPACE;
     const AttentionArgs a = attention_args(s);
     if (a.B == 0 || a.Tq == 0) return MST_OK;
     const Plan plan = carve_plan(const_cast<void*>(plan_dev), a);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int parts = parts_of(s), group = group_of(a, parts);
-    const Partials part{static_cast<float*>(ws), reinterpret_cast<float2*>(static_cast<char*>(ws) + align_up((size_t)group * a.Tq * a.NS * a.R * parts * a.D * 4))};
+    const int tiles = (int)cdiv(a.Tq, COLS / a.R);
     int status = MST_OK;
     with_type(s->type, [&](auto type) {
         using T = decltype(type);
-        const Heads<const T> qh = heads_of<const T>(q), kh = heads_of<const T>(k), vh = heads_of<const T>(v);
-        const Heads<T> oh = heads_of<T>(o);
-        for (int bg = 0; bg < a.B * a.G && status == MST_OK; bg += group) {
-            const unsigned n = (unsigned)std::min(group, a.B * a.G - bg);
-            const dim3 grid((unsigned)(plan.max_items * parts), n);
-            if (a.nb > 0) {
-                if (a.D <= 64) {
-                    if (a.BK == 32) k_attention_fwd<T, 64, 32><<<grid, FWD_THREADS, 0, st>>>(a, plan, qh, kh, vh, bg, part);
-                    else k_attention_fwd<T, 64, 64><<<grid, FWD_THREADS, 0, st>>>(a, plan, qh, kh, vh, bg, part);
-                } else {
-                    constexpr int KW = keys_held<T, 128>();
-                    if (a.BK == 32) k_attention_fwd<T, 128, 32><<<grid, FWD_THREADS, 0, st>>>(a, plan, qh, kh, vh, bg, part);
-                    else k_attention_fwd<T, 128, KW><<<grid, FWD_THREADS, 0, st>>>(a, plan, qh, kh, vh, bg, part);
-                }
-            }
-            if (a.D <= 64) k_attention_join<T, 16><<<dim3((unsigned)cdiv((int64_t)a.Tq * a.R, 16), n), 256, 0, st>>>(a, plan, parts, bg, part, oh, lse);
-            else k_attention_join<T, 32><<<dim3((unsigned)cdiv((int64_t)a.Tq * a.R, 8), n), 256, 0, st>>>(a, plan, parts, bg, part, oh, lse);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) {
-                g_last_hip_error = (int)e;
-                status = MST_ERR_HIP;
-            }
-        }
+        auto launch = [&](auto dp, auto kw) {
+            constexpr int DP = decltype(dp)::value, KW = decltype(kw)::value;
+            const UnionSpace space(a, KeyTiles<T, DP, KW>::BYTES);
+            static uint64_t allowed = 0;
+            const void* kernel = reinterpret_cast<const void*>(&k_attention_fwd<T, DP, KW>);
+            status = allow_lds(kernel, LDS_BYTES, allowed);
+            if (status) return;
+            k_attention_fwd<T, DP, KW><<<(unsigned)(tiles * a.B * a.G), ROW_THREADS, space.total, st>>>(a, plan, space, tiles, heads_of<const T>(q), heads_of<const T>(k), heads_of<const T>(v), heads_of<T>(o), lse);
+        };
+        auto width = [&](auto kw) {
+            if (a.D <= 64) launch(std::integral_constant<int, 64>{}, kw);
+            else launch(std::integral_constant<int, 128>{}, kw);
+        };
+        if (a.BK == 32) width(std::integral_constant<int, 32>{});
+        else width(std::integral_constant<int, keys_at_once<T>(64)>{});
     });
-    return status;
+    if (status) return status;
+    MST_LAUNCH_CHECK();
+    return MST_OK;
 }
 
 extern "C" int mst_block_attention_decode(const mst_attention_shape* s, const mst_heads* q, const mst_heads* k, const mst_heads* v, const int32_t* blocks,
@@ -345,8 +287,8 @@ extern "C" int mst_block_attention_decode(const mst_attention_shape* s, const ms
     using namespace mst;
     if (int e = check_attention(s)) return e;
     if (int e = check_heads(q, s->batch, s->queries, s->heads, s->type, false)) return e;
-    if (int e = check_heads(k, s->batch, s->keys, s->kv_heads, s->type, false)) return e;
-    if (int e = check_heads(v, s->batch, s->keys, s->kv_heads, s->type, false)) return e;
+    if (int e = check_keys(s, k, false)) return e;
+    if (int e = check_keys(s, v, false)) return e;
     if (int e = check_heads(o, s->batch, s->queries, s->heads, s->type, true)) return e;
     if (!blocks || !aligned16(blocks) || !aligned16(lse)) return MST_ERR_ARG;
     const AttentionArgs a = attention_args(s);

@@ -1,30 +1,22 @@
 // Gradients of the attention over selected blocks (mst_block_attention_bwd).  With P = exp(scale q.k - lse),
 // delta = sum of dO O over a row and dP = dO V^T:  dS = P (dP - delta),  dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K.
 //
-// Both kernels walk the plan's lists as the forward does, with the keys and values of a block in registers.  The first takes
-// 32 rows at a time through LDS (Q and dO are read along the rows for S and dP and across them for dK and dV) and sums dK and
-// dV in registers: no two workgroups meet in one sum, and an item leaves its sums in fp32, which a last launch adds in the order of
-// the list.  The second works like the forward on S^T and leaves dQ of each (row, block).
-#include "block_attention.h"
+// The first kernel walks the plan's lists: a workgroup takes a stretch of the rows that selected a block, whose keys and values its
+// wavefronts keep in registers, 32 keys each.  The rows' Q and dO come straight to LDS, each from its own address, and are read
+// along the rows for S and dP and across them for dK and dV, whose sums stay in registers: no two workgroups meet in one
+// sum.  A block with one item is written as it is; the sums of several items are left in fp32 and added in the order of the list.
+// The second works like the forward: rows that own their dQ walk the union of their blocks.
+#include "block_rows.h"
 
 namespace mst {
-
-size_t attention_fwd_bytes(const mst_attention_shape* s);
-
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr int BWD_THREADS = 256, BWD_WAVES = BWD_THREADS / 64;
 constexpr size_t PARTIAL_BYTES = size_t(256) << 20;
-
-// keys that a wavefront holds: both kernels have keys, values and sums in registers
-__host__ __device__ constexpr int bwd_keys(bool f32, bool wide, int block) { return f32 || wide ? 32 : (block < 64 ? block : 64); }
 
 struct BwdArgs {
     const float* lse;                    // [B][H][Tq]
     const float* delta;                  // [B][H][Tq]
-    float* dq;                           // [pair][R][parts][D]
-    float* dkv;                          // [item][part][2][KW][D]
+    float* dkv;                          // [item][2][BK][D]
 };
 
 template <typename T, int LANES>
@@ -44,159 +36,192 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionArgs a, Heads<
     if (lane == 0) delta[((int64_t)b * a.H + h) * a.Tq + t] = s;
 }
 
-// what the workgroup of an item works on
-struct Item {
-    int bg, b, g, len, block, part, key0, first, last, index;
-    bool there;
-    __device__ Item(const AttentionArgs& a, const Plan& plan, int bg0, int KW) {
-        bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G;
-        const int parts = a.BK / KW;
-        index = blockIdx.x / parts, part = blockIdx.x - index * parts;
-        there = index < plan.item_start[(int64_t)bg * (a.nb + 1) + a.nb];
-        if (!there) return;
-        const int2 it = plan.items[(int64_t)bg * plan.max_items + index];
-        block = it.x, first = it.y;
-        last = min(first + plan.item_pairs, plan.start[(int64_t)bg * (a.nb + 1) + block + 1]);
-        len = a.length(b), key0 = block * a.BK + part * KW;
-    }
+// a workgroup of dK and dV: KP parts of 32 keys times RG groups of 32 rows, a wavefront each
+template <typename T, int DP, int KP>
+struct DkvTiles {
+    using R = Rows<T, DP>;
+    static constexpr int RG = KP == 4 ? 1 : 2, WAVES = KP * RG, THREADS = WAVES * 64, RT = RG * 32;
+    static constexpr int TILE = RT * R::BYTES, BUFFER = 2 * TILE, EACH = BUFFER / 1024 / WAVES;      // Q and dO of RT rows
+    static constexpr int ROWS = 2 * BUFFER, STATS = ROWS + 2 * RT * 8, BYTES = STATS + 2 * RT * 12;  // byte offsets: queries of rows, their statistics
+    static_assert(TILE % (EACH * 1024) == 0 && BUFFER * 2 >= (RG - 1) * KP * 32 * DP * 8, "whole loads; room for the sums of half the wavefronts");
 };
 
-template <typename T, int DP, int KW>
-__global__ __launch_bounds__(BWD_THREADS) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
-                                                               int bg0, BwdArgs w) {
-    constexpr int KT = KW / 16, DC = DP / 32, DT = DP / 16, ROW = TileRow<T, DP>::stride;
+template <typename T, int DP, int KP>
+__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+                                                                               Heads<const T> d_o, int bg0, BwdArgs w, Heads<T> dk_out, Heads<T> dv_out) {
+    using Tiles = DkvTiles<T, DP, KP>;
+    using R = Rows<T, DP>;
+    constexpr int QC = DP / 16, DT = DP / 32, RT = Tiles::RT, RG = Tiles::RG, EACH = Tiles::EACH;
     extern __shared__ __align__(16) char lds[];
-    const Item it(a, plan, bg0, KW);
-    if (!it.there) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, quad = lane >> 4;
-    T* qt = reinterpret_cast<T*>(lds) + wave * 2 * 32 * ROW;   // 32 rows of Q, then of dO, of this wavefront alone
-    T* dt_ = qt + 32 * ROW;
+    const int bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G, index = blockIdx.x;
+    if (index >= plan.item_start[(int64_t)bg * (a.nb + 1) + a.nb]) return;
+    const int2 it = plan.items[(int64_t)bg * plan.max_items + index];
+    const int block = it.x, first = it.y, end = plan.start[(int64_t)bg * (a.nb + 1) + block + 1], pairs = min(plan.item_pairs, end - first);
+    const bool alone = pairs == end - first && plan.start[(int64_t)bg * (a.nb + 1) + block] == first;      // the block's only item
+    const int len = a.length(b), key0 = block * a.BK;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i32 = lane & 31, half = lane >> 5;
+    const int kp = wave % KP, rg = wave / KP, key = key0 + kp * 32 + i32;
+    const float scale2 = a.scale * LOG2E, inv_r = 1.f / (float)a.R;
 
-    Operand<T> kf[KT][DC], vf[KT][DC];   // columns = keys
+    Operand<T> kf[QC], vf[QC];           // columns = keys
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+    for (int c = 0; c < QC; ++c) {
+        const int d = c * 16 + half * 8;
+        const bool there = key < len && d < a.D;
+        kf[c] = there ? load_operand(k.at(b, key, g) + d) : zero_operand<T>();
+        vf[c] = there ? load_operand(v.at(b, key, g) + d) : zero_operand<T>();
+    }
+    floatx16 dk[DT], dv[DT];             // rows = components, columns = keys
 #pragma unroll
-        for (int c = 0; c < DC; ++c) {
-            const int key = it.key0 + kt * 16 + i16, d = c * 32 + quad * 8;
-            const bool there = key < it.len && d < a.D;
-            kf[kt][c] = there ? load_operand(k.at(it.b, key, it.g) + d) : zero_operand<T>();
-            vf[kt][c] = there ? load_operand(v.at(it.b, key, it.g) + d) : zero_operand<T>();
-        }
-    floatx4 dk[KT][DT], dv[KT][DT];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) dk[kt][d] = dv[kt][d] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DT; ++d) dk[d] = dv[d] = zero16();
 
-    const int rows = (it.last - it.first) * a.R;
-    const int* list = plan.list + (int64_t)it.bg * a.Tq * a.NS;
-    const float scale2 = a.scale * LOG2E;
-    for (int r0 = wave * 32; r0 < rows; r0 += BWD_WAVES * 32) {
-        // lane l knows row l % 32: its query, log-sum, delta and the last key that it sees of this part (-1 behind the rows)
-        const int row = r0 + (lane & 31);
-        const bool there = row < rows;
-        const int e = there ? row / a.R : 0, h = there ? row - e * a.R : 0, t = list[it.first + e] / a.NS;
-        const int64_t stat = ((int64_t)it.b * a.H + it.g * a.R + h) * a.Tq + t;
-        const float lse2 = there ? w.lse[stat] * LOG2E : 0.f, delta = there ? w.delta[stat] : 0.f;
-        const int limit = there ? it.len - a.Tq + t - it.key0 : -1;
-        const int at = there ? t * a.R + h : -1;
-        __builtin_amdgcn_wave_barrier();
+    // The rows of step x are known two steps ahead (their queries, by the first RT threads) and their statistics one.
+    const int rows = pairs * a.R, steps = (rows + RT - 1) / RT;
+    const int* list = plan.list + (int64_t)bg * a.Tq * a.NS + first;
+    int2* row_th = reinterpret_cast<int2*>(lds + Tiles::ROWS);                     // [2][RT] query and head of a row
+    float* stats = reinterpret_cast<float*>(lds + Tiles::STATS);                   // [2][3][RT] log-sum, delta, last key that it sees
+    const bool scout = (int)threadIdx.x < RT;
+    const bool is_q = wave < Tiles::WAVES / 2;
+    const Heads<const T>& mine = is_q ? q : d_o;
+    const char* base = reinterpret_cast<const char*>(mine.at(b, 0, g * a.R));
+    const int64_t st = mine.st * (int64_t)sizeof(T), sh = mine.sh * (int64_t)sizeof(T);
+    const uint32_t to = lds_address(lds) + wave * (EACH * 1024);
+    const int my_row = (wave % (Tiles::WAVES / 2)) * EACH * R::PER_KB + lane / R::CH;
+    auto row_of = [&](int x) {           // query and head of the thread's row of step x; rows past the last are read as that
+        const int row = min(x * RT + (int)threadIdx.x, rows - 1);
+        const int e = (int)(((float)row + 0.5f) * inv_r);      // (rows are below 2^13, heads up to 64: never within rounding of the next one)
+        return make_int2(list[e] / a.NS, row - e * a.R);
+    };
+    struct Stat { float lse, delta; int limit; };
+    auto stat_of = [&](int2 th, int x) {
+        const int64_t at = ((int64_t)b * a.H + g * a.R + th.y) * a.Tq + th.x;
+        return Stat{w.lse[at] * LOG2E, w.delta[at], x * RT + (int)threadIdx.x < rows ? len - a.Tq + th.x - key0 : -1};
+    };
+    auto put_stat = [&](const Stat& s, int x) {
+        float* p = stats + (x & 1) * 3 * RT + threadIdx.x;
+        p[0] = s.lse, p[RT] = s.delta, p[2 * RT] = __int_as_float(s.limit);
+    };
+    auto load_rows = [&](int x) {
+        const int2* row = row_th + (x & 1) * RT;
 #pragma unroll
-        for (int u0 = 0; u0 < 32 * (DP / 8); u0 += 64) {
-            const int u = u0 + lane, r = u / (DP / 8), d = (u % (DP / 8)) * 8;
-            const int th = __shfl(at, r);
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (th >= 0 && d < a.D) {
-                const int tt = th / a.R, hh = th - tt * a.R;
-                load8(q.at(it.b, tt, it.g * a.R + hh) + d, x);
-                load8(d_o.at(it.b, tt, it.g * a.R + hh) + d, y);
-            }
-            store8(&qt[r * ROW + d], x);
-            store8(&dt_[r * ROW + d], y);
+        for (int i = 0; i < EACH; ++i) {
+            const int r = my_row + i * R::PER_KB, c = min(((lane % R::CH) ^ R::mix(r)) * 16, a.D * (int)sizeof(T) - 16);
+            const int2 th = row[r];
+            gather_to_lds(base + th.x * st + th.y * sh + c, to + (x & 1) * Tiles::BUFFER + i * 1024);
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        float lse_r[2][4], delta_r[2][4];
-        int limit_r[2][4];
+    };
+    int2 th2 = make_int2(0, 0);
+    Stat stat1{0.f, 0.f, -1};
+    if (scout) {
+        const int2 th0 = row_of(0), th1 = row_of(1);
+        th2 = row_of(2);
+        row_th[threadIdx.x] = th0, row_th[RT + threadIdx.x] = th1;
+        put_stat(stat_of(th0, 0), 0);
+        stat1 = stat_of(th1, 1);
+    }
+    lds_barrier();
+    load_rows(0);
+    for (int x = 0; x < steps; ++x) {
+        wait_loads<0>();
+        lds_barrier();
+        const char *qt = lds + (x & 1) * Tiles::BUFFER, *ot = qt + Tiles::TILE;
+        if (x + 1 < steps) load_rows(x + 1);
+        if (scout && x + 1 < steps) {
+            put_stat(stat1, x + 1);
+            row_th[(x & 1) * RT + threadIdx.x] = th2;
+            stat1 = stat_of(th2, x + 2);
+            th2 = row_of(x + 3);
+        }
+        floatx16 s = zero16(), dp = zero16();
 #pragma unroll
-        for (int rt = 0; rt < 2; ++rt)
+        for (int c = 0; c < QC; ++c) {
+            s = product32(along_row<T, DP>(qt, rg * 32 + i32, c * 16 + half * 8), kf[c], s);
+            dp = product32(along_row<T, DP>(ot, rg * 32 + i32, c * 16 + half * 8), vf[c], dp);
+        }
+        const float* stat = stats + (x & 1) * 3 * RT + rg * 32 + 4 * half;
+        Operand<T> pf[2], sf[2];         // P and dS, columns = keys, contraction over the rows
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                lse_r[rt][r] = __shfl(lse2, rt * 16 + 4 * quad + r);
-                delta_r[rt][r] = __shfl(delta, rt * 16 + 4 * quad + r);
-                limit_r[rt][r] = __shfl(limit, rt * 16 + 4 * quad + r);
-            }
-        Operand<T> pf[KT], sf[KT];       // P and dS, rows = keys, contraction over the 32 rows
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int u = 0; u < 2; ++u) {
             float p[8], ds[8];
 #pragma unroll
-            for (int rt = 0; rt < 2; ++rt) {
-                floatx4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < DC; ++c) {
-                    s = product(load_operand(&qt[(rt * 16 + i16) * ROW + c * 32 + quad * 8]), kf[kt][c], s);
-                    dp = product(load_operand(&dt_[(rt * 16 + i16) * ROW + c * 32 + quad * 8]), vf[kt][c], dp);
-                }
+            for (int e = 0; e < 8; e += 4) {
+                const float4 ls = *reinterpret_cast<const float4*>(stat + u * 16 + 2 * e), de = *reinterpret_cast<const float4*>(stat + RT + u * 16 + 2 * e);
+                const int4 li = *reinterpret_cast<const int4*>(stat + 2 * RT + u * 16 + 2 * e);
+                const float l4[4] = {ls.x, ls.y, ls.z, ls.w}, d4[4] = {de.x, de.y, de.z, de.w};
+                const int i4[4] = {li.x, li.y, li.z, li.w};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float x = kt * 16 + i16 <= limit_r[rt][r] ? exp2f(s[r] * scale2 - lse_r[rt][r]) : 0.f;
-                    p[rt * 4 + r] = x;
-                    ds[rt * 4 + r] = x * (dp[r] - delta_r[rt][r]);
+                    const int n = u * 8 + e + r;
+                    p[e + r] = kp * 32 + i32 <= i4[r] ? exp2_fast(__builtin_fmaf(s[n], scale2, -l4[r])) : 0.f;
+                    ds[e + r] = p[e + r] * (dp[n] - d4[r]);
                 }
             }
-            set_operand(pf[kt], p);
-            set_operand(sf[kt], ds);
+            set_operand(pf[u], p);
+            set_operand(sf[u], ds);
         }
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            const Operand<T> qc = across<ROW>(qt + d * 16, lane), oc = across<ROW>(dt_ + d * 16, lane);
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                dv[kt][d] = product(pf[kt], oc, dv[kt][d]);
-                dk[kt][d] = product(sf[kt], qc, dk[kt][d]);
+            for (int u = 0; u < 2; ++u) {
+                dv[d] = product32(across_rows<T, DP>(ot, rg * 32 + u * 16, d * 32, lane), pf[u], dv[d]);
+                dk[d] = product32(across_rows<T, DP>(qt, rg * 32 + u * 16, d * 32, lane), sf[u], dk[d]);
             }
-        }
     }
-    // the wavefronts' sums, one wavefront after the other: rows = keys 4 quad + r, columns = components
-    float* sums = reinterpret_cast<float*>(lds);               // [2][KW][DP]
-    for (int turn = 0; turn < BWD_WAVES; ++turn) {
+    if (RG == 2) {                       // the second group of rows to the first
         __syncthreads();
-        if (wave != turn) continue;
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+        float* sums = reinterpret_cast<float*>(lds) + kp * (DT * 32 * 64) + lane;
+        if (rg == 1)
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float* p = &sums[(kt * 16 + 4 * quad + r) * DP + d * 16 + i16];
-                    if (turn == 0) p[0] = dk[kt][d][r], p[KW * DP] = dv[kt][d][r];
-                    else p[0] += dk[kt][d][r], p[KW * DP] += dv[kt][d][r];
-                }
+                for (int r = 0; r < 16; ++r) sums[(d * 32 + r) * 64] = dk[d][r], sums[(d * 32 + 16 + r) * 64] = dv[d][r];
+        __syncthreads();
+        if (rg == 1) return;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dk[d][r] += sums[(d * 32 + r) * 64], dv[d][r] += sums[(d * 32 + 16 + r) * 64];
     }
-    __syncthreads();
-    const int parts = a.BK / KW;
-    float* out = w.dkv + (((int64_t)blockIdx.y * plan.max_items + it.index) * parts + it.part) * 2 * KW * a.D;
-    for (int u = threadIdx.x; u < 2 * KW * (a.D / 4); u += BWD_THREADS) {
-        const int r = u / (a.D / 4), d = (u - r * (a.D / 4)) * 4;
-        *reinterpret_cast<float4*>(out + r * a.D + d) = *reinterpret_cast<const float4*>(&sums[r * DP + d]);
+    if (alone) {
+        if (key >= a.S) return;
+        T *pk = dk_out.at(b, key, g), *pv = dv_out.at(b, key, g);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int c = d * 32 + 2 * r + 4 * half;
+                if (c >= a.D) continue;
+                store4(pk + c, dk[d][r] * a.scale, dk[d][r + 1] * a.scale, dk[d][r + 2] * a.scale, dk[d][r + 3] * a.scale);
+                store4(pv + c, dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]);
+            }
+        return;
     }
+    float* out = w.dkv + (((int64_t)blockIdx.y * plan.max_items + index) * 2 * a.BK + kp * 32 + i32) * a.D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int c = d * 32 + 2 * r + 4 * half;
+            if (c >= a.D) continue;
+            store4(out + c, dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]);
+            store4(out + (int64_t)a.BK * a.D + c, dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]);
+        }
 }
 
-// dK and dV of four components of a key: the items of its block, in order
+// dK and dV of four components of a key whose block has no item or several: their sum, in order
 template <typename T>
-__global__ __launch_bounds__(256) void k_attention_dkv_join(AttentionArgs a, Plan plan, int KW, int bg0, BwdArgs w, Heads<T> dk, Heads<T> dv) {
-    const int bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G, units = a.D / 4, parts = a.BK / KW;
+__global__ __launch_bounds__(256) void k_attention_dkv_join(AttentionArgs a, Plan plan, int bg0, BwdArgs w, Heads<T> dk, Heads<T> dv) {
+    const int bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G, units = a.D / 4;
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t key = u / units;
     if (key >= a.S) return;
-    const int d = (int)(u - key * units) * 4, block = (int)(key / a.BK), in = (int)(key - (int64_t)block * a.BK), part = in / KW;
+    const int d = (int)(u - key * units) * 4, block = (int)(key / a.BK), in = (int)(key - (int64_t)block * a.BK);
     const int i0 = plan.item_start[(int64_t)bg * (a.nb + 1) + block], i1 = plan.item_start[(int64_t)bg * (a.nb + 1) + block + 1];
+    if (i1 - i0 == 1) return;
     float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
     for (int i = i0; i < i1; ++i) {
-        const float* p = w.dkv + ((((int64_t)blockIdx.y * plan.max_items + i) * parts + part) * 2 * KW + (in - part * KW)) * a.D + d;
-        const float4 s = *reinterpret_cast<const float4*>(p), z = *reinterpret_cast<const float4*>(p + (int64_t)KW * a.D);
+        const float* p = w.dkv + (((int64_t)blockIdx.y * plan.max_items + i) * 2 * a.BK + in) * a.D + d;
+        const float4 s = *reinterpret_cast<const float4*>(p), z = *reinterpret_cast<const float4*>(p + (int64_t)a.BK * a.D);
         x[0] += s.x; x[1] += s.y; x[2] += s.z; x[3] += s.w;
         y[0] += z.x; y[1] += z.y; y[2] += z.z; y[3] += z.w;
     }
@@ -205,147 +230,145 @@ __global__ __launch_bounds__(256) void k_attention_dkv_join(AttentionArgs a, Pla
 }
 
 template <typename T, int DP, int KW>
-__global__ __launch_bounds__(BWD_THREADS) void k_attention_dq(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
-                                                              int bg0, BwdArgs w) {
-    constexpr int KT = KW / 16, DC = DP / 32, DT = DP / 16, KS = KW / 32, ROW = TileRow<T, DP>::stride;
-    __shared__ __align__(16) T kt_[KW * ROW];
-    const Item it(a, plan, bg0, KW);
-    if (!it.there) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, quad = lane >> 4, parts = a.BK / KW;
-    Operand<T> kf[KT][DC], vf[KT][DC], kc[DT][KS];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int c = 0; c < DC; ++c) {
-            const int key = it.key0 + kt * 16 + i16, d = c * 32 + quad * 8;
-            const bool there = key < it.len && d < a.D;
-            kf[kt][c] = there ? load_operand(k.at(it.b, key, it.g) + d) : zero_operand<T>();
-            vf[kt][c] = there ? load_operand(v.at(it.b, key, it.g) + d) : zero_operand<T>();
-        }
-    for (int u = threadIdx.x; u < KW * (DP / 8); u += BWD_THREADS) {
-        const int r = u / (DP / 8), d = (u % (DP / 8)) * 8;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (it.key0 + r < it.len && d < a.D) load8(k.at(it.b, it.key0 + r, it.g) + d, x);
-        store8(&kt_[r * ROW + d], x);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) kc[dt][s] = across<ROW>(&kt_[s * 32 * ROW + dt * 16], lane);
-
-    const int rows = (it.last - it.first) * a.R;
-    const int* list = plan.list + (int64_t)it.bg * a.Tq * a.NS;
-    const int64_t pair0 = (int64_t)blockIdx.y * a.Tq * a.NS;
+__global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void k_attention_dq(AttentionArgs a, Plan plan, UnionSpace space, int tiles, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+                                                                 Heads<const T> d_o, const float* __restrict__ lse, const float* __restrict__ delta, Heads<T> dq) {
+    using Tiles = KeyTiles<T, DP, KW>;
+    constexpr int QC = DP / 16, DT = DP / 32, ST = KW / 32;
+    extern __shared__ __align__(16) char lds[];
+    const RowWork work(tiles);
+    const int bg = work.bg, b = bg / a.G, g = bg % a.G, len = a.length(b), tokens = COLS / a.R, t0 = work.tile * tokens;
+    uint32_t* list = reinterpret_cast<uint32_t*>(lds + space.list);
+    uint16_t* rows = reinterpret_cast<uint16_t*>(lds + space.rows);
+    const int n = make_union(a, plan.rows + (int64_t)bg * a.Tq * a.NS, t0, tokens, reinterpret_cast<uint32_t*>(lds + space.words), list, rows);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i32 = lane & 31, half = lane >> 5;
+    const int col = wave * 32 + i32, tok = col / a.R, t = t0 + tok, h = g * a.R + col - tok * a.R;
+    const bool there = tok < tokens && t < a.Tq;
+    const int p = len - a.Tq + t;
     const float scale2 = a.scale * LOG2E;
-    for (int r0 = wave * 16; r0 < rows; r0 += BWD_WAVES * 16) {
-        const int row = r0 + i16;
-        const bool there = row < rows;
-        const int e = there ? row / a.R : 0, h = there ? row - e * a.R : 0;
-        const int pair = list[it.first + e], t = pair / a.NS;
-        const int64_t stat = ((int64_t)it.b * a.H + it.g * a.R + h) * a.Tq + t;
-        const float lse2 = w.lse[stat] * LOG2E, delta = w.delta[stat];
-        const T *qp = q.at(it.b, t, it.g * a.R + h), *op = d_o.at(it.b, t, it.g * a.R + h);
-        Operand<T> qf[DC], of[DC];
+    const int64_t stat = ((int64_t)b * a.H + (there ? h : 0)) * a.Tq + (there ? t : 0);
+    const float lse2 = lse[stat] * LOG2E, dl = delta[stat];
+    Operand<T> qf[QC], of[QC];
+    const T *qp = q.at(b, there ? t : 0, there ? h : 0), *op = d_o.at(b, there ? t : 0, there ? h : 0);
 #pragma unroll
-        for (int c = 0; c < DC; ++c) {
-            const int d = c * 32 + quad * 8;
-            qf[c] = d < a.D ? load_operand(qp + d) : zero_operand<T>();
-            of[c] = d < a.D ? load_operand(op + d) : zero_operand<T>();
+    for (int c = 0; c < QC; ++c) {
+        const int d = c * 16 + half * 8;
+        qf[c] = there && d < a.D ? load_operand(qp + d) : zero_operand<T>();
+        of[c] = there && d < a.D ? load_operand(op + d) : zero_operand<T>();
+    }
+    floatx16 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = zero16();
+    Cursor cursor(a, rows, tok, there);
+    const Tiles tiles_in(a, k, v, b, g, wave, lds);
+    const int parts = a.BK / KW, all = n * parts;
+    auto entry_of = [&](int i) { return (uint32_t)__builtin_amdgcn_readfirstlane(list[i]); };
+    uint32_t entry = n > 0 ? entry_of(0) : 0;
+    if (n > 0) tiles_in.load((int)(entry & 0xFFFF) * a.BK, len, 0);
+    for (int x = 0, i = 0, part = 0; x < all; ++x) {
+        wait_loads<0>();
+        lds_barrier();
+        const uint32_t now = entry;
+        const int key0 = (int)(now & 0xFFFF) * a.BK + part * KW;
+        const char* tile = lds + (x & 1) * Tiles::BUFFER;
+        const bool block_ends = part + 1 == parts;
+        if (x + 1 < all) {
+            if (block_ends) entry = entry_of(i + 1);
+            tiles_in.load(block_ends ? (int)(entry & 0xFFFF) * a.BK : key0 + KW, len, (x + 1) & 1);
         }
-        const int limit = it.len - a.Tq + t - it.key0;
-        Operand<T> sf[KS];
+        part = block_ends ? 0 : part + 1;
+        i += block_ends;
+        if ((now >> (16 + wave)) & 1) {
+            const int limit = cursor.next == (int)(now & 0xFFFF) ? p - key0 : -1;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            float ds[8];
+            for (int st = 0; st < ST; ++st) {
+                floatx16 s = zero16(), dp = zero16();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int kt = 2 * ks + half;
-                floatx4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < DC; ++c) {
-                    s = product(kf[kt][c], qf[c], s);
-                    dp = product(vf[kt][c], of[c], dp);
+                for (int c = 0; c < QC; ++c) {
+                    s = product32(along_row<T, DP>(tile, st * 32 + i32, c * 16 + half * 8), qf[c], s);
+                    dp = product32(along_row<T, DP>(tile + Tiles::TILE, st * 32 + i32, c * 16 + half * 8), of[c], dp);
                 }
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    ds[half * 4 + r] = kt * 16 + 4 * quad + r <= limit ? exp2f(s[r] * scale2 - lse2) * (dp[r] - delta) : 0.f;
+                for (int u = 0; u < 2; ++u) {
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int r = u * 8 + e;
+                        y[e] = st * 32 + 8 * (r / 4) + 4 * half + r % 4 <= limit ? exp2_fast(__builtin_fmaf(s[r], scale2, -lse2)) * (dp[r] - dl) : 0.f;
+                    }
+                    Operand<T> sf;
+                    set_operand(sf, y);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) acc[d] = product32(across_rows<T, DP>(tile, st * 32 + u * 16, d * 32, lane), sf, acc[d]);
+                }
             }
-            set_operand(sf[ks], ds);
         }
-        float* out = w.dq + (((pair0 + pair) * a.R + h) * parts + it.part) * a.D;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) x = product(kc[dt][ks], sf[ks], x);
-            const int d = dt * 16 + 4 * quad;
-            if (there && d < a.D) store4(out + d, x[0], x[1], x[2], x[3]);
-        }
+        if (block_ends) cursor.pass(a, (int)(now & 0xFFFF));
     }
-}
-
-template <typename T, int LANES>
-__global__ __launch_bounds__(256) void k_attention_dq_join(AttentionArgs a, Plan plan, int parts, int bg0, BwdArgs w, Heads<T> dq) {
-    const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-    if (row >= (int64_t)a.Tq * a.R || lane * 4 >= a.D) return;
-    const int t = (int)(row / a.R), h = (int)(row - (int64_t)t * a.R), bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G;
-    const int64_t pair0 = (int64_t)blockIdx.y * a.Tq * a.NS + (int64_t)t * a.NS;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint64_t v = plan.valid[(int64_t)bg * a.Tq + t]; v; v &= v - 1) {
-        const float* p = w.dq + ((pair0 + __ffsll((unsigned long long)v) - 1) * a.R + h) * parts * a.D + lane * 4;
-        for (int i = 0; i < parts; ++i) {
-            const float4 y = *reinterpret_cast<const float4*>(p + (int64_t)i * a.D);
-            x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
+    if (!there) return;
+    T* po = dq.at(b, t, h);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int c = d * 32 + 2 * r + 4 * half;
+            if (c < a.D) store4(po + c, acc[d][r] * a.scale, acc[d][r + 1] * a.scale, acc[d][r + 2] * a.scale, acc[d][r + 3] * a.scale);
         }
-    }
-    store4(dq.at(b, t, g * a.R + h) + lane * 4, x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
 }
 
 struct BwdSpace {
-    int KW, parts, group, max_items;
-    size_t delta, dq, total;
+    int group, max_items;                // (batch, key head) that a launch takes
+    size_t delta, total;
 };
 
 BwdSpace bwd_space(const mst_attention_shape* s) {
     const AttentionArgs a = attention_args(s);
     BwdSpace w;
-    w.KW = bwd_keys(s->type == MST_F32, s->head_dim > 64, s->block);
-    w.parts = a.BK / w.KW;
     w.max_items = carve_plan(nullptr, a).max_items;
     w.delta = align_up((size_t)a.B * a.H * a.Tq * 4);
-    const size_t dq1 = (size_t)a.Tq * a.NS * a.R * w.parts * a.D * 4, dkv1 = (size_t)w.max_items * 2 * a.BK * a.D * 4;
-    w.group = (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(dq1 + dkv1, 1)));
-    w.dq = align_up(w.group * dq1);
-    w.total = std::max<size_t>(256, w.delta + w.dq + align_up(w.group * dkv1));
+    const size_t one = (size_t)w.max_items * 2 * a.BK * a.D * 4;
+    w.group = (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(one, 1)));
+    w.total = std::max<size_t>(256, w.delta + align_up(w.group * one));
     return w;
 }
 
-template <typename T, int DP, int KW>
-int launch_bwd(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, const Heads<const T>& q, const Heads<const T>& k, const Heads<const T>& v, const Heads<const T>& d_o, const Heads<T>& dq, const Heads<T>& dk, const Heads<T>& dv, const BwdArgs& w, hipStream_t st) {
-    constexpr int ROW = TileRow<T, DP>::stride;
-    constexpr int tiles = BWD_WAVES * 2 * 32 * ROW * (int)sizeof(T), sums = 2 * KW * DP * 4, lds = tiles > sums ? tiles : sums;
-    static_assert(lds <= 160 * 1024, "LDS of a CU");
+template <typename T, int DP, int KP>
+int launch_dkv(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, const Heads<const T>& q, const Heads<const T>& k, const Heads<const T>& v, const Heads<const T>& d_o,
+               const Heads<T>& dk, const Heads<T>& dv, const BwdArgs& w, hipStream_t st) {
+    using Tiles = DkvTiles<T, DP, KP>;
+    static_assert(Tiles::BYTES <= LDS_BYTES, "LDS of a CU");
     static uint64_t allowed = 0;
-    const void* kernel = reinterpret_cast<const void*>(&k_attention_dkv<T, DP, KW>);
-    if (int e = allow_lds(kernel, lds, allowed)) return e;
+    if (int e = allow_lds(reinterpret_cast<const void*>(&k_attention_dkv<T, DP, KP>), Tiles::BYTES, allowed)) return e;
     for (int bg = 0; bg < a.B * a.G; bg += sp.group) {
         const unsigned n = (unsigned)std::min(sp.group, a.B * a.G - bg);
-        const dim3 grid((unsigned)(plan.max_items * sp.parts), n);
-        if (a.nb > 0 && a.Tq > 0) {
-            k_attention_dkv<T, DP, KW><<<grid, BWD_THREADS, lds, st>>>(a, plan, q, k, v, d_o, bg, w);
-            MST_LAUNCH_CHECK();
-            k_attention_dq<T, DP, KW><<<grid, BWD_THREADS, 0, st>>>(a, plan, q, k, v, d_o, bg, w);
-            MST_LAUNCH_CHECK();
-        }
-        if (a.S > 0) k_attention_dkv_join<T><<<dim3((unsigned)cdiv((int64_t)a.S * (a.D / 4), 256), n), 256, 0, st>>>(a, plan, KW, bg, w, dk, dv);
+        k_attention_dkv<T, DP, KP><<<dim3((unsigned)plan.max_items, n), Tiles::THREADS, Tiles::BYTES, st>>>(a, plan, q, k, v, d_o, bg, w, dk, dv);
         MST_LAUNCH_CHECK();
-        constexpr int L = DP / 4;
-        if (a.Tq > 0) k_attention_dq_join<T, L><<<dim3((unsigned)cdiv((int64_t)a.Tq * a.R, 256 / L), n), 256, 0, st>>>(a, plan, sp.parts, bg, w, dq);
+        k_attention_dkv_join<T><<<dim3((unsigned)cdiv((int64_t)a.S * (a.D / 4), 256), n), 256, 0, st>>>(a, plan, bg, w, dk, dv);
         MST_LAUNCH_CHECK();
     }
     return MST_OK;
+}
+
+template <typename T, int DP, int KW>
+int launch_dq(const AttentionArgs& a, const Plan& plan, const Heads<const T>& q, const Heads<const T>& k, const Heads<const T>& v, const Heads<const T>& d_o, const BwdArgs& w,
+              const Heads<T>& dq, hipStream_t st) {
+    const UnionSpace space(a, KeyTiles<T, DP, KW>::BYTES);
+    static uint64_t allowed = 0;
+    if (int e = allow_lds(reinterpret_cast<const void*>(&k_attention_dq<T, DP, KW>), LDS_BYTES, allowed)) return e;
+    const int tiles = (int)cdiv(a.Tq, COLS / a.R);
+    k_attention_dq<T, DP, KW><<<(unsigned)(tiles * a.B * a.G), ROW_THREADS, space.total, st>>>(a, plan, space, tiles, q, k, v, d_o, w.lse, w.delta, dq);
+    MST_LAUNCH_CHECK();
+    return MST_OK;
+}
+
+// f(DP, parts of 32 keys of a block)
+template <typename F>
+int with_sizes(const AttentionArgs& a, F&& f) {
+    auto block = [&](auto dp) {
+        if (a.BK == 32) return f(dp, std::integral_constant<int, 1>{});
+        if (a.BK == 64) return f(dp, std::integral_constant<int, 2>{});
+        return f(dp, std::integral_constant<int, 4>{});
+    };
+    return a.D <= 64 ? block(std::integral_constant<int, 64>{}) : block(std::integral_constant<int, 128>{});
 }
 
 }  // namespace
@@ -354,8 +377,7 @@ int launch_bwd(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, con
 extern "C" size_t mst_block_attention_workspace_bytes(const mst_attention_shape* s, int backward) {
     using namespace mst;
     if (check_attention(s)) return 0;
-    const size_t f = attention_fwd_bytes(s);
-    return backward ? std::max(f, bwd_space(s).total) : f;
+    return backward ? bwd_space(s).total : 256;
 }
 
 extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_heads* q, const mst_heads* k, const mst_heads* v, const void* plan_dev,
@@ -365,7 +387,7 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
     if (int e = check_attention(s)) return e;
     const struct { const mst_heads* v; bool key, written; } views[] = {{q, false, false}, {k, true, false}, {v, true, false}, {o, false, false}, {d_o, false, false}, {dq, false, true}, {dk, true, true}, {dv, true, true}};
     for (const auto& x : views)
-        if (int e = check_heads(x.v, s->batch, x.key ? s->keys : s->queries, x.key ? s->kv_heads : s->heads, s->type, x.written)) return e;
+        if (int e = x.key ? check_keys(s, x.v, x.written) : check_heads(x.v, s->batch, s->queries, s->heads, s->type, x.written)) return e;
     if (!plan_dev || !lse || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
     const BwdSpace sp = bwd_space(s);
     if (ws_bytes < sp.total) return MST_ERR_WORKSPACE;
@@ -374,7 +396,7 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
     const Plan plan = carve_plan(const_cast<void*>(plan_dev), a);
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* base = static_cast<char*>(ws);
-    const BwdArgs w{lse, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + sp.delta), reinterpret_cast<float*>(base + sp.delta + sp.dq)};
+    const BwdArgs w{lse, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + sp.delta)};
     int status = MST_OK;
     with_type(s->type, [&](auto type) {
         using T = decltype(type);
@@ -392,13 +414,12 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
                 return;
             }
         }
-        constexpr bool f32 = sizeof(T) == 4;
-        if (a.D <= 64) {
-            if (a.BK == 32) status = launch_bwd<T, 64, 32>(a, plan, sp, qh, kh, vh, doh, dqh, dkh, dvh, w, st);
-            else status = launch_bwd<T, 64, bwd_keys(f32, false, 64)>(a, plan, sp, qh, kh, vh, doh, dqh, dkh, dvh, w, st);
-        } else {
-            status = launch_bwd<T, 128, 32>(a, plan, sp, qh, kh, vh, doh, dqh, dkh, dvh, w, st);
-        }
+        status = with_sizes(a, [&](auto dp, auto kp) {
+            constexpr int DP = decltype(dp)::value, KP = decltype(kp)::value;
+            if (a.S > 0)
+                if (int e = launch_dkv<T, DP, KP>(a, plan, sp, qh, kh, vh, doh, dkh, dvh, w, st)) return e;
+            return a.Tq == 0 ? (int)MST_OK : launch_dq<T, DP, keys_at_once<T>(KP * 32)>(a, plan, qh, kh, vh, doh, w, dqh, st);
+        });
     });
     return status;
 }

@@ -297,23 +297,23 @@ __global__ __launch_bounds__(FEW_THREADS) void k_block_select_few(AttentionArgs 
 
 // ---- plan.  A tile of 256 queries marks its queries in one bit word of 256 a block: a query has a block once at most, so the number
 // of bits below its own is its place among the tile's.  Counts per tile, their sums over the tiles, then every pair to its place.
-__device__ inline void mark_tile(const AttentionArgs& a, const int* __restrict__ blocks, int bg, int t, int len, uint32_t* bits, uint64_t* valid_out) {
+__device__ inline void mark_tile(const AttentionArgs& a, const int* __restrict__ blocks, int bg, int t, int len, uint32_t* bits, int* rows_out) {
     for (int i = threadIdx.x; i < a.nb * 8; i += PLAN_TILE) bits[i] = 0;
     __syncthreads();
     if (t < a.Tq) {
         const int p = len - a.Tq + t, own = p >= 0 ? p / a.BK : -1;
         const int* row = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
-        uint64_t valid = 0;
-        int last = -1;
+        int* out = rows_out + ((int64_t)bg * a.Tq + t) * a.NS;
+        int last = -1, n = 0;
         for (int s = 0; s < a.NS; ++s) {
             const int j = row[s];
             if (j > last && j <= own) {
-                valid |= 1ull << s;
+                out[n++] = j;
                 atomicOr(&bits[j * 8 + (threadIdx.x >> 5)], 1u << (threadIdx.x & 31));
                 last = j;
             }
         }
-        if (valid_out) valid_out[(int64_t)bg * a.Tq + t] = valid;
+        for (; n < a.NS; ++n) out[n] = a.nb;
     }
     __syncthreads();
 }
@@ -321,7 +321,7 @@ __device__ inline void mark_tile(const AttentionArgs& a, const int* __restrict__
 __global__ __launch_bounds__(PLAN_TILE) void k_plan_count(AttentionArgs a, const int* __restrict__ blocks, Plan plan) {
     extern __shared__ uint32_t bits[];
     const int bg = blockIdx.y, t = blockIdx.x * PLAN_TILE + threadIdx.x;
-    mark_tile(a, blocks, bg, t, a.length(bg / a.G), bits, plan.valid);
+    mark_tile(a, blocks, bg, t, a.length(bg / a.G), bits, plan.rows);
     int* row = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
     for (int j = threadIdx.x; j < a.nb; j += PLAN_TILE) {
         int c = 0;
@@ -383,19 +383,22 @@ __global__ __launch_bounds__(1024) void k_plan_sums(AttentionArgs a, Plan plan) 
     if (threadIdx.x == 0) start[a.nb] = done.x, item_start[a.nb] = done.y;
 }
 
-__global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, const int* __restrict__ blocks, Plan plan) {
+__global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan plan) {
     extern __shared__ uint32_t bits[];
     const int bg = blockIdx.y, t = blockIdx.x * PLAN_TILE + threadIdx.x;
-    mark_tile(a, blocks, bg, t, a.length(bg / a.G), bits, nullptr);
+    for (int i = threadIdx.x; i < a.nb * 8; i += PLAN_TILE) bits[i] = 0;
+    __syncthreads();
+    const int word = threadIdx.x >> 5;
+    const int* row = plan.rows + ((int64_t)bg * a.Tq + t) * a.NS;
+    if (t < a.Tq)
+        for (int s = 0; s < a.NS && row[s] < a.nb; ++s) atomicOr(&bits[row[s] * 8 + word], 1u << (threadIdx.x & 31));
+    __syncthreads();
     if (t >= a.Tq) return;
-    const int* row = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
     const int* before = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
     const int* start = plan.start + (int64_t)bg * (a.nb + 1);
     int* list = plan.list + (int64_t)bg * a.Tq * a.NS;
-    uint64_t valid = plan.valid[(int64_t)bg * a.Tq + t];
-    const int word = threadIdx.x >> 5;
-    for (; valid; valid &= valid - 1) {
-        const int s = __ffsll((unsigned long long)valid) - 1, j = row[s];
+    for (int s = 0; s < a.NS && row[s] < a.nb; ++s) {
+        const int j = row[s];
         int at = start[j] + before[j] + __popc(bits[j * 8 + word] & ((1u << (threadIdx.x & 31)) - 1));
         for (int w = 0; w < word; ++w) at += __popc(bits[j * 8 + w]);
         list[at] = t * a.NS + s;
@@ -476,7 +479,7 @@ extern "C" int mst_block_plan(const mst_attention_shape* s, const int32_t* block
     k_plan_sums<<<(unsigned)(a.B * a.G), 1024, 0, st>>>(a, plan);
     MST_LAUNCH_CHECK();
     if (plan.tiles > 0) {
-        k_plan_fill<<<grid, PLAN_TILE, lds, st>>>(a, blocks, plan);
+        k_plan_fill<<<grid, PLAN_TILE, lds, st>>>(a, plan);
         MST_LAUNCH_CHECK();
     }
     return MST_OK;

@@ -11,6 +11,7 @@ constexpr int HEAD_DIM_MAX = 128;        // of the attention; head_dim is a mult
 constexpr int SELECT_MAX = 64;           // blocks a query may select: one bit each in a word
 constexpr int KEY_BLOCKS_MAX = 2048;     // blocks of a sequence: their bit words for 256 queries are 64 KB of LDS
 constexpr int64_t HEADS_MAX = 1 << 16;
+constexpr int LDS_BYTES = 160 * 1024;     // of a CU
 
 template <typename T>
 struct Heads {                           // element strides of [batch][token][head][head_dim]
@@ -40,6 +41,17 @@ inline bool is_type(mst_dtype t) { return t == MST_F32 || t == MST_BF16; }
 
 struct bf16 { uint16_t bits; };          // storage of a bfloat16
 
+// {bf16(a), bf16(b)}, to nearest even: the instruction of cvt_pk_bf16 from the compiler itself, which knows that a number straight out
+// of an exponential has to be waited for (written as asm it has been read too early)
+__device__ inline uint32_t pack2(float a, float b) {
+    typedef float float2v __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 v = __builtin_convertvector((float2v{a, b}), bf16x2);
+    uint32_t r;
+    __builtin_memcpy(&r, &v, 4);
+    return r;
+}
+
 __device__ inline float to_float(float x) { return x; }
 __device__ inline float to_float(bf16 x) { return __uint_as_float((uint32_t)x.bits << 16); }
 
@@ -63,17 +75,17 @@ __device__ inline void store8(float* p, const float (&x)[8]) {
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 __device__ inline void store8(bf16* p, const float (&x)[8]) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(cvt_pk_bf16(x[0], x[1]), cvt_pk_bf16(x[2], x[3]), cvt_pk_bf16(x[4], x[5]), cvt_pk_bf16(x[6], x[7]));
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
 }
 __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ inline void store4(bf16* p, float a, float b, float c, float d) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(a, b), cvt_pk_bf16(c, d));
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(a, b), pack2(c, d));
 }
 
-// ---- operands of a 16 x 16 x 32 product.  Lane l holds row (or column) l % 16 and the eight contraction indices of lane
-// group l / 16.  Which eight is free as long as both operands agree: where an operand comes out of another product
-// (16 x 16, column l % 16, rows 4 (l / 16) + r), the indices of group q are 4q .. 4q+3 of one tile of 16 and 4q .. 4q+3 of the
-// next.  bfloat16: one instruction; fp32: eight of 16 x 16 x 4, in full precision.
+// ---- operands of a 32 x 32 x 16 product.  Lane l holds row (or column) l % 32 and the eight contraction indices of half l / 32.
+// Which eight is free as long as both operands agree.  Rows of a result: 8 (r / 4) + 4 (l / 32) + r % 4 in register r, column
+// l % 32; where a result is the next operand, half h of sixteen indices has 4h .. 4h+3 and 8 + 4h .. 8 + 4h+3, which are its registers
+// 8i .. 8i+7 in order.  bfloat16: one instruction; fp32: eight of 32 x 32 x 2, in full precision.
 template <typename T> struct Operand;
 template <> struct Operand<bf16> { bf16x8 v; };
 template <> struct Operand<float> { float v[8]; };
@@ -105,52 +117,102 @@ __device__ inline Operand<float> load_operand(const float* p) {
 // probabilities and their gradients as operands: bfloat16 operands round them to nearest, an error of the size of the
 // rounding of the values that they multiply; sums and statistics are taken before
 __device__ inline void set_operand(Operand<bf16>& o, const float (&x)[8]) {
-    const uint4 w = make_uint4(cvt_pk_bf16(x[0], x[1]), cvt_pk_bf16(x[2], x[3]), cvt_pk_bf16(x[4], x[5]), cvt_pk_bf16(x[6], x[7]));
+    const uint4 w = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
     __builtin_memcpy(&o.v, &w, 16);
 }
 __device__ inline void set_operand(Operand<float>& o, const float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) o.v[i] = x[i];
 }
-__device__ inline floatx4 product(const Operand<bf16>& a, const Operand<bf16>& b, floatx4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+__device__ inline floatx16 product32(const Operand<bf16>& a, const Operand<bf16>& b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
 }
-__device__ inline floatx4 product(const Operand<float>& a, const Operand<float>& b, floatx4 c) {
+__device__ inline floatx16 product32(const Operand<float>& a, const Operand<float>& b, floatx16 c) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], c, 0, 0, 0);
     return c;
 }
-
-// LDS rows of vectors that are read along the rows and across them: 16 bytes of padding, so that the four rows that a
-// transposing read takes at once lie in different banks
-template <typename T, int DP> struct TileRow { static constexpr int stride = DP + 16 / (int)sizeof(T); };
-
-// operand with column (or row) l % 16 of 16 columns and the rows 4q .. 4q+3 and 16 + 4q .. 16 + 4q+3 of 32 LDS rows as the
-// contraction indices; `tile`: first of the 32 rows at the first of the columns
-template <int STRIDE>
-__device__ inline Operand<bf16> across(const bf16* tile, int lane) {
+__device__ inline floatx16 zero16() {
+    floatx16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+// ---- LDS tiles of vectors that are read along the rows and across them.  A row is CH chunks of 16 bytes; chunk c of row r is
+// kept at place c ^ mix(r): eight consecutive rows then have a chunk in eight different places (a read along the rows takes
+// 16 bytes from each), and four consecutive rows, from a multiple of four on, have four neighbouring chunks in different ones (a
+// transposing read of 32 columns).  Lanes that load straight to LDS write a row's places in order and pick the chunks.
+template <typename T, int DP>
+struct Rows {
+    static constexpr int CH = DP * (int)sizeof(T) / 16, BYTES = CH * 16, PER_KB = 64 / CH;      // rows of one load of a wavefront
+    __device__ static int mix(int r) { return CH == 8 ? ((r & 2) << 1) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3); }
+    __device__ static int at(int r, int c) { return r * BYTES + ((c ^ mix(r)) << 4); }
+};
+template <int DP>
+__device__ inline Operand<bf16> along(const char* tile, int r, int d) {            // components d .. d+7 of row r
+    Operand<bf16> o;
+    o.v = *reinterpret_cast<const bf16x8*>(tile + Rows<bf16, DP>::at(r, d >> 3));
+    return o;
+}
+template <int DP>
+__device__ inline Operand<float> along_f32(const char* tile, int r, int d) {
+    Operand<float> o;
+    const float4 a = *reinterpret_cast<const float4*>(tile + Rows<float, DP>::at(r, d >> 2)), b = *reinterpret_cast<const float4*>(tile + Rows<float, DP>::at(r, (d >> 2) + 1));
+    o.v[0] = a.x; o.v[1] = a.y; o.v[2] = a.z; o.v[3] = a.w;
+    o.v[4] = b.x; o.v[5] = b.y; o.v[6] = b.z; o.v[7] = b.w;
+    return o;
+}
+// column d0 + l % 32 of the rows r0 .. r0+15 as contraction indices, in the order of a result; r0 a multiple of 16
+template <int DP>
+__device__ inline Operand<bf16> across(const char* tile, int r0, int d0, int lane) {
     typedef short short4v __attribute__((ext_vector_type(4)));
-    const int q = lane >> 4, i = lane & 15;
-    const bf16* p = tile + (4 * q + (i >> 2)) * STRIDE + (i & 3) * 4;
     typedef __attribute__((address_space(3))) short4v* lds4;
+    const int i = lane & 15, r = r0 + 4 * (lane >> 5) + (i >> 2), d = d0 + ((lane >> 4) & 1) * 16 + (i & 3) * 4;
     union { short4v s[2]; bf16x8 v; } u;
-    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
-    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 16 * STRIDE));
+    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tile + Rows<bf16, DP>::at(r, d >> 3) + (d & 7) * 2));
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tile + Rows<bf16, DP>::at(r + 8, d >> 3) + (d & 7) * 2));
     Operand<bf16> o;
     o.v = u.v;
     return o;
 }
-template <int STRIDE>
-__device__ inline Operand<float> across(const float* tile, int lane) {
-    const int q = lane >> 4, i = lane & 15;
+template <int DP>
+__device__ inline Operand<float> across_f32(const char* tile, int r0, int d0, int lane) {
+    const int d = d0 + (lane & 31), r = r0 + 4 * (lane >> 5);
     Operand<float> o;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        o.v[j] = tile[(4 * q + j) * STRIDE + i];
-        o.v[4 + j] = tile[(16 + 4 * q + j) * STRIDE + i];
+        o.v[j] = *reinterpret_cast<const float*>(tile + Rows<float, DP>::at(r + j, d >> 2) + (d & 3) * 4);
+        o.v[4 + j] = *reinterpret_cast<const float*>(tile + Rows<float, DP>::at(r + 8 + j, d >> 2) + (d & 3) * 4);
     }
     return o;
 }
+template <typename T, int DP>
+__device__ inline Operand<T> along_row(const char* tile, int r, int d) {
+    if constexpr (sizeof(T) == 2) return along<DP>(tile, r, d);
+    else return along_f32<DP>(tile, r, d);
+}
+template <typename T, int DP>
+__device__ inline Operand<T> across_rows(const char* tile, int r0, int d0, int lane) {
+    if constexpr (sizeof(T) == 2) return across<DP>(tile, r0, d0, lane);
+    else return across_f32<DP>(tile, r0, d0, lane);
+}
+// 16 bytes per lane from its own address to LDS, lane l to lds + 16 l
+__device__ __forceinline__ void gather_to_lds(const void* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)(const char*)p);
+}
+template <typename T> __device__ inline Operand<T> negated(Operand<T> o) {
+    uint32_t w[sizeof(o.v) / 4];
+    __builtin_memcpy(w, &o.v, sizeof(o.v));
+#pragma unroll
+    for (auto& x : w) x ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    __builtin_memcpy(&o.v, w, sizeof(o.v));
+    return o;
+}
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }    // results below 2^-126 are 0
 
 template <int WIDTH>
 __device__ inline float lanes_sum(float x) {        // over groups of WIDTH consecutive lanes
