@@ -540,9 +540,8 @@ typedef struct {
 
 /* Summaries of complete blocks of keys: sums_dev int8 [batch x kv_heads x ceil(keys / block) x head_dim] and scales_dev fp32
  * [batch x kv_heads x ceil(keys / block)], the sum of a block's keys in 8 bits a component and the value of its unit, a
- * power of two.  With E = floor(log2 max |key|) over the block (taken into -100 .. 100; components that are not finite count
- * as 0):  k8 = round(key 2^(6 - E)) into -127 .. 127,  s = sum over the keys,  r = max(0, floor(log2 max |s|) - 6),
- * sums = round(s 2^-r) into -127 .. 127,  scales = 2^(E - 6 + r); rounding is to nearest even.  A block of zeros has E = -100.
+ * power of two.  With E = floor(log2 max |key|) over the block (taken into -100 .. 100):  k8 = round(key 2^(6 - E)) into -127 .. 127,  s = sum over the keys,  r = max(0, floor(log2 max |s|) - 6),
+ * sums = round(s 2^-r) into -127 .. 127,  scales = 2^(E - 6 + r); rounding is to nearest even.  A block of zeros has E = -100; keys that are not finite give some sums.
  * Only blocks that the last new_tokens keys of their sequence completed are written (new_tokens >= keys: all complete blocks), so a
  * cache's summaries are kept up token by token; entries of other blocks stay as they are. */
 int mst_key_summary(const mst_attention_shape* shape, const mst_heads* k, int8_t* sums_dev, float* scales_dev,

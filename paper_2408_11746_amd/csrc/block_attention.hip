@@ -78,7 +78,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
             float top = s[0][0];
 #pragma unroll
             for (int e = 1; e < ST * 16; ++e) top = fmaxf(top, s[e / 16][e % 16]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * scale2;
+            top = apart<32>(top, [](float u, float w) { return fmaxf(u, w); }) * scale2;
             if (limit < 0) top = -INFINITY;
             if (__any(top > m + SLACK)) {
                 const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : exp2_fast(m - to);
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
         if (block_ends) cursor.pass(a, (int)(now & 0xFFFF));
     }
     if (!there) return;
-    l += __shfl_xor(l, 32);
+    l = apart<32>(l, [](float u, float w) { return u + w; });
     const float scale = l == 0.f ? 0.f : 1.f / l;              // (a row without keys; not one whose sum is no number)
     T* po = o.at(b, t, h);
 #pragma unroll

@@ -15,8 +15,13 @@ __device__ inline float power_of_two(int e) { return __int_as_float((e + 127) <<
 // floor(log2 x) of fp32 x >= 0, below -126 for zero and subnormal numbers
 __device__ inline int exponent(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }
 __device__ inline int unit_exponent(float top) { return min(max(exponent(top), -E_MAX), E_MAX); }
-__device__ inline float finite_or_0(float x) { return fabsf(x) <= 3.402823466e38f ? x : 0.f; }
-__device__ inline int round8(float x) { return (int)fminf(fmaxf(rintf(x), -127.f), 127.f); }
+// Whole numbers of 8 bits: x is cut at 127 units, and a number between -2^22 and 2^22 added to ROUND has its value, rounded to
+// nearest even, in the low bits.  (x is finite; what is not gives some number of 8 bits.)
+constexpr float ROUND = 12582912.f;      // 1.5 2^23
+__device__ inline int round8_bits(float x, float unit, float most) {       // ROUND's bits + round8(x unit); most = 127 / unit
+    return __float_as_int(__builtin_fmaf(__builtin_amdgcn_fmed3f(x, -most, most), unit, ROUND));
+}
+constexpr int ROUND_BITS = 0x4B400000;
 // shift that brings whole numbers up to `top` into 8 bits
 __device__ inline int sum_shift(int top) { return top > 0 ? max(31 - __clz(top) - 6, 0) : 0; }
 
@@ -38,296 +43,426 @@ __global__ __launch_bounds__(SUM_THREADS) void k_key_summary(AttentionArgs a, He
     const bool mine = k0 < per;
     const T* base = k.at(b, (int64_t)j * a.BK, g) + u * 8;
     for (int i = threadIdx.x; i < a.D; i += SUM_THREADS) part[i] = 0;
-    float top = 0.f;
-    if (mine)
-        for (int r = k0; r < a.BK; r += per) {
-            float x[8];
-            load8(base + r * k.st, x);
+    constexpr int PIECES = HEAD_DIM_MAX / 16;                  // 128 keys of 128 components: eight pieces a thread
+    float x[PIECES][8], top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(finite_or_0(x[e])));
-        }
+    for (int i = 0; i < PIECES; ++i) {
+        const int r = k0 + i * per;
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+        if (mine && r < a.BK) load8(base + r * k.st, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        if (i * per < a.BK)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+    top = lanes_max<64>(top);
     if ((threadIdx.x & 63) == 0) top4[threadIdx.x >> 6] = top;
     __syncthreads();
     const int E = unit_exponent(fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])));
-    const float unit = power_of_two(6 - E);
+    const float unit = power_of_two(6 - E), limit = 127.f * power_of_two(E - 6);
     if (mine) {
         int s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int r = k0; r < a.BK; r += per) {
-            float x[8];
-            load8(base + r * k.st, x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += round8(finite_or_0(x[e]) * unit);
-        }
+        for (int i = 0; i < PIECES; ++i)
+            if (i * per < a.BK)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] += round8_bits(x[i][e], unit, limit) - ROUND_BITS;
 #pragma unroll
         for (int e = 0; e < 8; ++e) atomicAdd(&part[u * 8 + e], s[e]);
     }
     __syncthreads();
     const int v = (int)threadIdx.x < a.D ? part[threadIdx.x] : 0;
-    int peak = abs(v);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) peak = max(peak, __shfl_xor(peak, d));
+    const int peak = lanes_max<64>(abs(v));
     if ((threadIdx.x & 63) == 0) peak4[threadIdx.x >> 6] = peak;
     __syncthreads();
     const int shift = sum_shift(max(max(peak4[0], peak4[1]), max(peak4[2], peak4[3])));
     const int64_t at = (int64_t)bg * a.nb + j;
-    if ((int)threadIdx.x < a.D) sums[at * a.D + threadIdx.x] = (int8_t)round8((float)v * power_of_two(-shift));
+    if ((int)threadIdx.x < a.D) sums[at * a.D + threadIdx.x] = (int8_t)(round8_bits((float)v, power_of_two(-shift), 127.f * power_of_two(shift)) - ROUND_BITS);
     if (threadIdx.x == 0) scales[at] = power_of_two(E - 6 + shift);
 }
 
-// ---- a query in 8 bits: the sixteen lanes of a query hold eight components each (lane c: 8c ..), over its R heads
-template <typename T>
-__device__ inline uint2 query8(const AttentionArgs& a, const Heads<const T>& q, int b, int t, int g, int c, bool there) {
-    const bool mine = there && c * 8 < a.D;
-    float top = 0.f;
-    if (mine)
-        for (int h = 0; h < a.R; ++h) {
-            float x[8];
-            load8(q.at(b, t, g * a.R + h) + c * 8, x);
+// ---- a query in 8 bits: the sixteen lanes of a query hold eight components each (lane c: 8c ..), HB of its R heads at a time.  Every
+// lane loads (one without a query or components of its own reads others'), so that the loads of several queries are on their way
+// together.
+template <typename T, int HB>
+struct Query8 {
+    const T* base;
+    int64_t sh;
+    int R;
+    bool mine;
+    Operand<T> raw[HB];
+    __device__ Query8() {}
+    __device__ Query8(const AttentionArgs& a, const Heads<const T>& q, int b, int t, int g, int c, bool there) : sh(q.sh), R(a.R), mine(there && c * 8 < a.D) {
+        base = q.at(b, there ? t : 0, g * a.R) + min(c * 8, a.D - 8);
+        fetch(0);
+    }
+    __device__ void fetch(int h0) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(finite_or_0(x[e])));
+        for (int i = 0; i < HB; ++i) raw[i] = load_operand(base + min(h0 + i, R - 1) * sh);
+    }
+    __device__ static void numbers(const Operand<bf16>& o, float (&x)[8]) {
+        uint4 w;
+        __builtin_memcpy(&w, &o.v, 16);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+    __device__ static void numbers(const Operand<float>& o, float (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = o.v[e];
+    }
+    __device__ uint2 value() {
+        float top = 0.f, x[8];
+        for (int h = 0; h < R; h += HB) {
+            if (h > 0) fetch(h);
+#pragma unroll
+            for (int i = 0; i < HB; ++i) {                     // (heads past the last are the last one again)
+                numbers(raw[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+            }
+        }
+        const int E = unit_exponent(lanes_max<16>(mine ? top : 0.f));
+        const float unit = power_of_two(6 - E), most = 127.f * power_of_two(E - 6);
+        uint32_t s[8];                                         // (modulo 2^32)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = 0u - (uint32_t)R * (uint32_t)ROUND_BITS;
+        for (int h = 0; h < R; h += HB) {
+            if (R > HB) fetch(h);
+#pragma unroll
+            for (int i = 0; i < HB; ++i)
+                if (h + i < R) {
+                    numbers(raw[i], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += (uint32_t)round8_bits(x[e], unit, most);
+                }
+        }
+        int peak = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) peak = max(peak, abs((int)s[e]));
+        const int shift = sum_shift(lanes_max<16>(mine ? peak : 0));
+        const float back = power_of_two(-shift), limit = 127.f * power_of_two(shift);
+        uint32_t w[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(round8_bits((float)(int)s[e], back, limit) & 255) << (8 * (e & 3));
+        return mine ? make_uint2(w[0], w[1]) : make_uint2(0, 0);
+    }
+};
+
+// ---- selection, a wavefront per 16 queries.  The 8-bit matrix instructions give the scores of 16 blocks at a time, four of them
+// to each of a query's four lanes, which keeps the KK highest of its own in order: one median a place.  The four lists are
+// merged; with the lowest score that is taken known, a second walk over the scores takes the blocks above it and,
+// on a tie, the first that are due, in ascending order.  Summaries go through LDS, 64 blocks at a time for the workgroup's 64
+// queries; the scores of up to 256 blocks stay in registers for the second walk (HELD), of more are formed again.
+typedef int intx4 __attribute__((ext_vector_type(4)));
+// the KK highest of the lists of lanes APART from each other, in order; the lists descend
+template <int KK, int APART>
+__device__ inline void merge_best(float (&x)[KK]) {
+    float y[KK], z[KK];
+#pragma unroll
+    for (int e = 0; e < KK; ++e) {
+        const Both b = both_lanes<APART>(__float_as_uint(x[e]));
+        y[e] = __uint_as_float(b.first), z[KK - 1 - e] = __uint_as_float(b.second);
+    }
+#pragma unroll
+    for (int e = 0; e < KK; ++e) x[e] = fmaxf(y[e], z[e]);     // first up, then down (or the other way round)
+#pragma unroll
+    for (int d = KK / 2; d >= 1; d >>= 1)
+#pragma unroll
+        for (int e = 0; e < KK; ++e)
+            if (!(e & d)) {
+                const float hi = fmaxf(x[e], x[e + d]), lo = fminf(x[e], x[e + d]);
+                x[e] = hi, x[e + d] = lo;
+            }
+}
+constexpr int SELECT_THREADS = 256, SELECT_CHUNK = 64, SELECT_HELD = 256;
+template <typename T, int KK, int HB, bool HELD>
+__global__ __launch_bounds__(SELECT_THREADS) void k_block_select(AttentionArgs a, Heads<const T> q, const int8_t* __restrict__ sums,
+                                                                 const float* __restrict__ scales, int* __restrict__ blocks) {
+    __shared__ __align__(16) uint2 q8_all[SELECT_THREADS / 64][16][17];    // a query's 128 components; 8 bytes of padding
+    __shared__ __align__(16) uint2 rows[SELECT_CHUNK][17];                 // summaries likewise
+    __shared__ __align__(16) float units[SELECT_CHUNK];
+    const int bg = blockIdx.y, b = bg / a.G, g = bg % a.G, len = a.length(b);
+    const int lane = threadIdx.x & 63, i = lane & 15, quad = lane >> 4, t0 = blockIdx.x * (SELECT_THREADS / 4) + (threadIdx.x >> 6) * 16;
+    uint2(*q8)[17] = q8_all[threadIdx.x >> 6];
+    const int wanted = a.NS - 1;
+    const int last_p = len - a.Tq + min((int)(blockIdx.x + 1) * (SELECT_THREADS / 4), a.Tq) - 1;
+    const int most = wanted > 0 && last_p >= 0 ? last_p / a.BK : 0;        // candidates of the workgroup's last query
+    // 8 D / 8 pieces of eight bytes of 64 rows that lie one behind the other, four a thread at most; past the candidates the last piece again
+    const int pieces = a.D / 8;
+    const uint2* from = reinterpret_cast<const uint2*>(sums + (int64_t)bg * a.nb * a.D);
+    const float* scl = scales + (int64_t)bg * a.nb;
+    uint2 staged[4];
+    float staged_unit = 0.f;
+    auto fetch = [&](int j0) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int u = n * SELECT_THREADS + (int)threadIdx.x;
+            if (n * SELECT_THREADS < SELECT_CHUNK * pieces) staged[n] = from[min(j0 * pieces + u, most * pieces - 1)];
+        }
+        staged_unit = scl[min(j0 + (int)threadIdx.x % SELECT_CHUNK, most - 1)];
+    };
+    auto put = [&]() {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int u = n * SELECT_THREADS + (int)threadIdx.x;
+            if (u < SELECT_CHUNK * pieces) rows[u / pieces][u % pieces] = staged[n];
+        }
+        if (threadIdx.x < SELECT_CHUNK) units[threadIdx.x] = staged_unit;
+    };
+    if (most > 0) fetch(0);
+    for (int u = threadIdx.x; u < SELECT_CHUNK * 17; u += SELECT_THREADS) rows[0][u] = make_uint2(0, 0);
+    {
+        Query8<T, HB> queries[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int tq = t0 + r * 4 + quad;
+            queries[r] = Query8<T, HB>(a, q, b, tq, g, i, tq < a.Tq && len - a.Tq + tq >= 0);
         }
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float unit = power_of_two(6 - unit_exponent(top));
-    int s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (mine)
-        for (int h = 0; h < a.R; ++h) {
-            float x[8];
-            load8(q.at(b, t, g * a.R + h) + c * 8, x);
+        for (int r = 0; r < 4; ++r) q8[r * 4 + quad][i] = queries[r].value();
+    }
+    __syncthreads();
+    intx4 qb[2];                                               // column = query, 16 components of every 64 to a lane
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += round8(finite_or_0(x[e]) * unit);
+    for (int c = 0; c < 2; ++c) {
+        const uint2 lo = q8[i][c * 8 + quad * 2], hi = q8[i][c * 8 + quad * 2 + 1];
+        qb[c] = intx4{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+    }
+    const int t = t0 + i, p = len - a.Tq + t;
+    const bool there = t < a.Tq && p >= 0;
+    const int mine = there ? p / a.BK : 0;                     // candidates: the blocks before it
+    auto scores = [&](int j0, int at, float* v) {              // of the blocks j0 + 4 quad + r, which lie at `at` of the chunk
+        intx4 c = {0, 0, 0, 0}, ab;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (h * 64 < a.D) {
+                const uint2 lo = rows[at + i][h * 8 + quad * 2], hi = rows[at + i][h * 8 + quad * 2 + 1];
+                ab = intx4{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+                c = __builtin_amdgcn_mfma_i32_16x16x64_i8(ab, qb[h], c, 0, 0, 0);
+            }
+        const float4 u = *reinterpret_cast<const float4*>(&units[at + 4 * quad]);
+        const float unit[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = j0 + 4 * quad + r < mine ? (float)c[r] * unit[r] : -INFINITY;
+    };
+    float best[KK];                                            // descending
+#pragma unroll
+    for (int e = 0; e < KK; ++e) best[e] = -INFINITY;
+    auto insert = [&](const float* v) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (__any(v[r] > best[KK - 1])) {
+#pragma unroll
+                for (int e = KK - 1; e > 0; --e) best[e] = __builtin_amdgcn_fmed3f(v[r], best[e - 1], best[e]);
+                best[0] = fmaxf(v[r], best[0]);
+            }
+    };
+    float held[HELD ? SELECT_HELD / 4 : 4];
+    constexpr int CHUNKS = HELD ? SELECT_HELD / SELECT_CHUNK : 1;
+    auto chunk_in = [&](int j0, bool again) {                  // the chunk to LDS, the next one on its way
+        __syncthreads();
+        put();
+        __syncthreads();
+        if (j0 + SELECT_CHUNK < most) fetch(j0 + SELECT_CHUNK);
+        else if (again) fetch(0);
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int n = 0; n < CHUNKS; ++n)
+            if (n * SELECT_CHUNK < most) {
+                chunk_in(n * SELECT_CHUNK, false);
+#pragma unroll
+                for (int s = 0; s < SELECT_CHUNK / 16; ++s)
+                    if (n * SELECT_CHUNK + s * 16 < most) {
+                        scores(n * SELECT_CHUNK + s * 16, s * 16, held + n * 16 + s * 4);
+                        insert(held + n * 16 + s * 4);
+                    }
+            }
+    } else {
+        for (int j0 = 0; j0 < most; j0 += SELECT_CHUNK) {
+            chunk_in(j0, true);
+            for (int s = 0; s < SELECT_CHUNK && j0 + s < most; s += 16) {
+                scores(j0 + s, s, held);
+                insert(held);
+            }
         }
-    int peak = 0;
+    }
+    merge_best<KK, 16>(best);
+    merge_best<KK, 32>(best);
+    float least = -INFINITY;                                   // the lowest that is taken
 #pragma unroll
-    for (int e = 0; e < 8; ++e) peak = max(peak, abs(s[e]));
+    for (int e = 0; e < KK; ++e)
+        if (e == wanted - 1) least = best[e];
+    int due = 0;                                               // how many equal to it are taken
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) peak = max(peak, __shfl_xor(peak, d));
-    const float back = power_of_two(-sum_shift(peak));
-    uint32_t w[2] = {0, 0};
+    for (int e = 0; e < KK; ++e) due += (e < wanted && best[e] == least) ? 1 : 0;
+    int* out = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
+    int n_out = 0;
+    auto take = [&](int j0, const float* v) {
+        uint32_t both = 0;                                     // bits of the query's sixteen blocks: above, equal
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(round8((float)s[e] * back) & 255) << (8 * (e & 3));
-    return make_uint2(w[0], w[1]);
+        for (int r = 0; r < 4; ++r) both |= (v[r] > least ? 1u : v[r] == least && v[r] > -INFINITY ? 0x10000u : 0u) << r;
+        both <<= 4 * quad;
+        both = apart<16>(both, [](uint32_t x, uint32_t y) { return x | y; });
+        both = apart<32>(both, [](uint32_t x, uint32_t y) { return x | y; });
+        uint32_t above = both & 0xFFFF, equal = both >> 16;
+        while (__popc(equal) > due) equal &= ~(1u << (31 - __clz(equal)));
+        due -= __popc(equal);
+        above |= equal;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int bit = 4 * quad + r;
+            if (above >> bit & 1) out[n_out + __popc(above & ((1u << bit) - 1))] = j0 + bit;
+        }
+        n_out += __popc(above);
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int n = 0; n < SELECT_HELD / 16; ++n)
+            if (n * 16 < most) take(n * 16, held + n * 4);
+    } else {
+        for (int j0 = 0; j0 < most; j0 += SELECT_CHUNK) {
+            chunk_in(j0, false);
+            for (int s = 0; s < SELECT_CHUNK && j0 + s < most; s += 16) {
+                scores(j0 + s, s, held);
+                take(j0 + s, held);
+            }
+        }
+    }
+    if (t < a.Tq)
+        for (int e = n_out + quad; e < a.NS; e += 4) out[e] = e == n_out && there ? mine : -1;
 }
 
-// scores as unsigned numbers of the same order; 0 (below every score) for no candidate
+// ---- selection for few queries: a workgroup per query and key head.  Every thread scores blocks; then one wavefront takes the scores
+// to registers, U a lane, finds the lowest that is taken bit by bit, counting the scores at or above a trial value in its lane
+// masks, and writes the blocks in order: no barrier in 32 steps.
+constexpr int FEW_THREADS = 256;
+// scores as unsigned numbers of the same order, above 0
 __device__ inline uint32_t ordered(float x) {
     x += 0.f;                                                  // -0 and +0 are one score
     const uint32_t u = __float_as_uint(x);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
-
-// ---- selection, a wavefront per 64 queries.  16 blocks at a time the scores come from the 8-bit matrix instructions, go through
-// LDS and to the query's own lane, which keeps the KK highest in order: one median a place.  With the lowest of them known a second
-// walk over the same scores takes the blocks above it and, on a tie, the first that are due, in ascending order.
-typedef int intx4 __attribute__((ext_vector_type(4)));
-template <typename T, int KK>
-__global__ __launch_bounds__(64) void k_block_select(AttentionArgs a, Heads<const T> q, const int8_t* __restrict__ sums,
-                                                     const float* __restrict__ scales, int* __restrict__ blocks) {
-    __shared__ __align__(16) uint2 q8[64][17];                 // a query's 128 components; 8 bytes of padding
-    __shared__ uint32_t score[16][65];
-    const int bg = blockIdx.y, b = bg / a.G, g = bg % a.G, len = a.length(b);
-    const int lane = threadIdx.x, i = lane & 15, quad = lane >> 4;
-    const int t0 = blockIdx.x * 64;
-    for (int r = quad; r < 64; r += 4) q8[r][i] = query8(a, q, b, t0 + r, g, i, t0 + r < a.Tq && len - a.Tq + t0 + r >= 0);
-    __syncthreads();
-    intx4 qb[4][2];                                            // column = query, 16 components of every 64 to a lane
+template <int U>
+__device__ inline void take_best(const uint32_t* score, int candidates, int wanted, int own, int NS, int* __restrict__ out) {
+    const int lane = threadIdx.x;
+    uint32_t v[U];                                             // block u 64 + lane; 0: none
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int u = 0; u < U; ++u) v[u] = u * 64 + lane < candidates ? score[u * 64 + lane] : 0u;
+    uint32_t least = 0;                                        // the highest value with at least `wanted` scores at or above it
+    int at_least = candidates;
+    if (wanted < candidates)
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t trial = least | (1u << bit);
+            int c = 0;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const uint2 lo = q8[n * 16 + i][c * 8 + quad * 2], hi = q8[n * 16 + i][c * 8 + quad * 2 + 1];
-            qb[n][c] = intx4{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
+            for (int u = 0; u < U; ++u) c += __popcll(__ballot(v[u] >= trial));
+            if (c >= wanted) least = trial, at_least = c;
+            if (c == wanted) break;
         }
-    const int t = t0 + lane, p = len - a.Tq + t;
-    const bool there = t < a.Tq && p >= 0;
-    const int mine = there ? p / a.BK : 0;                     // candidates: the blocks before it
-    const int last_t = min(t0 + 63, a.Tq - 1), last_p = len - a.Tq + last_t;
-    const int most = last_p >= 0 ? last_p / a.BK : 0;
-    const int8_t* srow = sums + (int64_t)bg * a.nb * a.D;
-    const float* scl = scales + (int64_t)bg * a.nb;
-    const int wanted = a.NS - 1;
-    auto scores = [&](int j0) {
-        intx4 ab[2] = {intx4{0, 0, 0, 0}, intx4{0, 0, 0, 0}};  // row = block
-        const int j = j0 + i;
+    int equal = 0;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int d = c * 64 + quad * 16;
-            if (j < most && d < a.D) {                         // (rows are whole eights of bytes, at eights)
-                const uint2* s = reinterpret_cast<const uint2*>(srow + (int64_t)j * a.D + d);
-                const uint2 lo = s[0], hi = d + 8 < a.D ? s[1] : make_uint2(0, 0);
-                ab[c] = intx4{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
-            }
-        }
-        float unit[4];
+    for (int u = 0; u < U; ++u) equal += __popcll(__ballot(v[u] == least && v[u] != 0));
+    int due = wanted - (at_least - equal), n = 0;              // of the equal ones, the first so many
 #pragma unroll
-        for (int r = 0; r < 4; ++r) unit[r] = j0 + 4 * quad + r < most ? scl[j0 + 4 * quad + r] : 0.f;
-        __syncthreads();                                       // (one wavefront: the reads of the scores before these)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            intx4 c = {0, 0, 0, 0};
-            c = __builtin_amdgcn_mfma_i32_16x16x64_i8(ab[0], qb[n][0], c, 0, 0, 0);
-            if (a.D > 64) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(ab[1], qb[n][1], c, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) score[4 * quad + r][n * 16 + i] = ordered((float)c[r] * unit[r]);
-        }
-        __syncthreads();
-    };
-    uint32_t best[KK];                                         // descending; the places past `wanted` are taken from the start
-#pragma unroll
-    for (int e = 0; e < KK; ++e) best[e] = e < KK - wanted ? 0xFFFFFFFFu : 0u;
-    if (wanted > 0)
-        for (int j0 = 0; j0 < most; j0 += 16) {
-            scores(j0);
-#pragma unroll 4
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t v = j0 + r < mine ? score[r][lane] : 0u;
-                if (__any(v > best[KK - 1])) {
-#pragma unroll
-                    for (int e = KK - 1; e > 0; --e) {         // median of v and two neighbours: v sinks to its place
-                        const uint32_t hi = best[e - 1], lo = best[e];
-                        best[e] = max(min(v, hi), lo);
-                    }
-                    best[0] = max(v, best[0]);
-                }
-            }
-        }
-    const uint32_t least = best[KK - 1];
-    int due = 0;                                               // how many equal to the lowest one are taken
-#pragma unroll
-    for (int e = 0; e < KK; ++e) due += (e >= KK - wanted && best[e] == least) ? 1 : 0;
-    int* out = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
-    int n = 0;
-    if (wanted > 0)
-        for (int j0 = 0; j0 < most; j0 += 16) {
-            scores(j0);
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t v = score[r][lane];
-                if (j0 + r < mine && (v > least || (v == least && due > 0))) {
-                    if (v == least) --due;
-                    out[n++] = j0 + r;
-                }
-            }
-        }
-    if (t < a.Tq) {
-        if (there) out[n++] = mine;
-        for (; n < a.NS; ++n) out[n] = -1;
+    for (int u = 0; u < U; ++u) {
+        const uint64_t below = (1ull << lane) - 1, same = __ballot(v[u] == least && v[u] != 0);
+        const bool take = v[u] > least || ((same >> lane & 1) && __popcll(same & below) < due);
+        const uint64_t all = __ballot(take);
+        if (take) out[n + __popcll(all & below)] = u * 64 + lane;
+        n += __popcll(all);
+        due -= min(due, (int)__popcll(same));
     }
+    for (int i = n + lane; i < NS; i += 64) out[i] = i == n ? own : -1;
 }
-
-// ---- selection for few queries: a workgroup per query and key head.  Scores in LDS; the lowest that is taken is found bit by
-// bit, the workgroup counting the scores at or above a trial value.
-constexpr int FEW_THREADS = 256;
 template <typename T>
 __global__ __launch_bounds__(FEW_THREADS) void k_block_select_few(AttentionArgs a, Heads<const T> q, const int8_t* __restrict__ sums,
                                                                   const float* __restrict__ scales, int* __restrict__ blocks) {
     __shared__ __align__(16) uint2 q8[16];
     __shared__ uint32_t score[KEY_BLOCKS_MAX];
-    __shared__ int count[2][4];
-    __shared__ int before[FEW_THREADS];
     const int bg = blockIdx.y, b = bg / a.G, g = bg % a.G, len = a.length(b), t = blockIdx.x;
-    const int p = len - a.Tq + t, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int p = len - a.Tq + t;
     int* out = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
     if (p < 0) {
         for (int n = threadIdx.x; n < a.NS; n += FEW_THREADS) out[n] = -1;
         return;
     }
-    const int mine = p / a.BK, wanted = min(a.NS - 1, mine);
-    if (wave == 0) {
-        const uint2 w = query8(a, q, b, t, g, lane & 15, true);
-        if (lane < 16) q8[lane] = w;
+    const int own = p / a.BK, wanted = min(a.NS - 1, own);
+    if (threadIdx.x < 64) {
+        const uint2 w = Query8<T, 4>(a, q, b, t, g, threadIdx.x & 15, true).value();
+        if (threadIdx.x < 16) q8[threadIdx.x] = w;
     }
     __syncthreads();
     const int8_t* srow = sums + (int64_t)bg * a.nb * a.D;
     const float* scl = scales + (int64_t)bg * a.nb;
-    for (int j = threadIdx.x; j < mine; j += FEW_THREADS) {
-        const uint2* s = reinterpret_cast<const uint2*>(srow + (int64_t)j * a.D);
-        int dot = 0;
-        for (int u = 0; u < a.D / 8; ++u) {
-            const uint2 w = s[u], x = q8[u];
-            dot = __builtin_amdgcn_sdot4((int)w.x, (int)x.x, dot, false);
-            dot = __builtin_amdgcn_sdot4((int)w.y, (int)x.y, dot, false);
-        }
-        score[j] = ordered((float)dot * scl[j]);
-    }
-    __syncthreads();
-    // the highest value with at least `wanted` scores at or above it
-    uint32_t least = 0;
-    if (wanted > 0 && wanted < mine)
-        for (int bit = 31, turn = 0; bit >= 0; --bit, turn ^= 1) {
-            const uint32_t trial = least | (1u << bit);
-            int c = 0;
-            for (int j = threadIdx.x; j < mine; j += FEW_THREADS) c += score[j] >= trial;
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d);
-            if (lane == 0) count[turn][wave] = c;
-            __syncthreads();
-            const int all = count[turn][0] + count[turn][1] + count[turn][2] + count[turn][3];
-            if (all >= wanted) least = trial;
-            if (all == wanted) break;
-        }
-    // every thread takes a stretch of blocks: its number above and equal, then its places
-    const int each = (mine + FEW_THREADS - 1) / FEW_THREADS, j0 = threadIdx.x * each, j1 = min(j0 + each, mine);
-    int above = 0, equal = 0;
     if (wanted > 0)
-        for (int j = j0; j < j1; ++j) {
-            above += score[j] > least;
-            equal += score[j] == least;
+        for (int j = threadIdx.x; j < own; j += FEW_THREADS) {
+            const uint2* s = reinterpret_cast<const uint2*>(srow + (int64_t)j * a.D);
+            int dot = 0;
+#pragma unroll 4
+            for (int u = 0; u < a.D / 8; ++u) {
+                const uint2 w = s[u], x = q8[u];
+                dot = __builtin_amdgcn_sdot4((int)w.x, (int)x.x, dot, false);
+                dot = __builtin_amdgcn_sdot4((int)w.y, (int)x.y, dot, false);
+            }
+            score[j] = ordered((float)dot * scl[j]);
         }
-    before[threadIdx.x] = above << 16 | equal;                 // (up to 2048 of either)
     __syncthreads();
-    int a0 = 0, e0 = 0, total_above = 0;
-    for (int i = 0; i < FEW_THREADS; ++i) {
-        const int w = before[i];
-        if (i < (int)threadIdx.x) a0 += w >> 16, e0 += w & 0xFFFF;
-        total_above += w >> 16;
-    }
-    const int ties = wanted - total_above;                     // of the equal ones, the first so many
-    if (wanted > 0)
-        for (int j = j0; j < j1; ++j) {
-            const uint32_t v = score[j];
-            if (v > least || (v == least && e0 < ties)) out[a0 + min(e0, ties)] = j;
-            if (v > least) ++a0;
-            else if (v == least) ++e0;
-        }
-    if (threadIdx.x == 0) out[wanted] = mine;
-    for (int n = wanted + 1 + threadIdx.x; n < a.NS; n += FEW_THREADS) out[n] = -1;
+    if (threadIdx.x >= 64) return;
+    const int candidates = wanted > 0 ? own : 0;
+    if (candidates <= 256) take_best<4>(score, candidates, wanted, own, a.NS, out);
+    else if (candidates <= 1024) take_best<16>(score, candidates, wanted, own, a.NS, out);
+    else take_best<32>(score, candidates, wanted, own, a.NS, out);
 }
 
 // ---- plan.  A tile of 256 queries marks its queries in one bit word of 256 a block: a query has a block once at most, so the number
 // of bits below its own is its place among the tile's.  Counts per tile, their sums over the tiles, then every pair to its place.
-__device__ inline void mark_tile(const AttentionArgs& a, const int* __restrict__ blocks, int bg, int t, int len, uint32_t* bits, int* rows_out) {
+// Selections go through LDS, from and to memory in order.
+struct PlanSpace {
+    int bits, rows, total;               // LDS: [nb][8] words, [256][NS + 1] (odd rows: a thread each, in different banks)
+    PlanSpace(const AttentionArgs& a) : bits(0), rows(a.nb * 32), total(a.nb * 32 + PLAN_TILE * (a.NS | 1) * 4) {}
+};
+__device__ inline void clear_bits(const AttentionArgs& a, uint32_t* bits) {
     for (int i = threadIdx.x; i < a.nb * 8; i += PLAN_TILE) bits[i] = 0;
+}
+__device__ inline void rows_to_lds(const AttentionArgs& a, const int* __restrict__ from, int n, int* rows) {
+    for (int i = threadIdx.x; i < n * a.NS; i += PLAN_TILE) rows[i / a.NS * (a.NS | 1) + i % a.NS] = from[i];
+}
+
+__global__ __launch_bounds__(PLAN_TILE) void k_plan_count(AttentionArgs a, const int* __restrict__ blocks, Plan plan, PlanSpace space) {
+    extern __shared__ __align__(16) char lds[];
+    uint32_t* bits = reinterpret_cast<uint32_t*>(lds + space.bits);
+    int* rows = reinterpret_cast<int*>(lds + space.rows);
+    const int bg = blockIdx.y, t0 = blockIdx.x * PLAN_TILE, n = min(PLAN_TILE, a.Tq - t0);
+    const int64_t first = ((int64_t)bg * a.Tq + t0) * a.NS;
+    clear_bits(a, bits);
+    rows_to_lds(a, blocks + first, n, rows);
     __syncthreads();
-    if (t < a.Tq) {
-        const int p = len - a.Tq + t, own = p >= 0 ? p / a.BK : -1;
-        const int* row = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
-        int* out = rows_out + ((int64_t)bg * a.Tq + t) * a.NS;
-        int last = -1, n = 0;
+    if ((int)threadIdx.x < n) {
+        const int p = a.length(bg / a.G) - a.Tq + t0 + (int)threadIdx.x, own = p >= 0 ? p / a.BK : -1;
+        int* row = rows + threadIdx.x * (a.NS | 1);
+        int last = -1, kept = 0;
         for (int s = 0; s < a.NS; ++s) {
             const int j = row[s];
             if (j > last && j <= own) {
-                out[n++] = j;
+                row[kept++] = j;
                 atomicOr(&bits[j * 8 + (threadIdx.x >> 5)], 1u << (threadIdx.x & 31));
                 last = j;
             }
         }
-        for (; n < a.NS; ++n) out[n] = a.nb;
+        for (; kept < a.NS; ++kept) row[kept] = a.nb;
     }
     __syncthreads();
-}
-
-__global__ __launch_bounds__(PLAN_TILE) void k_plan_count(AttentionArgs a, const int* __restrict__ blocks, Plan plan) {
-    extern __shared__ uint32_t bits[];
-    const int bg = blockIdx.y, t = blockIdx.x * PLAN_TILE + threadIdx.x;
-    mark_tile(a, blocks, bg, t, a.length(bg / a.G), bits, plan.rows);
-    int* row = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
+    for (int i = threadIdx.x; i < n * a.NS; i += PLAN_TILE) plan.rows[first + i] = rows[i / a.NS * (a.NS | 1) + i % a.NS];
+    int* counts = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
     for (int j = threadIdx.x; j < a.nb; j += PLAN_TILE) {
         int c = 0;
 #pragma unroll
         for (int w = 0; w < 8; ++w) c += __popc(bits[j * 8 + w]);
-        row[j] = c;
+        counts[j] = c;
     }
 }
 
@@ -354,26 +489,42 @@ __device__ inline int2 exclusive(int2 v, int2* total) {
     return make_int2(before.x + x.x - v.x, before.y + x.y - v.y);
 }
 
-__global__ __launch_bounds__(1024) void k_plan_sums(AttentionArgs a, Plan plan) {
-    const int bg = blockIdx.x;
+// a workgroup per (batch, key head): `width` blocks at a time, 1024 / width stretches of the tiles side by side
+__global__ __launch_bounds__(1024) void k_plan_sums(AttentionArgs a, Plan plan, int width) {
+    __shared__ int stretch_sum[1024];
+    const int bg = blockIdx.x, stretches = 1024 / width, mine = threadIdx.x / width;
+    const int i0 = (int)((int64_t)plan.tiles * mine / stretches), i1 = (int)((int64_t)plan.tiles * (mine + 1) / stretches);
     int* tile = plan.tile + (int64_t)bg * plan.tiles * a.nb;
     int* start = plan.start + (int64_t)bg * (a.nb + 1);
     int* item_start = plan.item_start + (int64_t)bg * (a.nb + 1);
     int2* items = plan.items + (int64_t)bg * plan.max_items;
     int2 done = make_int2(0, 0);
-    for (int j0 = 0; j0 < a.nb; j0 += 1024) {
-        const int j = j0 + threadIdx.x;
+    for (int j0 = 0; j0 < a.nb; j0 += width) {
+        const int j = j0 + (int)(threadIdx.x % width);
+        const bool there = j < a.nb;
         int n = 0;
-        if (j < a.nb)
-            for (int i = 0; i < plan.tiles; ++i) {
+        if (there)
+#pragma unroll 8
+            for (int i = i0; i < i1; ++i) n += tile[(int64_t)i * a.nb + j];
+        stretch_sum[threadIdx.x] = n;
+        __syncthreads();
+        int before = 0, whole = 0;
+        for (int s = 0; s < stretches; ++s) {
+            const int c = stretch_sum[s * width + threadIdx.x % width];
+            before += s < mine ? c : 0;
+            whole += c;
+        }
+        if (there)
+#pragma unroll 8
+            for (int i = i0; i < i1; ++i) {
                 const int c = tile[(int64_t)i * a.nb + j];
-                tile[(int64_t)i * a.nb + j] = n;
-                n += c;
+                tile[(int64_t)i * a.nb + j] = before;
+                before += c;
             }
-        const int parts = (n + plan.item_pairs - 1) / plan.item_pairs;
+        const int pairs = there && mine == 0 ? whole : 0, parts = (pairs + plan.item_pairs - 1) / plan.item_pairs;
         int2 all;
-        const int2 at = exclusive(make_int2(n, parts), &all);
-        if (j < a.nb) {
+        const int2 at = exclusive(make_int2(pairs, parts), &all);          // (the threads of the first stretch come first)
+        if (there && mine == 0) {
             start[j] = done.x + at.x;
             item_start[j] = done.y + at.y;
             for (int i = 0; i < parts; ++i) items[done.y + at.y + i] = make_int2(j, done.x + at.x + i * plan.item_pairs);
@@ -383,17 +534,20 @@ __global__ __launch_bounds__(1024) void k_plan_sums(AttentionArgs a, Plan plan) 
     if (threadIdx.x == 0) start[a.nb] = done.x, item_start[a.nb] = done.y;
 }
 
-__global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan plan) {
-    extern __shared__ uint32_t bits[];
-    const int bg = blockIdx.y, t = blockIdx.x * PLAN_TILE + threadIdx.x;
-    for (int i = threadIdx.x; i < a.nb * 8; i += PLAN_TILE) bits[i] = 0;
+__global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan plan, PlanSpace space) {
+    extern __shared__ __align__(16) char lds[];
+    uint32_t* bits = reinterpret_cast<uint32_t*>(lds + space.bits);
+    int* rows = reinterpret_cast<int*>(lds + space.rows);
+    const int bg = blockIdx.y, t0 = blockIdx.x * PLAN_TILE, n = min(PLAN_TILE, a.Tq - t0), word = threadIdx.x >> 5;
+    clear_bits(a, bits);
+    rows_to_lds(a, plan.rows + ((int64_t)bg * a.Tq + t0) * a.NS, n, rows);
     __syncthreads();
-    const int word = threadIdx.x >> 5;
-    const int* row = plan.rows + ((int64_t)bg * a.Tq + t) * a.NS;
-    if (t < a.Tq)
+    const int* row = rows + threadIdx.x * (a.NS | 1);
+    const bool there = (int)threadIdx.x < n;
+    if (there)
         for (int s = 0; s < a.NS && row[s] < a.nb; ++s) atomicOr(&bits[row[s] * 8 + word], 1u << (threadIdx.x & 31));
     __syncthreads();
-    if (t >= a.Tq) return;
+    if (!there) return;
     const int* before = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
     const int* start = plan.start + (int64_t)bg * (a.nb + 1);
     int* list = plan.list + (int64_t)bg * a.Tq * a.NS;
@@ -401,7 +555,7 @@ __global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan p
         const int j = row[s];
         int at = start[j] + before[j] + __popc(bits[j * 8 + word] & ((1u << (threadIdx.x & 31)) - 1));
         for (int w = 0; w < word; ++w) at += __popc(bits[j * 8 + w]);
-        list[at] = t * a.NS + s;
+        list[at] = (t0 + (int)threadIdx.x) * a.NS + s;
     }
 }
 
@@ -443,13 +597,23 @@ extern "C" int mst_block_select(const mst_attention_shape* s, const mst_heads* q
             k_block_select_few<T><<<dim3((unsigned)a.Tq, (unsigned)(a.B * a.G)), FEW_THREADS, 0, st>>>(a, qh, sums, scales, blocks);
             return;
         }
-        const dim3 grid((unsigned)cdiv(a.Tq, 64), (unsigned)(a.B * a.G));
+        const dim3 grid((unsigned)cdiv(a.Tq, SELECT_THREADS / 4), (unsigned)(a.B * a.G));
         const int wanted = a.NS - 1;
-        if (wanted <= 4) k_block_select<T, 4><<<grid, 64, 0, st>>>(a, qh, sums, scales, blocks);
-        else if (wanted <= 8) k_block_select<T, 8><<<grid, 64, 0, st>>>(a, qh, sums, scales, blocks);
-        else if (wanted <= 16) k_block_select<T, 16><<<grid, 64, 0, st>>>(a, qh, sums, scales, blocks);
-        else if (wanted <= 32) k_block_select<T, 32><<<grid, 64, 0, st>>>(a, qh, sums, scales, blocks);
-        else k_block_select<T, 63><<<grid, 64, 0, st>>>(a, qh, sums, scales, blocks);
+        auto launch = [&](auto kk) {
+            constexpr int KK = decltype(kk)::value;
+            auto go = [&](auto hb, auto held) { k_block_select<T, KK, decltype(hb)::value, decltype(held)::value><<<grid, SELECT_THREADS, 0, st>>>(a, qh, sums, scales, blocks); };
+            auto heads = [&](auto held) {
+                if (a.R == 1) go(std::integral_constant<int, 1>{}, held);
+                else go(std::integral_constant<int, 4>{}, held);
+            };
+            if (a.nb <= SELECT_HELD) heads(std::true_type{});
+            else heads(std::false_type{});
+        };
+        if (wanted <= 4) launch(std::integral_constant<int, 4>{});
+        else if (wanted <= 8) launch(std::integral_constant<int, 8>{});
+        else if (wanted <= 16) launch(std::integral_constant<int, 16>{});
+        else if (wanted <= 32) launch(std::integral_constant<int, 32>{});
+        else launch(std::integral_constant<int, 64>{});
     });
     MST_LAUNCH_CHECK();
     return MST_OK;
@@ -471,15 +635,22 @@ extern "C" int mst_block_plan(const mst_attention_shape* s, const int32_t* block
     if (a.B == 0) return MST_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)plan.tiles, (unsigned)(a.B * a.G));
-    const size_t lds = (size_t)std::max(a.nb, 1) * 32;          // 64 KB at most
+    const PlanSpace space(a);                                   // 129 KB at most
+    static uint64_t allowed_count = 0, allowed_fill = 0;
+    if (space.total > 64 * 1024) {
+        if (int e = allow_lds(reinterpret_cast<const void*>(&k_plan_count), LDS_BYTES, allowed_count)) return e;
+        if (int e = allow_lds(reinterpret_cast<const void*>(&k_plan_fill), LDS_BYTES, allowed_fill)) return e;
+    }
     if (plan.tiles > 0) {
-        k_plan_count<<<grid, PLAN_TILE, lds, st>>>(a, blocks, plan);
+        k_plan_count<<<grid, PLAN_TILE, space.total, st>>>(a, blocks, plan, space);
         MST_LAUNCH_CHECK();
     }
-    k_plan_sums<<<(unsigned)(a.B * a.G), 1024, 0, st>>>(a, plan);
+    int width = 16;                                             // blocks that the threads of the sums stand for: a power of two
+    while (width < a.nb && width < 1024) width *= 2;
+    k_plan_sums<<<(unsigned)(a.B * a.G), 1024, 0, st>>>(a, plan, width);
     MST_LAUNCH_CHECK();
     if (plan.tiles > 0) {
-        k_plan_fill<<<grid, PLAN_TILE, lds, st>>>(a, plan);
+        k_plan_fill<<<grid, PLAN_TILE, space.total, st>>>(a, plan, space);
         MST_LAUNCH_CHECK();
     }
     return MST_OK;

@@ -214,11 +214,42 @@ template <typename T> __device__ inline Operand<T> negated(Operand<T> o) {
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }    // results below 2^-126 are 0
 
-template <int WIDTH>
-__device__ inline float lanes_sum(float x) {        // over groups of WIDTH consecutive lanes
-#pragma unroll
-    for (int d = WIDTH / 2; d >= 1; d >>= 1) x += __shfl_xor(x, d);
+// Rows of 16 lanes: both numbers of lanes 16 (or 32) apart, the even row's (the lower half's) first, in either of them
+struct Both { uint32_t first, second; };
+template <int APART>
+__device__ inline Both both_lanes(uint32_t x) {
+    typedef unsigned uint2v __attribute__((ext_vector_type(2)));
+    uint2v r;
+    if constexpr (APART == 16) r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    else r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return {r[0], r[1]};
+}
+template <int APART, typename V, typename F>
+__device__ inline V apart(V x, F&& f) {
+    const Both b = both_lanes<APART>(__builtin_bit_cast(uint32_t, x));
+    return f(__builtin_bit_cast(V, b.first), __builtin_bit_cast(V, b.second));
+}
+// f(x, the same of another lane) over groups of WIDTH consecutive lanes, WIDTH up to 64; every lane gets the result.  Within 16 lanes the
+// other lane's number comes with the instruction (pairs, pairs of pairs, mirrored eights, mirrored rows).
+template <int CONTROL>
+__device__ inline float other_lane(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CONTROL, 0xF, 0xF, true)); }
+template <int CONTROL>
+__device__ inline int other_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, 0xF, 0xF, true); }
+template <int WIDTH, typename V, typename F>
+__device__ inline V over_lanes(V x, F&& f) {
+    if (WIDTH >= 2) x = f(x, other_lane<0xB1>(x));
+    if (WIDTH >= 4) x = f(x, other_lane<0x4E>(x));
+    if (WIDTH >= 8) x = f(x, other_lane<0x141>(x));
+    if (WIDTH >= 16) x = f(x, other_lane<0x140>(x));
+    if (WIDTH >= 32) x = apart<16>(x, f);
+    if (WIDTH >= 64) x = apart<32>(x, f);
     return x;
 }
+template <int WIDTH>
+__device__ inline float lanes_sum(float x) { return over_lanes<WIDTH>(x, [](float a, float b) { return a + b; }); }
+template <int WIDTH>
+__device__ inline float lanes_max(float x) { return over_lanes<WIDTH>(x, [](float a, float b) { return fmaxf(a, b); }); }
+template <int WIDTH>
+__device__ inline int lanes_max(int x) { return over_lanes<WIDTH>(x, [](int a, int b) { return max(a, b); }); }
 
 }  // namespace mst
