@@ -244,15 +244,17 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
     const int col = wave * 32 + i32, tok = col / a.R, t = t0 + tok, h = g * a.R + col - tok * a.R;
     const bool there = tok < tokens && t < a.Tq;
     const int p = len - a.Tq + t;
-    const float scale2 = a.scale * LOG2E;
     const int64_t stat = ((int64_t)b * a.H + (there ? h : 0)) * a.Tq + (there ? t : 0);
     const float lse2 = lse[stat] * LOG2E, dl = delta[stat];
+    // a positive factor, so that -inf is below every score: its sign goes to the query
+    const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, 1.17549435e-38f);
     Operand<T> qf[QC], of[QC];
     const T *qp = q.at(b, there ? t : 0, there ? h : 0), *op = d_o.at(b, there ? t : 0, there ? h : 0);
 #pragma unroll
     for (int c = 0; c < QC; ++c) {
         const int d = c * 16 + half * 8;
         qf[c] = there && d < a.D ? load_operand(qp + d) : zero_operand<T>();
+        if (a.scale < 0.f) qf[c] = negated(qf[c]);
         of[c] = there && d < a.D ? load_operand(op + d) : zero_operand<T>();
     }
     floatx16 acc[DT];
@@ -279,6 +281,8 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
         i += block_ends;
         if ((now >> (16 + wave)) & 1) {
             const int limit = cursor.next == (int)(now & 0xFFFF) ? p - key0 : -1;
+            const bool cut = __any(limit < KW - 1 && limit >= 0);          // some row sees some of these keys, not all
+            const float less = limit < 0 ? INFINITY : lse2;    // a row that sees nothing here: weights 2^-inf
 #pragma unroll
             for (int st = 0; st < ST; ++st) {
                 floatx16 s = zero16(), dp = zero16();
@@ -287,14 +291,15 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
                     s = product32(along_row<T, DP>(tile, st * 32 + i32, c * 16 + half * 8), qf[c], s);
                     dp = product32(along_row<T, DP>(tile + Tiles::TILE, st * 32 + i32, c * 16 + half * 8), of[c], dp);
                 }
+                if (cut)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (st * 32 + 8 * (r / 4) + 4 * half + r % 4 > limit) s[r] = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float y[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int r = u * 8 + e;
-                        y[e] = st * 32 + 8 * (r / 4) + 4 * half + r % 4 <= limit ? exp2_fast(__builtin_fmaf(s[r], scale2, -lse2)) * (dp[r] - dl) : 0.f;
-                    }
+                    for (int e = 0; e < 8; ++e) y[e] = exp2_fast(__builtin_fmaf(s[u * 8 + e], scale2, -less)) * (dp[u * 8 + e] - dl);
                     Operand<T> sf;
                     set_operand(sf, y);
 #pragma unroll

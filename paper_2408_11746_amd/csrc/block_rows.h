@@ -69,15 +69,14 @@ struct UnionSpace {
     }
 };
 
-// grid: a workgroup per (batch, key head) and COLS / R queries, the later queries first (theirs are the longer walks).  Workgroups
-// go to the eight XCDs in turn: those of one key head are given to one of them, whose L2 then holds its keys and values.
+// grid: a workgroup per (batch, key head) and COLS / R queries.  The last queries of every head come first: theirs are the longest
+// walks, and the short ones fill what they leave (8192 queries of 20 heads: forward 177 -> 142 us against head after head).
 struct RowWork {
     int bg, tile;
     __device__ RowWork(int tiles) {
-        const int n = gridDim.x, even = n / 8 * 8, i = blockIdx.x;
-        const int id = i < even ? (i % 8) * (even / 8) + i / 8 : i;
-        bg = id / tiles;
-        tile = tiles - 1 - (id - bg * tiles);
+        const int heads = gridDim.x / tiles;
+        bg = blockIdx.x % heads;
+        tile = tiles - 1 - blockIdx.x / heads;
     }
 };
 
