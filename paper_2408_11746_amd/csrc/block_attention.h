@@ -14,13 +14,13 @@ struct AttentionArgs {
 };
 
 // The selection as the kernels read it: rows without the entries that do not count, and the lists of the queries of each block
-// of keys.  bg = b G + g; a pair is query * NS + place in the query's row.
+// of keys.  bg = b G + g; a pair is one entry of a query's row.
 constexpr int PLAN_TILE = 256;           // queries that a workgroup of the builders takes
 constexpr int ITEM_ROWS = 512, ITEM_ROWS_MOST = 4096;          // rows (query, head) of an item: a workgroup of the kernel that walks lists
 constexpr int ITEMS = 2048;              // and about so many items, where that makes none shorter
 struct Plan {
     int* rows = nullptr;                 // [bg][Tq][NS] the entries of a selection that count, nb behind them
-    int* list = nullptr;                 // [bg][Tq NS] pairs, block after block, ascending inside a block
+    int* list = nullptr;                 // [bg][Tq NS] queries of the pairs, block after block, ascending inside a block
     int* start = nullptr;                // [bg][nb + 1] first pair of a block
     int* item_start = nullptr;           // [bg][nb + 1] first item of a block
     int2* items = nullptr;               // [bg][max_items] block and first pair

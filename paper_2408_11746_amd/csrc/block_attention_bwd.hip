@@ -42,7 +42,7 @@ struct DkvTiles {
     using R = Rows<T, DP>;
     static constexpr int RG = KP == 4 ? 1 : 2, WAVES = KP * RG, THREADS = WAVES * 64, RT = RG * 32;
     static constexpr int TILE = RT * R::BYTES, BUFFER = 2 * TILE, EACH = BUFFER / 1024 / WAVES;      // Q and dO of RT rows
-    static constexpr int ROWS = 2 * BUFFER, STATS = ROWS + 2 * RT * 8, BYTES = STATS + 2 * RT * 12;  // byte offsets: queries of rows, their statistics
+    static constexpr int ROWS = 2 * BUFFER, STATS = ROWS + 2 * 2 * RT * 8, BYTES = STATS + 2 * RT * 12;        // LDS: where a row's Q and dO are, its statistics
     static_assert(TILE % (EACH * 1024) == 0 && BUFFER * 2 >= (RG - 1) * KP * 32 * DP * 8, "whole loads; room for the sums of half the wavefronts");
 };
 
@@ -78,19 +78,20 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dk
     // The rows of step x are known two steps ahead (their queries, by the first RT threads) and their statistics one.
     const int rows = pairs * a.R, steps = (rows + RT - 1) / RT;
     const int* list = plan.list + (int64_t)bg * a.Tq * a.NS + first;
-    int2* row_th = reinterpret_cast<int2*>(lds + Tiles::ROWS);                     // [2][RT] query and head of a row
+    int64_t* row_at = reinterpret_cast<int64_t*>(lds + Tiles::ROWS);               // [2][2][RT] byte offsets of a row's Q and dO from the batch's
     float* stats = reinterpret_cast<float*>(lds + Tiles::STATS);                   // [2][3][RT] log-sum, delta, last key that it sees
     const bool scout = (int)threadIdx.x < RT;
     const bool is_q = wave < Tiles::WAVES / 2;
-    const Heads<const T>& mine = is_q ? q : d_o;
-    const char* base = reinterpret_cast<const char*>(mine.at(b, 0, g * a.R));
-    const int64_t st = mine.st * (int64_t)sizeof(T), sh = mine.sh * (int64_t)sizeof(T);
+    const char* base = reinterpret_cast<const char*>(is_q ? q.at(b, 0, g * a.R) : d_o.at(b, 0, g * a.R));
     const uint32_t to = lds_address(lds) + wave * (EACH * 1024);
     const int my_row = (wave % (Tiles::WAVES / 2)) * EACH * R::PER_KB + lane / R::CH;
+    int chunk[EACH];                     // a lane's chunk of a row
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) chunk[i] = min(((lane % R::CH) ^ R::mix(my_row + i * R::PER_KB)) * 16, a.D * (int)sizeof(T) - 16);
     auto row_of = [&](int x) {           // query and head of the thread's row of step x; rows past the last are read as that
         const int row = min(x * RT + (int)threadIdx.x, rows - 1);
         const int e = (int)(((float)row + 0.5f) * inv_r);      // (rows are below 2^13, heads up to 64: never within rounding of the next one)
-        return make_int2(list[e] / a.NS, row - e * a.R);
+        return make_int2(list[e], row - e * a.R);
     };
     struct Stat { float lse, delta; int limit; };
     auto stat_of = [&](int2 th, int x) {
@@ -101,21 +102,21 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dk
         float* p = stats + (x & 1) * 3 * RT + threadIdx.x;
         p[0] = s.lse, p[RT] = s.delta, p[2 * RT] = __int_as_float(s.limit);
     };
+    auto put_row = [&](int2 th, int x) {
+        int64_t* p = row_at + (x & 1) * 2 * RT + threadIdx.x;
+        p[0] = (th.x * q.st + th.y * q.sh) * (int64_t)sizeof(T), p[RT] = (th.x * d_o.st + th.y * d_o.sh) * (int64_t)sizeof(T);
+    };
     auto load_rows = [&](int x) {
-        const int2* row = row_th + (x & 1) * RT;
+        const int64_t* row = row_at + ((x & 1) * 2 + (is_q ? 0 : 1)) * RT + my_row;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int r = my_row + i * R::PER_KB, c = min(((lane % R::CH) ^ R::mix(r)) * 16, a.D * (int)sizeof(T) - 16);
-            const int2 th = row[r];
-            gather_to_lds(base + th.x * st + th.y * sh + c, to + (x & 1) * Tiles::BUFFER + i * 1024);
-        }
+        for (int i = 0; i < EACH; ++i) gather_to_lds(base + (row[i * R::PER_KB] + chunk[i]), to + (x & 1) * Tiles::BUFFER + i * 1024);
     };
     int2 th2 = make_int2(0, 0);
     Stat stat1{0.f, 0.f, -1};
     if (scout) {
         const int2 th0 = row_of(0), th1 = row_of(1);
         th2 = row_of(2);
-        row_th[threadIdx.x] = th0, row_th[RT + threadIdx.x] = th1;
+        put_row(th0, 0), put_row(th1, 1);
         put_stat(stat_of(th0, 0), 0);
         stat1 = stat_of(th1, 1);
     }
@@ -128,7 +129,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dk
         if (x + 1 < steps) load_rows(x + 1);
         if (scout && x + 1 < steps) {
             put_stat(stat1, x + 1);
-            row_th[(x & 1) * RT + threadIdx.x] = th2;
+            put_row(th2, x);
             stat1 = stat_of(th2, x + 2);
             th2 = row_of(x + 3);
         }
@@ -139,6 +140,8 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dk
             dp = product32(along_row<T, DP>(ot, rg * 32 + i32, c * 16 + half * 8), vf[c], dp);
         }
         const float* stat = stats + (x & 1) * 3 * RT + rg * 32 + 4 * half;
+        // rows that see all of this part's keys need no comparison (those of later blocks, which are most)
+        const bool cut = __any(__float_as_int(stats[(x & 1) * 3 * RT + 2 * RT + rg * 32 + i32]) < kp * 32 + 31);
         Operand<T> pf[2], sf[2];         // P and dS, columns = keys, contraction over the rows
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -146,14 +149,19 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dk
 #pragma unroll
             for (int e = 0; e < 8; e += 4) {
                 const float4 ls = *reinterpret_cast<const float4*>(stat + u * 16 + 2 * e), de = *reinterpret_cast<const float4*>(stat + RT + u * 16 + 2 * e);
-                const int4 li = *reinterpret_cast<const int4*>(stat + 2 * RT + u * 16 + 2 * e);
                 const float l4[4] = {ls.x, ls.y, ls.z, ls.w}, d4[4] = {de.x, de.y, de.z, de.w};
-                const int i4[4] = {li.x, li.y, li.z, li.w};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int n = u * 8 + e + r;
-                    p[e + r] = kp * 32 + i32 <= i4[r] ? exp2_fast(__builtin_fmaf(s[n], scale2, -l4[r])) : 0.f;
+                    p[e + r] = exp2_fast(__builtin_fmaf(s[n], scale2, -l4[r]));
                     ds[e + r] = p[e + r] * (dp[n] - d4[r]);
+                }
+                if (cut) {
+                    const int4 li = *reinterpret_cast<const int4*>(stat + 2 * RT + u * 16 + 2 * e);
+                    const int i4[4] = {li.x, li.y, li.z, li.w};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (kp * 32 + i32 > i4[r]) p[e + r] = ds[e + r] = 0.f;
                 }
             }
             set_operand(pf[u], p);
