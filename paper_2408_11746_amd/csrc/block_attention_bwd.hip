@@ -47,13 +47,14 @@ struct DkvTiles {
 };
 
 template <typename T, int DP, int KP>
-__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v,
-                                                                               Heads<const T> d_o, int bg0, BwdArgs w, Heads<T> dk_out, Heads<T> dv_out) {
+__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1 : 2)) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+                                                                               Heads<const T> d_o, int bg0, int group, BwdArgs w, Heads<T> dk_out, Heads<T> dv_out) {
     using Tiles = DkvTiles<T, DP, KP>;
     using R = Rows<T, DP>;
     constexpr int QC = DP / 16, DT = DP / 32, RT = Tiles::RT, RG = Tiles::RG, EACH = Tiles::EACH;
     extern __shared__ __align__(16) char lds[];
-    const int bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G, index = blockIdx.x;
+    // the items of a key head lie `group` workgroups apart: mostly on one XCD, whose L2 then holds the head's queries
+    const int index = blockIdx.x / group, in_group = blockIdx.x - index * group, bg = bg0 + in_group, b = bg / a.G, g = bg % a.G;
     if (index >= plan.item_start[(int64_t)bg * (a.nb + 1) + a.nb]) return;
     const int2 it = plan.items[(int64_t)bg * plan.max_items + index];
     const int block = it.x, first = it.y, end = plan.start[(int64_t)bg * (a.nb + 1) + block + 1], pairs = min(plan.item_pairs, end - first);
@@ -204,7 +205,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS)) void k_attention_dk
             }
         return;
     }
-    float* out = w.dkv + (((int64_t)blockIdx.y * plan.max_items + index) * 2 * a.BK + kp * 32 + i32) * a.D;
+    float* out = w.dkv + (((int64_t)in_group * plan.max_items + index) * 2 * a.BK + kp * 32 + i32) * a.D;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -353,7 +354,7 @@ int launch_dkv(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, con
     if (int e = allow_lds(reinterpret_cast<const void*>(&k_attention_dkv<T, DP, KP>), Tiles::BYTES, allowed)) return e;
     for (int bg = 0; bg < a.B * a.G; bg += sp.group) {
         const unsigned n = (unsigned)std::min(sp.group, a.B * a.G - bg);
-        k_attention_dkv<T, DP, KP><<<dim3((unsigned)plan.max_items, n), Tiles::THREADS, Tiles::BYTES, st>>>(a, plan, q, k, v, d_o, bg, w, dk, dv);
+        k_attention_dkv<T, DP, KP><<<(unsigned)plan.max_items * n, Tiles::THREADS, Tiles::BYTES, st>>>(a, plan, q, k, v, d_o, bg, (int)n, w, dk, dv);
         MST_LAUNCH_CHECK();
         k_attention_dkv_join<T><<<dim3((unsigned)cdiv((int64_t)a.S * (a.D / 4), 256), n), 256, 0, st>>>(a, plan, bg, w, dk, dv);
         MST_LAUNCH_CHECK();
