@@ -14,13 +14,13 @@ struct AttentionArgs {
 };
 
 // The selection as the kernels read it: rows without the entries that do not count, and the lists of the queries of each block
-// of keys.  bg = b G + g; a pair is one entry of a query's row.
+// of keys.  bg = b G + g; a pair is an entry of a query's row: query << SELECT_BITS | place.
 constexpr int PLAN_TILE = 256;           // queries that a workgroup of the builders takes
 constexpr int ITEM_ROWS = 512, ITEM_ROWS_MOST = 4096;          // rows (query, head) of an item: a workgroup of the kernel that walks lists
 constexpr int ITEMS = 2048;              // and about so many items, where that makes none shorter
 struct Plan {
     int* rows = nullptr;                 // [bg][Tq][NS] the entries of a selection that count, nb behind them
-    int* list = nullptr;                 // [bg][Tq NS] queries of the pairs, block after block, ascending inside a block
+    int* list = nullptr;                 // [bg][Tq NS] pairs, block after block, ascending inside a block
     int* start = nullptr;                // [bg][nb + 1] first pair of a block
     int* item_start = nullptr;           // [bg][nb + 1] first item of a block
     int2* items = nullptr;               // [bg][max_items] block and first pair
@@ -65,9 +65,9 @@ inline int check_attention(const mst_attention_shape* s) {
     if (s->block != 32 && s->block != 64 && s->block != 128) return MST_ERR_SHAPE;
     if (s->n_select < 1 || s->n_select > SELECT_MAX) return MST_ERR_SHAPE;
     if ((int64_t)s->keys > (int64_t)KEY_BLOCKS_MAX * s->block) return MST_ERR_SHAPE;
-    // grids of (batch, key head): 65535; pairs and rows of one of them: 31 bits
+    // grids of (batch, key head): 65535; pairs and rows of one of them: 31 bits, as a pair itself
     if ((int64_t)s->batch * s->kv_heads > 65535) return MST_ERR_SHAPE;
-    if ((int64_t)s->queries * s->n_select * (s->heads / s->kv_heads) >= (int64_t(1) << 30)) return MST_ERR_SHAPE;
+    if ((int64_t)s->queries * s->n_select * (s->heads / s->kv_heads) >= (int64_t(1) << 30) || s->queries >= 1 << (31 - SELECT_BITS)) return MST_ERR_SHAPE;
     return MST_OK;
 }
 

@@ -6,6 +6,12 @@
 // along the rows for S and dP and across them for dK and dV, whose sums stay in registers: no two workgroups meet in one
 // sum.  A block with one item is written as it is; the sums of several items are left in fp32 and added in the order of the list.
 // The second works like the forward: rows that own their dQ walk the union of their blocks.
+//
+// dQ is a difference: the rows of dS add up to zero, and what the keys have in common falls out.  An error in delta, or one in
+// dS that does not add up to zero, brings it back.  delta from the rounded O is off by a bfloat16 rounding of O, and a bfloat16 dS by its own:
+// with keys of a common direction dQ was 3.5e-3 off (2-norm; its own rounding makes 1.7e-3).  So the first kernel, which has
+// dS with that delta in fp32, also leaves the sum of each of its rows, which is what delta lacks; a small launch adds them; and
+// the second takes dS as two bfloat16 numbers, high and low: 1.7e-3.
 #include "block_rows.h"
 
 namespace mst {
@@ -17,6 +23,7 @@ struct BwdArgs {
     const float* lse;                    // [B][H][Tq]
     const float* delta;                  // [B][H][Tq]
     float* dkv;                          // [item][2][BK][D]
+    float* lack;                         // [pair][R] sums of rows of dS over a block (bfloat16 operands)
 };
 
 template <typename T, int LANES>
@@ -42,12 +49,14 @@ struct DkvTiles {
     using R = Rows<T, DP>;
     static constexpr int RG = KP == 4 ? 1 : 2, WAVES = KP * RG, THREADS = WAVES * 64, RT = RG * 32;
     static constexpr int TILE = RT * R::BYTES, BUFFER = 2 * TILE, EACH = BUFFER / 1024 / WAVES;      // Q and dO of RT rows
-    static constexpr int ROWS = 2 * BUFFER, STATS = ROWS + 2 * 2 * RT * 8, BYTES = STATS + 2 * RT * 12;        // LDS: where a row's Q and dO are, its statistics
+    static constexpr int ROWS = 2 * BUFFER, STATS = ROWS + 2 * 2 * RT * 8, LACK = STATS + 2 * RT * 12, BYTES = LACK + 2 * (KP + 1) * RT * 4;   // LDS: where a row's Q and dO are, its statistics, sums of dS
     static_assert(TILE % (EACH * 1024) == 0 && BUFFER * 2 >= (RG - 1) * KP * 32 * DP * 8, "whole loads; room for the sums of half the wavefronts");
 };
 
+// (128 components take more registers than two wavefronts a SIMD have: so bound, it spills 170 bytes a lane, and 4099 queries of 24 heads
+// with 8 key heads take 368 us, not 281)
 template <typename T, int DP, int KP>
-__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1 : 2)) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 256 ? 1 : 2)) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v,
                                                                                Heads<const T> d_o, int bg0, int group, BwdArgs w, Heads<T> dk_out, Heads<T> dv_out) {
     using Tiles = DkvTiles<T, DP, KP>;
     using R = Rows<T, DP>;
@@ -89,15 +98,30 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1
     int chunk[EACH];                     // a lane's chunk of a row
 #pragma unroll
     for (int i = 0; i < EACH; ++i) chunk[i] = min(((lane % R::CH) ^ R::mix(my_row + i * R::PER_KB)) * 16, a.D * (int)sizeof(T) - 16);
-    auto row_of = [&](int x) {           // query and head of the thread's row of step x; rows past the last are read as that
+    auto row_of = [&](int x) {           // pair and head of the thread's row of step x; rows past the last are read as that
         const int row = min(x * RT + (int)threadIdx.x, rows - 1);
         const int e = (int)(((float)row + 0.5f) * inv_r);      // (rows are below 2^13, heads up to 64: never within rounding of the next one)
-        return make_int2(list[e], row - e * a.R);
+        return make_int2(list[e], row - e * a.R);              // (its pair)
+    };
+    // where the sum of a row of dS goes: for each buffer the sums of the KP parts and the row's place (-1 behind the rows)
+    float* lack = reinterpret_cast<float*>(lds + Tiles::LACK);
+    auto put_place = [&](int2 th, int x) {
+        const int place = ((th.x >> SELECT_BITS) * a.NS + (th.x & (SELECT_MAX - 1))) * a.R + th.y;
+        reinterpret_cast<int*>(lack)[(x & 1) * (KP + 1) * RT + KP * RT + threadIdx.x] = x * RT + (int)threadIdx.x < rows ? place : -1;
+    };
+    auto store_lack = [&](int x) {
+        const float* p = lack + (x & 1) * (KP + 1) * RT + threadIdx.x;
+        const int place = __float_as_int(p[KP * RT]);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < KP; ++i) sum += p[i * RT];
+        if (place >= 0) w.lack[(int64_t)in_group * a.Tq * a.NS * a.R + place] = sum;
     };
     struct Stat { float lse, delta; int limit; };
     auto stat_of = [&](int2 th, int x) {
-        const int64_t at = ((int64_t)b * a.H + g * a.R + th.y) * a.Tq + th.x;
-        return Stat{w.lse[at] * LOG2E, w.delta[at], x * RT + (int)threadIdx.x < rows ? len - a.Tq + th.x - key0 : -1};
+        const int t = th.x >> SELECT_BITS;
+        const int64_t at = ((int64_t)b * a.H + g * a.R + th.y) * a.Tq + t;
+        return Stat{w.lse[at] * LOG2E, w.delta[at], x * RT + (int)threadIdx.x < rows ? len - a.Tq + t - key0 : -1};
     };
     auto put_stat = [&](const Stat& s, int x) {
         float* p = stats + (x & 1) * 3 * RT + threadIdx.x;
@@ -105,18 +129,22 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1
     };
     auto put_row = [&](int2 th, int x) {
         int64_t* p = row_at + (x & 1) * 2 * RT + threadIdx.x;
-        p[0] = (th.x * q.st + th.y * q.sh) * (int64_t)sizeof(T), p[RT] = (th.x * d_o.st + th.y * d_o.sh) * (int64_t)sizeof(T);
+        const int t = th.x >> SELECT_BITS;
+        p[0] = (t * q.st + th.y * q.sh) * (int64_t)sizeof(T), p[RT] = (t * d_o.st + th.y * d_o.sh) * (int64_t)sizeof(T);
     };
     auto load_rows = [&](int x) {
         const int64_t* row = row_at + ((x & 1) * 2 + (is_q ? 0 : 1)) * RT + my_row;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) gather_to_lds(base + (row[i * R::PER_KB] + chunk[i]), to + (x & 1) * Tiles::BUFFER + i * 1024);
     };
-    int2 th2 = make_int2(0, 0);
+    constexpr bool LACKS = sizeof(T) == 2;
+    int2 th1 = make_int2(0, 0), th2 = th1;
     Stat stat1{0.f, 0.f, -1};
     if (scout) {
-        const int2 th0 = row_of(0), th1 = row_of(1);
+        const int2 th0 = row_of(0);
+        th1 = row_of(1);
         th2 = row_of(2);
+        if (LACKS) put_place(th0, 0);
         put_row(th0, 0), put_row(th1, 1);
         put_stat(stat_of(th0, 0), 0);
         stat1 = stat_of(th1, 1);
@@ -128,8 +156,11 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1
         lds_barrier();
         const char *qt = lds + (x & 1) * Tiles::BUFFER, *ot = qt + Tiles::TILE;
         if (x + 1 < steps) load_rows(x + 1);
+        if (LACKS && scout && x > 0) store_lack(x - 1);
         if (scout && x + 1 < steps) {
+            if (LACKS) put_place(th1, x + 1);
             put_stat(stat1, x + 1);
+            th1 = th2;
             put_row(th2, x);
             stat1 = stat_of(th2, x + 2);
             th2 = row_of(x + 3);
@@ -143,7 +174,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1
         const float* stat = stats + (x & 1) * 3 * RT + rg * 32 + 4 * half;
         // rows that see all of this part's keys need no comparison (those of later blocks, which are most)
         const bool cut = __any(__float_as_int(stats[(x & 1) * 3 * RT + 2 * RT + rg * 32 + i32]) < kp * 32 + 31);
-        Operand<T> pf[2], sf[2];         // P and dS, columns = keys, contraction over the rows
+        float row_sum[8];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float p[8], ds[8];
@@ -165,19 +196,33 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1
                         if (kp * 32 + i32 > i4[r]) p[e + r] = ds[e + r] = 0.f;
                 }
             }
-            set_operand(pf[u], p);
-            set_operand(sf[u], ds);
-        }
+            Operand<T> pf, sf;           // columns = keys, contraction over the rows
+            set_operand(pf, p);
+            set_operand(sf, ds);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                dv[d] = product32(across_rows<T, DP>(ot, rg * 32 + u * 16, d * 32, lane), pf[u], dv[d]);
-                dk[d] = product32(across_rows<T, DP>(qt, rg * 32 + u * 16, d * 32, lane), sf[u], dk[d]);
+            for (int d = 0; d < DT; ++d) {
+                dv[d] = product32(across_rows<T, DP>(ot, rg * 32 + u * 16, d * 32, lane), pf, dv[d]);
+                dk[d] = product32(across_rows<T, DP>(qt, rg * 32 + u * 16, d * 32, lane), sf, dk[d]);
             }
+            if (LACKS)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) row_sum[u * 4 + e] = sixteen_apart_sum(ds[2 * e], ds[2 * e + 1]);
+        }
+        if (LACKS) {
+            // rows of 16 lanes (half, odd): sums over their lanes of the registers 2j + odd; lane j keeps the jth
+            float mine = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float sum = lanes_sum<16>(row_sum[j]);
+                if ((lane & 15) == j) mine = sum;
+            }
+            const int n = 2 * (lane & 7) + ((lane >> 4) & 1);
+            if ((lane & 15) < 8) lack[((x & 1) * (KP + 1) + kp) * RT + rg * 32 + 8 * (n / 4) + 4 * half + n % 4] = mine;
+        }
     }
+    __syncthreads();
+    if (LACKS && scout) store_lack(steps - 1);
     if (RG == 2) {                       // the second group of rows to the first
-        __syncthreads();
         float* sums = reinterpret_cast<float*>(lds) + kp * (DT * 32 * 64) + lane;
         if (rg == 1)
 #pragma unroll
@@ -215,6 +260,18 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) == 4 ? 1
             store4(out + c, dk[d][r], dk[d][r + 1], dk[d][r + 2], dk[d][r + 3]);
             store4(out + (int64_t)a.BK * a.D + c, dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]);
         }
+}
+
+// delta of a row and what it lacked, block after block
+__global__ __launch_bounds__(256) void k_attention_delta_whole(AttentionArgs a, Plan plan, int bg0, const float* __restrict__ lack, float* __restrict__ delta) {
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;                       // (query, head) of a key head
+    if (row >= (int64_t)a.Tq * a.R) return;
+    const int t = (int)(row / a.R), h = (int)(row - (int64_t)t * a.R), bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G;
+    const int* blocks = plan.rows + ((int64_t)bg * a.Tq + t) * a.NS;
+    const float* p = lack + ((int64_t)blockIdx.y * a.Tq + t) * a.NS * a.R + h;
+    float sum = 0.f;
+    for (int s = 0; s < a.NS && blocks[s] < a.nb; ++s) sum += p[s * a.R];
+    delta[((int64_t)b * a.H + g * a.R + h) * a.Tq + t] += sum;
 }
 
 // dK and dV of four components of a key whose block has no item or several: their sum, in order
@@ -309,10 +366,15 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
                     float y[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = exp2_fast(__builtin_fmaf(s[u * 8 + e], scale2, -less)) * (dp[u * 8 + e] - dl);
-                    Operand<T> sf;
+                    Operand<T> sf, low;
                     set_operand(sf, y);
+                    if (sizeof(T) == 2) set_operand_rest(low, sf, y);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) acc[d] = product32(across_rows<T, DP>(tile, st * 32 + u * 16, d * 32, lane), sf, acc[d]);
+                    for (int d = 0; d < DT; ++d) {
+                        const Operand<T> keys = across_rows<T, DP>(tile, st * 32 + u * 16, d * 32, lane);
+                        acc[d] = product32(keys, sf, acc[d]);
+                        if (sizeof(T) == 2) acc[d] = product32(keys, low, acc[d]);
+                    }
                 }
             }
         }
@@ -331,7 +393,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
 
 struct BwdSpace {
     int group, max_items;                // (batch, key head) that a launch takes
-    size_t delta, total;
+    size_t delta, dkv, total;
 };
 
 BwdSpace bwd_space(const mst_attention_shape* s) {
@@ -339,9 +401,10 @@ BwdSpace bwd_space(const mst_attention_shape* s) {
     BwdSpace w;
     w.max_items = carve_plan(nullptr, a).max_items;
     w.delta = align_up((size_t)a.B * a.H * a.Tq * 4);
-    const size_t one = (size_t)w.max_items * 2 * a.BK * a.D * 4;
-    w.group = (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(one, 1)));
-    w.total = std::max<size_t>(256, w.delta + align_up(w.group * one));
+    const size_t one = (size_t)w.max_items * 2 * a.BK * a.D * 4, lack = s->type == MST_BF16 ? (size_t)a.Tq * a.NS * a.R * 4 : 0;
+    w.group = (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(one + lack, 1)));
+    w.dkv = align_up(w.group * one);
+    w.total = std::max<size_t>(256, w.delta + w.dkv + align_up(w.group * lack));
     return w;
 }
 
@@ -358,6 +421,10 @@ int launch_dkv(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, con
         MST_LAUNCH_CHECK();
         k_attention_dkv_join<T><<<dim3((unsigned)cdiv((int64_t)a.S * (a.D / 4), 256), n), 256, 0, st>>>(a, plan, bg, w, dk, dv);
         MST_LAUNCH_CHECK();
+        if (sizeof(T) == 2 && a.Tq > 0) {
+            k_attention_delta_whole<<<dim3((unsigned)cdiv((int64_t)a.Tq * a.R, 256), n), 256, 0, st>>>(a, plan, bg, w.lack, const_cast<float*>(w.delta));
+            MST_LAUNCH_CHECK();
+        }
     }
     return MST_OK;
 }
@@ -410,7 +477,7 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
     const Plan plan = carve_plan(const_cast<void*>(plan_dev), a);
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* base = static_cast<char*>(ws);
-    const BwdArgs w{lse, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + sp.delta)};
+    const BwdArgs w{lse, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + sp.delta), reinterpret_cast<float*>(base + sp.delta + sp.dkv)};
     int status = MST_OK;
     with_type(s->type, [&](auto type) {
         using T = decltype(type);

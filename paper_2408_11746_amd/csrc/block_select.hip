@@ -555,7 +555,7 @@ __global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan p
         const int j = row[s];
         int at = start[j] + before[j] + __popc(bits[j * 8 + word] & ((1u << (threadIdx.x & 31)) - 1));
         for (int w = 0; w < word; ++w) at += __popc(bits[j * 8 + w]);
-        list[at] = t0 + (int)threadIdx.x;
+        list[at] = (t0 + (int)threadIdx.x) << SELECT_BITS | s;
     }
 }
 

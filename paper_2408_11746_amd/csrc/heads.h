@@ -8,7 +8,7 @@
 namespace mst {
 
 constexpr int HEAD_DIM_MAX = 128;        // of the attention; head_dim is a multiple of 8
-constexpr int SELECT_MAX = 64;           // blocks a query may select: one bit each in a word
+constexpr int SELECT_MAX = 64, SELECT_BITS = 6;      // blocks a query may select; a pair is query << 6 | place in its row
 constexpr int KEY_BLOCKS_MAX = 2048;     // blocks of a sequence: their bit words for 256 queries are 64 KB of LDS
 constexpr int64_t HEADS_MAX = 1 << 16;
 constexpr int LDS_BYTES = 160 * 1024;     // of a CU
@@ -124,6 +124,17 @@ __device__ inline void set_operand(Operand<float>& o, const float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) o.v[i] = x[i];
 }
+// what the rounding to `o` left: x - o, rounded in turn
+__device__ inline void set_operand_rest(Operand<bf16>& rest, const Operand<bf16>& o, const float (&x)[8]) {
+    uint4 w;
+    __builtin_memcpy(&w, &o.v, 16);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[2 * i] = x[2 * i] - __uint_as_float(u[i] << 16), y[2 * i + 1] = x[2 * i + 1] - __uint_as_float(u[i] & 0xFFFF0000u);
+    set_operand(rest, y);
+}
+__device__ inline void set_operand_rest(Operand<float>&, const Operand<float>&, const float (&)[8]) {}
 __device__ inline floatx16 product32(const Operand<bf16>& a, const Operand<bf16>& b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
 }
@@ -244,6 +255,12 @@ __device__ inline V over_lanes(V x, F&& f) {
     if (WIDTH >= 32) x = apart<16>(x, f);
     if (WIDTH >= 64) x = apart<32>(x, f);
     return x;
+}
+// in rows of 16 lanes: the sum of x over this row and the odd one behind it where the row is even, else that of y over the one before and this
+__device__ inline float sixteen_apart_sum(float x, float y) {
+    typedef unsigned uint2v __attribute__((ext_vector_type(2)));
+    const uint2v r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 template <int WIDTH>
 __device__ inline float lanes_sum(float x) { return over_lanes<WIDTH>(x, [](float a, float b) { return a + b; }); }
