@@ -247,6 +247,7 @@ extern "C" int mst_block_attention_fwd(const mst_attention_shape* s, const mst_h
                                        const mst_heads* o, float* lse, void* ws, size_t ws_bytes, mst_stream_t stream) {
     using namespace mst;
     if (int e = check_attention(s)) return e;
+    if (s->batch == 0 || s->queries == 0) return MST_OK;       // (empty buffers may be null)
     if (int e = check_heads(q, s->batch, s->queries, s->heads, s->type, false)) return e;
     if (int e = check_keys(s, k, false)) return e;
     if (int e = check_keys(s, v, false)) return e;
@@ -254,7 +255,6 @@ extern "C" int mst_block_attention_fwd(const mst_attention_shape* s, const mst_h
     if (!plan_dev || !lse || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
     if (ws_bytes < mst_block_attention_workspace_bytes(s, 0)) return MST_ERR_WORKSPACE;
     const AttentionArgs a = attention_args(s);
-    if (a.B == 0 || a.Tq == 0) return MST_OK;
     const Plan plan = carve_plan(const_cast<void*>(plan_dev), a);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int tiles = (int)cdiv(a.Tq, COLS / a.R);
@@ -286,13 +286,13 @@ extern "C" int mst_block_attention_decode(const mst_attention_shape* s, const ms
                                           const mst_heads* o, float* lse, mst_stream_t stream) {
     using namespace mst;
     if (int e = check_attention(s)) return e;
+    if (s->batch == 0 || s->queries == 0) return MST_OK;       // (empty buffers may be null)
     if (int e = check_heads(q, s->batch, s->queries, s->heads, s->type, false)) return e;
     if (int e = check_keys(s, k, false)) return e;
     if (int e = check_keys(s, v, false)) return e;
     if (int e = check_heads(o, s->batch, s->queries, s->heads, s->type, true)) return e;
     if (!blocks || !aligned16(blocks) || !aligned16(lse)) return MST_ERR_ARG;
     const AttentionArgs a = attention_args(s);
-    if (a.B == 0 || a.Tq == 0) return MST_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     with_type(s->type, [&](auto type) {
         using T = decltype(type);
