@@ -122,99 +122,119 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
     if (half == 0) lse[((int64_t)b * a.H + h) * a.Tq + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
-// ---- single tokens: a workgroup per (query, key head, RT of its heads), a wavefront per selected block at a time.  A key is LANES
-// lanes of eight components, so a wavefront reads 64 / LANES keys in a row; with one to eight rows the products are no work
-// for matrix instructions (the reads take longer) and every value stays in registers until the wavefronts are joined.
+// ---- single tokens: a workgroup per (query, key head, RT of its heads); its wavefronts take pieces of the selected blocks in turn, the
+// next piece on its way while they work on one.  A key is LANES lanes of eight components, so a wavefront reads 64 / LANES keys in
+// a row; with one to four rows the products are no work for matrix instructions (the reads take longer) and every value stays
+// in registers, in fp32, until the wavefronts are joined.
 constexpr int DEC_THREADS = 512;
 template <typename T, int LANES, int RT>
 __global__ __launch_bounds__(DEC_THREADS) void k_attention_decode(AttentionArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, const int* __restrict__ blocks,
                                                                   Heads<T> o, float* __restrict__ lse) {
-    constexpr int KEYS = 64 / LANES, WAVES = DEC_THREADS / 64, STEPS = 32 / KEYS;    // 32 keys at a time
+    constexpr int KEYS = 64 / LANES, WAVES = DEC_THREADS / 64, PIECE = sizeof(T) == 2 ? 32 : 16, STEPS = PIECE / KEYS;
     __shared__ float part[WAVES][RT][LANES * 8];
     __shared__ float part_m[WAVES][RT], part_l[WAVES][RT];
+    __shared__ int list[SELECT_MAX];
     const int groups = (a.R + RT - 1) / RT, t = blockIdx.x / groups, r0 = (blockIdx.x - t * groups) * RT;
     const int bg = blockIdx.y, b = bg / a.G, g = bg % a.G, len = a.length(b), p = len - a.Tq + t;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane % LANES, key_of = lane / LANES;
-    const bool mine = c * 8 < a.D;
-    const int own = p >= 0 ? p / a.BK : -1;
-    const int* row = blocks + ((int64_t)bg * a.Tq + t) * a.NS;
-    float qs[RT][8], acc[RT][8], m[RT], l[RT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % LANES, key_of = lane / LANES;
+    const int own = p >= 0 ? p / a.BK : -1, at = min(c * 8, a.D - 8);          // (past head_dim: the last components again, met by zeros)
     const float scale2 = a.scale * LOG2E;
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        m[r] = -INFINITY, l[r] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qs[r][e] = acc[r][e] = 0.f;
-        if (mine && r0 + r < a.R) load8(q.at(b, t, g * a.R + r0 + r) + c * 8, qs[r]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qs[r][e] *= scale2;
-    }
     // entries that count, one lane each: above all before them and up to the own block
-    int j_lane = lane < a.NS ? row[lane] : -1, high = j_lane >= 0 && j_lane <= own ? j_lane : -1;
+    const int j = lane < a.NS ? blocks[((int64_t)bg * a.Tq + t) * a.NS + lane] : -1;
+    int high = j >= 0 && j <= own ? j : -1;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const int x = __shfl_up(high, d);
         if (lane >= d) high = max(high, x);
     }
     const int before = __shfl_up(high, 1);
-    const bool counts = j_lane >= 0 && j_lane <= own && (lane == 0 || j_lane > before);
-    uint64_t valid = __ballot(counts);
-    const int halves = a.BK / 32;
-    int n = 0;                                                 // pieces of 32 keys, dealt to the wavefronts in turn
-    for (; valid; valid &= valid - 1) {
-        const int j = __shfl(j_lane, __ffsll((unsigned long long)valid) - 1);
-        for (int half = 0; half < halves; ++half, ++n) {
-            if (n % WAVES != wave) continue;
-            const int key0 = j * a.BK + half * 32;
-            if (key0 > p) continue;
-            float ks[STEPS][8], vs[STEPS][8];
+    const bool counts = j >= 0 && j <= own && (lane == 0 || j > before);
+    const uint64_t valid = __ballot(counts);
+    if (wave == 0 && counts) list[__popcll(valid & ((1ull << lane) - 1))] = j;
+    float qs[RT][8], acc[RT][8], m[RT], l[RT];
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                const int key = key0 + s * KEYS + key_of;
+    for (int r = 0; r < RT; ++r) {
+        m[r] = -INFINITY, l[r] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ks[s][e] = vs[s][e] = 0.f;
-                if (mine && key <= p) {
-                    load8(k.at(b, key, g) + c * 8, ks[s]);
-                    load8(v.at(b, key, g) + c * 8, vs[s]);
-                }
-            }
+        for (int e = 0; e < 8; ++e) qs[r][e] = acc[r][e] = 0.f;
+        if (c * 8 < a.D && r0 + r < a.R) load8(q.at(b, t, g * a.R + r0 + r) + c * 8, qs[r]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qs[r][e] *= scale2;
+    }
+    __syncthreads();
+    const int per = a.BK / PIECE, pieces = __popcll(valid) * per;
+    struct Piece { Operand<T> k[STEPS], v[STEPS]; };
+    auto key_of_piece = [&](int n) { return list[n / per] * a.BK + n % per * PIECE; };
+    auto fetch = [&](int n, Piece& x) {
+        const int key0 = key_of_piece(n) + key_of;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) x.k[s] = load_operand(k.at(b, min(key0 + s * KEYS, p), g) + at);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) x.v[s] = load_operand(v.at(b, min(key0 + s * KEYS, p), g) + at);
+    };
+    auto work = [&](int n, const Piece& piece) {
+        const int key0 = key_of_piece(n);
+        if (key0 > p) return;                                  // (behind the query in its own block)
+        float x[RT][STEPS], y[8];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            numbers(piece.k[s], y);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                float x[STEPS], top = -INFINITY;
+                float d = 0.f;
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) {
-                    float d = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) d += qs[r][e] * ks[s][e];
-                    d = lanes_sum<LANES>(d);
-                    x[s] = key0 + s * KEYS + key_of <= p ? d : -INFINITY;
-                    top = fmaxf(top, x[s]);
-                }
-#pragma unroll
-                for (int d = LANES; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-                const float to = fmaxf(m[r], top), f = exp2f(m[r] - to);     // (key0 is visible: `to` is a number)
-                m[r] = to;
-                l[r] *= f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) acc[r][e] *= f;
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s) {
-                    const float w = exp2f(x[s] - to);
-                    l[r] += w;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[r][e] += w * vs[s][e];
-                }
+                for (int e = 0; e < 8; ++e) d += qs[r][e] * y[e];
+                d = lanes_sum<LANES>(d);
+                x[r][s] = key0 + s * KEYS + key_of <= p ? d : -INFINITY;
             }
         }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = x[r][0];
+#pragma unroll
+            for (int s = 1; s < STEPS; ++s) top = fmaxf(top, x[r][s]);
+            auto higher = [](float u, float w) { return fmaxf(u, w); };
+            if (LANES <= 8) top = higher(top, __shfl_xor(top, 8));
+            top = apart<32>(apart<16>(top, higher), higher);
+            const float to = fmaxf(m[r], top), f = exp2_fast(m[r] - to);     // (key0 is visible: `to` is a number)
+            m[r] = to;
+            l[r] *= f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[r][e] *= f;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                x[r][s] = exp2_fast(x[r][s] - to);
+                l[r] += x[r][s];
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            numbers(piece.v[s], y);
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[r][e] += x[r][s] * y[e];
+        }
+    };
+    Piece one, two;
+    int n = wave;
+    if (n < pieces) fetch(n, one);
+    for (; n < pieces; n += 2 * WAVES) {
+        if (n + WAVES < pieces) fetch(n + WAVES, two);
+        work(n, one);
+        if (n + 2 * WAVES < pieces) fetch(n + 2 * WAVES, one);
+        if (n + WAVES < pieces) work(n + WAVES, two);
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
+        auto add = [](float u, float w) { return u + w; };
+        auto over_keys = [&](float u) {
+            if (LANES <= 8) u += __shfl_xor(u, 8);
+            return apart<32>(apart<16>(u, add), add);
+        };
+        l[r] = over_keys(l[r]);
 #pragma unroll
-        for (int d = LANES; d < 64; d <<= 1) {
-            l[r] += __shfl_xor(l[r], d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[r][e] += __shfl_xor(acc[r][e], d);
-        }
+        for (int e = 0; e < 8; ++e) acc[r][e] = over_keys(acc[r][e]);
         if (key_of == 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) part[wave][r][c * 8 + e] = acc[r][e];

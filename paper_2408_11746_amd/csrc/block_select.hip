@@ -102,17 +102,6 @@ struct Query8 {
 #pragma unroll
         for (int i = 0; i < HB; ++i) raw[i] = load_operand(base + min(h0 + i, R - 1) * sh);
     }
-    __device__ static void numbers(const Operand<bf16>& o, float (&x)[8]) {
-        uint4 w;
-        __builtin_memcpy(&w, &o.v, 16);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-    __device__ static void numbers(const Operand<float>& o, float (&x)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = o.v[e];
-    }
     __device__ uint2 value() {
         float top = 0.f, x[8];
         for (int h = 0; h < R; h += HB) {

@@ -124,6 +124,17 @@ __device__ inline void set_operand(Operand<float>& o, const float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) o.v[i] = x[i];
 }
+__device__ inline void numbers(const Operand<bf16>& o, float (&x)[8]) {
+    uint4 w;
+    __builtin_memcpy(&w, &o.v, 16);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+}
+__device__ inline void numbers(const Operand<float>& o, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = o.v[e];
+}
 // what the rounding to `o` left: x - o, rounded in turn
 __device__ inline void set_operand_rest(Operand<bf16>& rest, const Operand<bf16>& o, const float (&x)[8]) {
     uint4 w;
