@@ -555,9 +555,9 @@ int mst_key_summary(const mst_attention_shape* shape, const mst_heads* k, int8_t
 int mst_block_select(const mst_attention_shape* shape, const mst_heads* q, const int8_t* sums_dev, const float* scales_dev,
                      int32_t* blocks_dev, mst_stream_t stream);
 
-/* The plan of a selection: for every block of keys the list of its queries, which forward and backward walk.  blocks_dev may be any
- * selection; an entry that is negative, past the query's own block or not above the entries before it is left out.
- * A plan holds for the shape that it was made with, whatever the inputs.  0 bytes on invalid arguments. */
+/* The plan of a selection: what of it counts, as forward and backward read it.  blocks_dev may be any selection; an entry that is negative, past
+ * the query's own block or not above the entries before it is left out.  A plan holds for the shape (and the lengths) that it was made with,
+ * whatever the inputs.  0 bytes on invalid arguments. */
 size_t mst_block_plan_bytes(const mst_attention_shape* shape);
 int mst_block_plan(const mst_attention_shape* shape, const int32_t* blocks_dev, void* plan_dev, size_t plan_bytes,
                    mst_stream_t stream);
@@ -575,7 +575,7 @@ int mst_block_attention_bwd(const mst_attention_shape* shape, const mst_heads* q
                             const mst_heads* dq, const mst_heads* dk, const mst_heads* dv,
                             void* ws_dev, size_t ws_bytes, mst_stream_t stream);
 
-/* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments. */
+/* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments.  The forward keeps nothing in it for the backward. */
 size_t mst_block_attention_workspace_bytes(const mst_attention_shape* shape, int backward);
 
 /* The forward for few queries (single tokens over a cache), from blocks_dev itself, without plan or workspace.  The same rules

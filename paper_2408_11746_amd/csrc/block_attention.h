@@ -13,32 +13,36 @@ struct AttentionArgs {
     __device__ int length(int b) const { return lengths ? min(max(lengths[b], 0), S) : S; }
 };
 
-// The selection as the kernels read it: rows without the entries that do not count, and the lists of the queries of each block
-// of keys.  bg = b G + g; a pair is an entry of a query's row: query << SELECT_BITS | place.
-constexpr int PLAN_TILE = 256;           // queries that a workgroup of the builders takes
+// The selection as the kernels read it (a plan): the rows of blocks without the entries that do not count.  bg = b G + g.
+struct Plan {
+    int* rows = nullptr;                 // [bg][Tq][NS] ascending, nb behind them
+    size_t total = 0;
+};
+inline Plan carve_plan(const void* base, const AttentionArgs& a) {
+    return {static_cast<int*>(const_cast<void*>(base)), align_up(std::max<size_t>(1, (size_t)a.B * a.G * a.Tq * a.NS * 4))};
+}
+
+// The other way round, for the gradients of keys and values: the queries of each block of keys, in the workspace.  A pair is an entry of a
+// query's row: query << SELECT_BITS | place.  Lists are made for `group` (batch, key head) at a time; gg counts those of a group.
+constexpr int LIST_TILE = 256;           // queries that a workgroup of the builders takes
 constexpr int ITEM_ROWS = 512, ITEM_ROWS_MOST = 4096;          // rows (query, head) of an item: a workgroup of the kernel that walks lists
 constexpr int ITEMS = 2048;              // and about so many items, where that makes none shorter
-struct Plan {
-    int* rows = nullptr;                 // [bg][Tq][NS] the entries of a selection that count, nb behind them
-    int* list = nullptr;                 // [bg][Tq NS] pairs, block after block, ascending inside a block
-    int* start = nullptr;                // [bg][nb + 1] first pair of a block
-    int* item_start = nullptr;           // [bg][nb + 1] first item of a block
-    int2* items = nullptr;               // [bg][max_items] block and first pair
-    int* tile = nullptr;                 // [bg][tiles][nb] pairs of a block before those of this tile of queries
+struct Lists {
+    int* list = nullptr;                 // [gg][Tq NS] pairs, block after block, ascending inside a block
+    int* start = nullptr;                // [gg][nb + 1] first pair of a block
+    int* item_start = nullptr;           // [gg][nb + 1] first item of a block
+    int2* items = nullptr;               // [gg][max_items] block and first pair
+    int* tile = nullptr;                 // [gg][tiles][nb] pairs of a block before those of this tile of queries
     int tiles = 0, max_items = 0, item_pairs = 0;
     size_t total = 0;
 };
 
-inline int item_pairs(const AttentionArgs& a) {
-    const int64_t rows = (int64_t)a.B * a.G * a.Tq * a.NS * a.R;
-    return (int)std::max<int64_t>(8, std::min<int64_t>(ITEM_ROWS_MOST, std::max<int64_t>(ITEM_ROWS, rows / ITEMS)) / a.R);
-}
-
-inline Plan carve_plan(void* base, const AttentionArgs& a) {
-    Plan p;
-    const size_t bg = (size_t)a.B * a.G, pairs = (size_t)a.Tq * a.NS;
-    p.tiles = (int)cdiv(a.Tq, PLAN_TILE);
-    p.item_pairs = item_pairs(a);
+inline Lists carve_lists(void* base, const AttentionArgs& a, size_t group) {
+    Lists p;
+    const size_t pairs = (size_t)a.Tq * a.NS;
+    const int64_t rows = (int64_t)((size_t)a.B * a.G * pairs) * a.R;
+    p.tiles = (int)cdiv(a.Tq, LIST_TILE);
+    p.item_pairs = (int)std::max<int64_t>(8, std::min<int64_t>(ITEM_ROWS_MOST, std::max<int64_t>(ITEM_ROWS, rows / ITEMS)) / a.R);
     p.max_items = a.nb + (int)cdiv((int64_t)pairs, p.item_pairs);
     char* c = static_cast<char*>(base);
     size_t at = 0;
@@ -47,15 +51,16 @@ inline Plan carve_plan(void* base, const AttentionArgs& a) {
         at = align_up(at + bytes);
         return r;
     };
-    p.rows = reinterpret_cast<int*>(take(bg * pairs * 4));
-    p.list = reinterpret_cast<int*>(take(bg * pairs * 4));
-    p.start = reinterpret_cast<int*>(take(bg * (a.nb + 1) * 4));
-    p.item_start = reinterpret_cast<int*>(take(bg * (a.nb + 1) * 4));
-    p.items = reinterpret_cast<int2*>(take(bg * p.max_items * 8));
-    p.tile = reinterpret_cast<int*>(take(bg * p.tiles * a.nb * 4));
-    p.total = std::max<size_t>(at, 256);
+    p.list = reinterpret_cast<int*>(take(group * pairs * 4));
+    p.start = reinterpret_cast<int*>(take(group * (a.nb + 1) * 4));
+    p.item_start = reinterpret_cast<int*>(take(group * (a.nb + 1) * 4));
+    p.items = reinterpret_cast<int2*>(take(group * p.max_items * 8));
+    p.tile = reinterpret_cast<int*>(take(group * p.tiles * a.nb * 4));
+    p.total = at;
     return p;
 }
+// lists of a plan's selection for the n (batch, key head) from bg0 on (block_select.hip)
+int build_lists(const AttentionArgs& a, const Plan& plan, const Lists& lists, int bg0, int n, hipStream_t s);
 
 inline int check_attention(const mst_attention_shape* s) {
     if (!s || !is_type(s->type) || !(s->scale > -1e30f && s->scale < 1e30f) || !aligned16(s->lengths_dev)) return MST_ERR_ARG;

@@ -66,7 +66,8 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
             for (int st = 0; st < ST; ++st) {
                 s[st] = zero16();
 #pragma unroll
-                for (int c = 0; c < QC; ++c) s[st] = product32(along_row<T, DP>(tile, st * 32 + i32, c * 16 + half * 8), qf[c], s[st]);
+                for (int c = 0; c < QC; ++c)
+                    if (worth<T>(c * 16, a.D)) s[st] = product32(along_row<T, DP>(tile, st * 32 + i32, c * 16 + half * 8), qf[c], s[st]);
             }
             if (__any(limit < KW - 1 && limit >= 0)) {         // some row sees some of these keys, not all
 #pragma unroll
@@ -103,8 +104,9 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d)
+                if (worth<T>(d * 32, a.D))
 #pragma unroll
-                for (int u = 0; u < 2 * ST; ++u) acc[d] = product32(across_rows<T, DP>(tile + Tiles::TILE, u * 16, d * 32, lane), pf[u], acc[d]);
+                    for (int u = 0; u < 2 * ST; ++u) acc[d] = product32(across_rows<T, DP>(tile + Tiles::TILE, u * 16, d * 32, lane), pf[u], acc[d]);
         }
         if (block_ends) cursor.pass(a, (int)(now & 0xFFFF));
     }
@@ -275,7 +277,7 @@ extern "C" int mst_block_attention_fwd(const mst_attention_shape* s, const mst_h
     if (!plan_dev || !lse || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
     if (ws_bytes < mst_block_attention_workspace_bytes(s, 0)) return MST_ERR_WORKSPACE;
     const AttentionArgs a = attention_args(s);
-    const Plan plan = carve_plan(const_cast<void*>(plan_dev), a);
+    const Plan plan = carve_plan(plan_dev, a);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int tiles = (int)cdiv(a.Tq, COLS / a.R);
     int status = MST_OK;
@@ -326,8 +328,12 @@ extern "C" int mst_block_attention_decode(const mst_attention_shape* s, const ms
             if (a.D <= 64) launch(std::integral_constant<int, 8>{}, rt);
             else launch(std::integral_constant<int, 16>{}, rt);
         };
-        if (a.R == 1) width(std::integral_constant<int, 1>{});
-        else if (a.R == 2) width(std::integral_constant<int, 2>{});
+        // as many heads to a workgroup as read the keys once, but one for each CU if there are heads (one sequence, 8 key heads of 4, 16 blocks
+        // of 64: 21.5 us with four heads to a workgroup, 11.7 with one; 64 such sequences 64 either way)
+        int rt = a.R == 1 ? 1 : a.R == 2 ? 2 : 4;
+        while (rt > 1 && (int64_t)a.B * a.G * a.Tq * cdiv(a.R, rt) < 256) rt /= 2;
+        if (rt == 1) width(std::integral_constant<int, 1>{});
+        else if (rt == 2) width(std::integral_constant<int, 2>{});
         else width(std::integral_constant<int, 4>{});
     });
     MST_LAUNCH_CHECK();

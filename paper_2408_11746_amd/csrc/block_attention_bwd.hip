@@ -1,7 +1,7 @@
 // Gradients of the attention over selected blocks (mst_block_attention_bwd).  With P = exp(scale q.k - lse),
 // delta = sum of dO O over a row and dP = dO V^T:  dS = P (dP - delta),  dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K.
 //
-// The first kernel walks the plan's lists: a workgroup takes a stretch of the rows that selected a block, whose keys and values its
+// The first kernel walks lists of the queries of each block: a workgroup takes a stretch of the rows that selected a block, whose keys and values its
 // wavefronts keep in registers, 32 keys each.  The rows' Q and dO come straight to LDS, each from its own address, and are read
 // along the rows for S and dP and across them for dK and dV, whose sums stay in registers: no two workgroups meet in one
 // sum.  A block with one item is written as it is; the sums of several items are left in fp32 and added in the order of the list.
@@ -56,7 +56,7 @@ struct DkvTiles {
 // (128 components take more registers than two wavefronts a SIMD have: so bound, it spills 170 bytes a lane, and 4099 queries of 24 heads
 // with 8 key heads take 368 us, not 281)
 template <typename T, int DP, int KP>
-__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 256 ? 1 : 2)) void k_attention_dkv(AttentionArgs a, Plan plan, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+__global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 256 ? 1 : 2)) void k_attention_dkv(AttentionArgs a, Lists lists, Heads<const T> q, Heads<const T> k, Heads<const T> v,
                                                                                Heads<const T> d_o, int bg0, int group, BwdArgs w, Heads<T> dk_out, Heads<T> dv_out) {
     using Tiles = DkvTiles<T, DP, KP>;
     using R = Rows<T, DP>;
@@ -64,10 +64,10 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
     extern __shared__ __align__(16) char lds[];
     // the items of a key head lie `group` workgroups apart: mostly on one XCD, whose L2 then holds the head's queries
     const int index = blockIdx.x / group, in_group = blockIdx.x - index * group, bg = bg0 + in_group, b = bg / a.G, g = bg % a.G;
-    if (index >= plan.item_start[(int64_t)bg * (a.nb + 1) + a.nb]) return;
-    const int2 it = plan.items[(int64_t)bg * plan.max_items + index];
-    const int block = it.x, first = it.y, end = plan.start[(int64_t)bg * (a.nb + 1) + block + 1], pairs = min(plan.item_pairs, end - first);
-    const bool alone = pairs == end - first && plan.start[(int64_t)bg * (a.nb + 1) + block] == first;      // the block's only item
+    if (index >= lists.item_start[(int64_t)in_group * (a.nb + 1) + a.nb]) return;
+    const int2 it = lists.items[(int64_t)in_group * lists.max_items + index];
+    const int block = it.x, first = it.y, end = lists.start[(int64_t)in_group * (a.nb + 1) + block + 1], pairs = min(lists.item_pairs, end - first);
+    const bool alone = pairs == end - first && lists.start[(int64_t)in_group * (a.nb + 1) + block] == first;      // the block's only item
     const int len = a.length(b), key0 = block * a.BK;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i32 = lane & 31, half = lane >> 5;
     const int kp = wave % KP, rg = wave / KP, key = key0 + kp * 32 + i32;
@@ -87,7 +87,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
 
     // The rows of step x are known two steps ahead (their queries, by the first RT threads) and their statistics one.
     const int rows = pairs * a.R, steps = (rows + RT - 1) / RT;
-    const int* list = plan.list + (int64_t)bg * a.Tq * a.NS + first;
+    const int* list = lists.list + (int64_t)in_group * a.Tq * a.NS + first;
     int64_t* row_at = reinterpret_cast<int64_t*>(lds + Tiles::ROWS);               // [2][2][RT] byte offsets of a row's Q and dO from the batch's
     float* stats = reinterpret_cast<float*>(lds + Tiles::STATS);                   // [2][3][RT] log-sum, delta, last key that it sees
     const bool scout = (int)threadIdx.x < RT;
@@ -168,6 +168,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
         floatx16 s = zero16(), dp = zero16();
 #pragma unroll
         for (int c = 0; c < QC; ++c) {
+            if (!worth<T>(c * 16, a.D)) continue;
             s = product32(along_row<T, DP>(qt, rg * 32 + i32, c * 16 + half * 8), kf[c], s);
             dp = product32(along_row<T, DP>(ot, rg * 32 + i32, c * 16 + half * 8), vf[c], dp);
         }
@@ -201,6 +202,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
             set_operand(sf, ds);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
+                if (!worth<T>(d * 32, a.D)) continue;
                 dv[d] = product32(across_rows<T, DP>(ot, rg * 32 + u * 16, d * 32, lane), pf, dv[d]);
                 dk[d] = product32(across_rows<T, DP>(qt, rg * 32 + u * 16, d * 32, lane), sf, dk[d]);
             }
@@ -250,7 +252,7 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
             }
         return;
     }
-    float* out = w.dkv + (((int64_t)in_group * plan.max_items + index) * 2 * a.BK + kp * 32 + i32) * a.D;
+    float* out = w.dkv + (((int64_t)in_group * lists.max_items + index) * 2 * a.BK + kp * 32 + i32) * a.D;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -276,17 +278,17 @@ __global__ __launch_bounds__(256) void k_attention_delta_whole(AttentionArgs a, 
 
 // dK and dV of four components of a key whose block has no item or several: their sum, in order
 template <typename T>
-__global__ __launch_bounds__(256) void k_attention_dkv_join(AttentionArgs a, Plan plan, int bg0, BwdArgs w, Heads<T> dk, Heads<T> dv) {
+__global__ __launch_bounds__(256) void k_attention_dkv_join(AttentionArgs a, Lists lists, int bg0, BwdArgs w, Heads<T> dk, Heads<T> dv) {
     const int bg = bg0 + blockIdx.y, b = bg / a.G, g = bg % a.G, units = a.D / 4;
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t key = u / units;
     if (key >= a.S) return;
     const int d = (int)(u - key * units) * 4, block = (int)(key / a.BK), in = (int)(key - (int64_t)block * a.BK);
-    const int i0 = plan.item_start[(int64_t)bg * (a.nb + 1) + block], i1 = plan.item_start[(int64_t)bg * (a.nb + 1) + block + 1];
+    const int i0 = lists.item_start[(int64_t)blockIdx.y * (a.nb + 1) + block], i1 = lists.item_start[(int64_t)blockIdx.y * (a.nb + 1) + block + 1];
     if (i1 - i0 == 1) return;
     float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
     for (int i = i0; i < i1; ++i) {
-        const float* p = w.dkv + (((int64_t)blockIdx.y * plan.max_items + i) * 2 * a.BK + in) * a.D + d;
+        const float* p = w.dkv + (((int64_t)blockIdx.y * lists.max_items + i) * 2 * a.BK + in) * a.D + d;
         const float4 s = *reinterpret_cast<const float4*>(p), z = *reinterpret_cast<const float4*>(p + (int64_t)a.BK * a.D);
         x[0] += s.x; x[1] += s.y; x[2] += s.z; x[3] += s.w;
         y[0] += z.x; y[1] += z.y; y[2] += z.z; y[3] += z.w;
@@ -295,8 +297,10 @@ __global__ __launch_bounds__(256) void k_attention_dkv_join(AttentionArgs a, Pla
     store4(dv.at(b, key, g) + d, y[0], y[1], y[2], y[3]);
 }
 
+// (three workgroups a CU at 64 components of 2 bytes, 168 registers without spilling: 8192 queries of 20 heads 236 -> 215 us, 4 x 1024 of 12
+// heads, too few workgroups to fill the card, 32.3 -> 33.2.  More components, or wider ones, take the registers of two or of one.)
 template <typename T, int DP, int KW>
-__global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void k_attention_dq(AttentionArgs a, Plan plan, UnionSpace space, int tiles, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+__global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : sizeof(T) * DP == 128 ? 3 : 2)) void k_attention_dq(AttentionArgs a, Plan plan, UnionSpace space, int tiles, Heads<const T> q, Heads<const T> k, Heads<const T> v,
                                                                  Heads<const T> d_o, const float* __restrict__ lse, const float* __restrict__ delta, Heads<T> dq) {
     using Tiles = KeyTiles<T, DP, KW>;
     constexpr int QC = DP / 16, DT = DP / 32, ST = KW / 32;
@@ -371,6 +375,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
                     if (sizeof(T) == 2) set_operand_rest(low, sf, y);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
+                        if (!worth<T>(d * 32, a.D)) continue;
                         const Operand<T> keys = across_rows<T, DP>(tile, st * 32 + u * 16, d * 32, lane);
                         acc[d] = product32(keys, sf, acc[d]);
                         if (sizeof(T) == 2) acc[d] = product32(keys, low, acc[d]);
@@ -392,24 +397,25 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
 }
 
 struct BwdSpace {
-    int group, max_items;                // (batch, key head) that a launch takes
-    size_t delta, dkv, total;
+    int group;                           // (batch, key head) that a launch takes
+    size_t lists, delta, dkv, total;
 };
 
 BwdSpace bwd_space(const mst_attention_shape* s) {
     const AttentionArgs a = attention_args(s);
     BwdSpace w;
-    w.max_items = carve_plan(nullptr, a).max_items;
+    const Lists lists = carve_lists(nullptr, a, 1);
     w.delta = align_up((size_t)a.B * a.H * a.Tq * 4);
-    const size_t one = (size_t)w.max_items * 2 * a.BK * a.D * 4, lack = s->type == MST_BF16 ? (size_t)a.Tq * a.NS * a.R * 4 : 0;
-    w.group = (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(one + lack, 1)));
+    const size_t one = (size_t)lists.max_items * 2 * a.BK * a.D * 4, lack = s->type == MST_BF16 ? (size_t)a.Tq * a.NS * a.R * 4 : 0;
+    w.group = (int)std::min<size_t>((size_t)a.B * a.G, std::max<size_t>(1, PARTIAL_BYTES / std::max<size_t>(lists.total + one + lack, 1)));
+    w.lists = carve_lists(nullptr, a, w.group).total;
     w.dkv = align_up(w.group * one);
-    w.total = std::max<size_t>(256, w.delta + w.dkv + align_up(w.group * lack));
+    w.total = std::max<size_t>(256, w.lists + w.delta + w.dkv + align_up(w.group * lack));
     return w;
 }
 
 template <typename T, int DP, int KP>
-int launch_dkv(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, const Heads<const T>& q, const Heads<const T>& k, const Heads<const T>& v, const Heads<const T>& d_o,
+int launch_dkv(const AttentionArgs& a, const Plan& plan, const Lists& lists, const BwdSpace& sp, const Heads<const T>& q, const Heads<const T>& k, const Heads<const T>& v, const Heads<const T>& d_o,
                const Heads<T>& dk, const Heads<T>& dv, const BwdArgs& w, hipStream_t st) {
     using Tiles = DkvTiles<T, DP, KP>;
     static_assert(Tiles::BYTES <= LDS_BYTES, "LDS of a CU");
@@ -417,9 +423,10 @@ int launch_dkv(const AttentionArgs& a, const Plan& plan, const BwdSpace& sp, con
     if (int e = allow_lds(reinterpret_cast<const void*>(&k_attention_dkv<T, DP, KP>), Tiles::BYTES, allowed)) return e;
     for (int bg = 0; bg < a.B * a.G; bg += sp.group) {
         const unsigned n = (unsigned)std::min(sp.group, a.B * a.G - bg);
-        k_attention_dkv<T, DP, KP><<<(unsigned)plan.max_items * n, Tiles::THREADS, Tiles::BYTES, st>>>(a, plan, q, k, v, d_o, bg, (int)n, w, dk, dv);
+        if (int e = build_lists(a, plan, lists, bg, (int)n, st)) return e;
+        k_attention_dkv<T, DP, KP><<<(unsigned)lists.max_items * n, Tiles::THREADS, Tiles::BYTES, st>>>(a, lists, q, k, v, d_o, bg, (int)n, w, dk, dv);
         MST_LAUNCH_CHECK();
-        k_attention_dkv_join<T><<<dim3((unsigned)cdiv((int64_t)a.S * (a.D / 4), 256), n), 256, 0, st>>>(a, plan, bg, w, dk, dv);
+        k_attention_dkv_join<T><<<dim3((unsigned)cdiv((int64_t)a.S * (a.D / 4), 256), n), 256, 0, st>>>(a, lists, bg, w, dk, dv);
         MST_LAUNCH_CHECK();
         if (sizeof(T) == 2 && a.Tq > 0) {
             k_attention_delta_whole<<<dim3((unsigned)cdiv((int64_t)a.Tq * a.R, 256), n), 256, 0, st>>>(a, plan, bg, w.lack, const_cast<float*>(w.delta));
@@ -474,9 +481,10 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
     const BwdSpace sp = bwd_space(s);
     if (ws_bytes < sp.total) return MST_ERR_WORKSPACE;
     const AttentionArgs a = attention_args(s);
-    const Plan plan = carve_plan(const_cast<void*>(plan_dev), a);
+    const Plan plan = carve_plan(plan_dev, a);
+    const Lists lists = carve_lists(ws, a, sp.group);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    char* base = static_cast<char*>(ws);
+    char* base = static_cast<char*>(ws) + sp.lists;
     const BwdArgs w{lse, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + sp.delta), reinterpret_cast<float*>(base + sp.delta + sp.dkv)};
     int status = MST_OK;
     with_type(s->type, [&](auto type) {
@@ -498,7 +506,7 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
         status = with_sizes(a, [&](auto dp, auto kp) {
             constexpr int DP = decltype(dp)::value, KP = decltype(kp)::value;
             if (a.S > 0)
-                if (int e = launch_dkv<T, DP, KP>(a, plan, sp, qh, kh, vh, doh, dkh, dvh, w, st)) return e;
+                if (int e = launch_dkv<T, DP, KP>(a, plan, lists, sp, qh, kh, vh, doh, dkh, dvh, w, st)) return e;
             return a.Tq == 0 ? (int)MST_OK : launch_dq<T, DP, keys_at_once<T>(KP * 32)>(a, plan, qh, kh, vh, doh, w, dqh, st);
         });
     });

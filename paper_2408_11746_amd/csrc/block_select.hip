@@ -407,27 +407,16 @@ __global__ __launch_bounds__(FEW_THREADS) void k_block_select_few(AttentionArgs 
     else take_best<32>(score, candidates, wanted, own, a.NS, out);
 }
 
-// ---- plan.  A tile of 256 queries marks its queries in one bit word of 256 a block: a query has a block once at most, so the number
-// of bits below its own is its place among the tile's.  Counts per tile, their sums over the tiles, then every pair to its place.
-// Selections go through LDS, from and to memory in order.
-struct PlanSpace {
-    int bits, rows, total;               // LDS: [nb][8] words, [256][NS + 1] (odd rows: a thread each, in different banks)
-    PlanSpace(const AttentionArgs& a) : bits(0), rows(a.nb * 32), total(a.nb * 32 + PLAN_TILE * (a.NS | 1) * 4) {}
-};
-__device__ inline void clear_bits(const AttentionArgs& a, uint32_t* bits) {
-    for (int i = threadIdx.x; i < a.nb * 8; i += PLAN_TILE) bits[i] = 0;
-}
+// ---- plan: the entries of a selection that count, in order.  Selections go through LDS, from and to memory in order.
+constexpr int PLAN_ROWS = 256;           // queries of a workgroup
 __device__ inline void rows_to_lds(const AttentionArgs& a, const int* __restrict__ from, int n, int* rows) {
-    for (int i = threadIdx.x; i < n * a.NS; i += PLAN_TILE) rows[i / a.NS * (a.NS | 1) + i % a.NS] = from[i];
+    for (int i = threadIdx.x; i < n * a.NS; i += PLAN_ROWS) rows[i / a.NS * (a.NS | 1) + i % a.NS] = from[i];      // (odd rows: a thread each, in different banks)
 }
-
-__global__ __launch_bounds__(PLAN_TILE) void k_plan_count(AttentionArgs a, const int* __restrict__ blocks, Plan plan, PlanSpace space) {
+__global__ __launch_bounds__(PLAN_ROWS) void k_plan_rows(AttentionArgs a, const int* __restrict__ blocks, Plan plan) {
     extern __shared__ __align__(16) char lds[];
-    uint32_t* bits = reinterpret_cast<uint32_t*>(lds + space.bits);
-    int* rows = reinterpret_cast<int*>(lds + space.rows);
-    const int bg = blockIdx.y, t0 = blockIdx.x * PLAN_TILE, n = min(PLAN_TILE, a.Tq - t0);
+    int* rows = reinterpret_cast<int*>(lds);
+    const int bg = blockIdx.y, t0 = blockIdx.x * PLAN_ROWS, n = min(PLAN_ROWS, a.Tq - t0);
     const int64_t first = ((int64_t)bg * a.Tq + t0) * a.NS;
-    clear_bits(a, bits);
     rows_to_lds(a, blocks + first, n, rows);
     __syncthreads();
     if ((int)threadIdx.x < n) {
@@ -436,18 +425,36 @@ __global__ __launch_bounds__(PLAN_TILE) void k_plan_count(AttentionArgs a, const
         int last = -1, kept = 0;
         for (int s = 0; s < a.NS; ++s) {
             const int j = row[s];
-            if (j > last && j <= own) {
-                row[kept++] = j;
-                atomicOr(&bits[j * 8 + (threadIdx.x >> 5)], 1u << (threadIdx.x & 31));
-                last = j;
-            }
+            if (j > last && j <= own) row[kept++] = last = j;
         }
         for (; kept < a.NS; ++kept) row[kept] = a.nb;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n * a.NS; i += PLAN_TILE) plan.rows[first + i] = rows[i / a.NS * (a.NS | 1) + i % a.NS];
-    int* counts = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
-    for (int j = threadIdx.x; j < a.nb; j += PLAN_TILE) {
+    for (int i = threadIdx.x; i < n * a.NS; i += PLAN_ROWS) plan.rows[first + i] = rows[i / a.NS * (a.NS | 1) + i % a.NS];
+}
+
+// ---- lists.  A tile of 256 queries marks its queries in one bit word of 256 a block: a query has a block once at most, so the number
+// of bits below its own is its place among the tile's.  Counts per tile, their sums over the tiles, then every pair to its place.
+struct ListSpace {
+    int bits, rows, total;               // LDS: [nb][8] words, [256][NS + 1]
+    ListSpace(const AttentionArgs& a) : bits(0), rows(a.nb * 32), total(a.nb * 32 + LIST_TILE * (a.NS | 1) * 4) {}
+};
+__device__ inline void mark_tile(const AttentionArgs& a, const int* __restrict__ from, int n, uint32_t* bits, int* rows) {
+    for (int i = threadIdx.x; i < a.nb * 8; i += LIST_TILE) bits[i] = 0;
+    rows_to_lds(a, from, n, rows);
+    __syncthreads();
+    const int* row = rows + threadIdx.x * (a.NS | 1);
+    if ((int)threadIdx.x < n)
+        for (int s = 0; s < a.NS && row[s] < a.nb; ++s) atomicOr(&bits[row[s] * 8 + (threadIdx.x >> 5)], 1u << (threadIdx.x & 31));
+    __syncthreads();
+}
+__global__ __launch_bounds__(LIST_TILE) void k_list_count(AttentionArgs a, Plan plan, Lists lists, int bg0, ListSpace space) {
+    extern __shared__ __align__(16) char lds[];
+    uint32_t* bits = reinterpret_cast<uint32_t*>(lds + space.bits);
+    const int gg = blockIdx.y, t0 = blockIdx.x * LIST_TILE;
+    mark_tile(a, plan.rows + ((int64_t)(bg0 + gg) * a.Tq + t0) * a.NS, min(LIST_TILE, a.Tq - t0), bits, reinterpret_cast<int*>(lds + space.rows));
+    int* counts = lists.tile + ((int64_t)gg * lists.tiles + blockIdx.x) * a.nb;
+    for (int j = threadIdx.x; j < a.nb; j += LIST_TILE) {
         int c = 0;
 #pragma unroll
         for (int w = 0; w < 8; ++w) c += __popc(bits[j * 8 + w]);
@@ -479,14 +486,14 @@ __device__ inline int2 exclusive(int2 v, int2* total) {
 }
 
 // a workgroup per (batch, key head): `width` blocks at a time, 1024 / width stretches of the tiles side by side
-__global__ __launch_bounds__(1024) void k_plan_sums(AttentionArgs a, Plan plan, int width) {
+__global__ __launch_bounds__(1024) void k_list_sums(AttentionArgs a, Lists lists, int width) {
     __shared__ int stretch_sum[1024];
-    const int bg = blockIdx.x, stretches = 1024 / width, mine = threadIdx.x / width;
-    const int i0 = (int)((int64_t)plan.tiles * mine / stretches), i1 = (int)((int64_t)plan.tiles * (mine + 1) / stretches);
-    int* tile = plan.tile + (int64_t)bg * plan.tiles * a.nb;
-    int* start = plan.start + (int64_t)bg * (a.nb + 1);
-    int* item_start = plan.item_start + (int64_t)bg * (a.nb + 1);
-    int2* items = plan.items + (int64_t)bg * plan.max_items;
+    const int gg = blockIdx.x, stretches = 1024 / width, mine = threadIdx.x / width;
+    const int i0 = (int)((int64_t)lists.tiles * mine / stretches), i1 = (int)((int64_t)lists.tiles * (mine + 1) / stretches);
+    int* tile = lists.tile + (int64_t)gg * lists.tiles * a.nb;
+    int* start = lists.start + (int64_t)gg * (a.nb + 1);
+    int* item_start = lists.item_start + (int64_t)gg * (a.nb + 1);
+    int2* items = lists.items + (int64_t)gg * lists.max_items;
     int2 done = make_int2(0, 0);
     for (int j0 = 0; j0 < a.nb; j0 += width) {
         const int j = j0 + (int)(threadIdx.x % width);
@@ -510,36 +517,30 @@ __global__ __launch_bounds__(1024) void k_plan_sums(AttentionArgs a, Plan plan, 
                 tile[(int64_t)i * a.nb + j] = before;
                 before += c;
             }
-        const int pairs = there && mine == 0 ? whole : 0, parts = (pairs + plan.item_pairs - 1) / plan.item_pairs;
+        const int pairs = there && mine == 0 ? whole : 0, parts = (pairs + lists.item_pairs - 1) / lists.item_pairs;
         int2 all;
         const int2 at = exclusive(make_int2(pairs, parts), &all);          // (the threads of the first stretch come first)
         if (there && mine == 0) {
             start[j] = done.x + at.x;
             item_start[j] = done.y + at.y;
-            for (int i = 0; i < parts; ++i) items[done.y + at.y + i] = make_int2(j, done.x + at.x + i * plan.item_pairs);
+            for (int i = 0; i < parts; ++i) items[done.y + at.y + i] = make_int2(j, done.x + at.x + i * lists.item_pairs);
         }
         done.x += all.x, done.y += all.y;
     }
     if (threadIdx.x == 0) start[a.nb] = done.x, item_start[a.nb] = done.y;
 }
 
-__global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan plan, PlanSpace space) {
+__global__ __launch_bounds__(LIST_TILE) void k_list_fill(AttentionArgs a, Plan plan, Lists lists, int bg0, ListSpace space) {
     extern __shared__ __align__(16) char lds[];
     uint32_t* bits = reinterpret_cast<uint32_t*>(lds + space.bits);
     int* rows = reinterpret_cast<int*>(lds + space.rows);
-    const int bg = blockIdx.y, t0 = blockIdx.x * PLAN_TILE, n = min(PLAN_TILE, a.Tq - t0), word = threadIdx.x >> 5;
-    clear_bits(a, bits);
-    rows_to_lds(a, plan.rows + ((int64_t)bg * a.Tq + t0) * a.NS, n, rows);
-    __syncthreads();
+    const int gg = blockIdx.y, t0 = blockIdx.x * LIST_TILE, n = min(LIST_TILE, a.Tq - t0), word = threadIdx.x >> 5;
+    mark_tile(a, plan.rows + ((int64_t)(bg0 + gg) * a.Tq + t0) * a.NS, n, bits, rows);
+    if ((int)threadIdx.x >= n) return;
     const int* row = rows + threadIdx.x * (a.NS | 1);
-    const bool there = (int)threadIdx.x < n;
-    if (there)
-        for (int s = 0; s < a.NS && row[s] < a.nb; ++s) atomicOr(&bits[row[s] * 8 + word], 1u << (threadIdx.x & 31));
-    __syncthreads();
-    if (!there) return;
-    const int* before = plan.tile + ((int64_t)bg * plan.tiles + blockIdx.x) * a.nb;
-    const int* start = plan.start + (int64_t)bg * (a.nb + 1);
-    int* list = plan.list + (int64_t)bg * a.Tq * a.NS;
+    const int* before = lists.tile + ((int64_t)gg * lists.tiles + blockIdx.x) * a.nb;
+    const int* start = lists.start + (int64_t)gg * (a.nb + 1);
+    int* list = lists.list + (int64_t)gg * a.Tq * a.NS;
     for (int s = 0; s < a.NS && row[s] < a.nb; ++s) {
         const int j = row[s];
         int at = start[j] + before[j] + __popc(bits[j * 8 + word] & ((1u << (threadIdx.x & 31)) - 1));
@@ -552,6 +553,30 @@ __global__ __launch_bounds__(PLAN_TILE) void k_plan_fill(AttentionArgs a, Plan p
 constexpr int FEW_QUERIES = 16;
 
 }  // namespace
+
+int build_lists(const AttentionArgs& a, const Plan& plan, const Lists& lists, int bg0, int n, hipStream_t st) {
+    const dim3 grid((unsigned)lists.tiles, (unsigned)n);
+    const ListSpace space(a);                                   // 129 KB at most
+    static uint64_t allowed_count = 0, allowed_fill = 0;
+    if (space.total > 64 * 1024) {
+        if (int e = allow_lds(reinterpret_cast<const void*>(&k_list_count), LDS_BYTES, allowed_count)) return e;
+        if (int e = allow_lds(reinterpret_cast<const void*>(&k_list_fill), LDS_BYTES, allowed_fill)) return e;
+    }
+    if (lists.tiles > 0) {
+        k_list_count<<<grid, LIST_TILE, space.total, st>>>(a, plan, lists, bg0, space);
+        MST_LAUNCH_CHECK();
+    }
+    int width = 16;                                             // blocks that the threads of the sums stand for: a power of two
+    while (width < a.nb && width < 1024) width *= 2;
+    k_list_sums<<<(unsigned)n, 1024, 0, st>>>(a, lists, width);
+    MST_LAUNCH_CHECK();
+    if (lists.tiles > 0) {
+        k_list_fill<<<grid, LIST_TILE, space.total, st>>>(a, plan, lists, bg0, space);
+        MST_LAUNCH_CHECK();
+    }
+    return MST_OK;
+}
+
 }  // namespace mst
 
 extern "C" int mst_key_summary(const mst_attention_shape* s, const mst_heads* k, int8_t* sums, float* scales, int new_tokens, mst_stream_t stream) {
@@ -624,25 +649,12 @@ extern "C" int mst_block_plan(const mst_attention_shape* s, const int32_t* block
     const AttentionArgs a = attention_args(s);
     const Plan plan = carve_plan(plan_dev, a);
     if (plan_bytes < plan.total) return MST_ERR_WORKSPACE;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)plan.tiles, (unsigned)(a.B * a.G));
-    const PlanSpace space(a);                                   // 129 KB at most
-    static uint64_t allowed_count = 0, allowed_fill = 0;
-    if (space.total > 64 * 1024) {
-        if (int e = allow_lds(reinterpret_cast<const void*>(&k_plan_count), LDS_BYTES, allowed_count)) return e;
-        if (int e = allow_lds(reinterpret_cast<const void*>(&k_plan_fill), LDS_BYTES, allowed_fill)) return e;
-    }
-    if (plan.tiles > 0) {
-        k_plan_count<<<grid, PLAN_TILE, space.total, st>>>(a, blocks, plan, space);
-        MST_LAUNCH_CHECK();
-    }
-    int width = 16;                                             // blocks that the threads of the sums stand for: a power of two
-    while (width < a.nb && width < 1024) width *= 2;
-    k_plan_sums<<<(unsigned)(a.B * a.G), 1024, 0, st>>>(a, plan, width);
+    if (a.Tq == 0) return MST_OK;
+    const size_t lds = (size_t)PLAN_ROWS * (a.NS | 1) * 4;      // 65 KB at most
+    static uint64_t allowed = 0;
+    if (lds > 64 * 1024)
+        if (int e = allow_lds(reinterpret_cast<const void*>(&k_plan_rows), LDS_BYTES, allowed)) return e;
+    k_plan_rows<<<dim3((unsigned)cdiv(a.Tq, PLAN_ROWS), (unsigned)(a.B * a.G)), PLAN_ROWS, lds, static_cast<hipStream_t>(stream)>>>(a, blocks, plan);
     MST_LAUNCH_CHECK();
-    if (plan.tiles > 0) {
-        k_plan_fill<<<grid, PLAN_TILE, space.total, st>>>(a, plan, space);
-        MST_LAUNCH_CHECK();
-    }
     return MST_OK;
 }

@@ -154,6 +154,10 @@ __device__ inline floatx16 product32(const Operand<float>& a, const Operand<floa
     for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], c, 0, 0, 0);
     return c;
 }
+// components from `d` on are there?  fp32 products take eight instructions, each twice the time of bfloat16's one: they are left out where
+// head_dim ends before the padded width does (80 components: 5 of 8 and 3 of 4).  bfloat16 ones are not worth the branch.
+template <typename T>
+__device__ inline bool worth(int d, int D) { return sizeof(T) == 2 || d == 0 || d < D; }
 __device__ inline floatx16 zero16() {
     floatx16 z;
 #pragma unroll

@@ -275,3 +275,24 @@ def test_few_queries_of_no_sequence():
     run = Run(q, k, k, np.zeros((2, 2, 3, 1), dtype=np.int32), 32, 1.0, "f32", None, q)
     assert (run.o == 0).all() and torch.isneginf(run.lse).all() and (run.dq == 0).all()
     assert (Run(q, k, k, np.zeros((2, 2, 3, 1), dtype=np.int32), 32, 1.0, "f32", decode=True).o == 0).all()
+
+
+def test_gradients_of_many_key_heads_over_a_long_cache():
+    # more than the workspace takes at a time: the key heads go in two groups, to the same bits as heads by themselves
+    T, S, G, D, block, n_select = 64, 262144, 24, 8, 128, 4
+    torch.manual_seed(16)
+    q, d_o = (torch.randn(1, T, G, D, device=DEV).bfloat16() for _ in range(2))
+    k, v = (torch.randn(1, S, G, D, device=DEV).bfloat16() for _ in range(2))
+    rng = np.random.default_rng(16)
+    nb = S // block
+    before = np.sort(rng.integers(0, nb - 1, (1, G, T, n_select - 1)), axis=-1)     # some twice
+    blocks = np.concatenate([before, np.full((1, G, T, 1), nb - 1)], axis=-1).astype(np.int32)
+    shape = mst.BlockAttentionShape(1, T, S, G, G, D, block, n_select, 0.3, mst.MST_BF16)
+    one = mst.BlockAttentionShape(1, T, S, 1, 1, D, block, n_select, 0.3, mst.MST_BF16)
+    assert mst.mst_block_attention_workspace_bytes(shape, True) < 20 * mst.mst_block_attention_workspace_bytes(one, True)      # (not 24)
+    run = Run(q, k, v, blocks, block, 0.3, "bf16", None, d_o)
+    for g in (0, 14, 15, 23):
+        head = [x[:, :, g:g + 1].contiguous() for x in (q, k, v, d_o)]
+        alone = Run(*head[:3], blocks[:, g:g + 1], block, 0.3, "bf16", None, head[3])
+        for name in ("o", "dq", "dk", "dv"):
+            assert torch.equal(getattr(run, name)[:, :, g:g + 1], getattr(alone, name)), (g, name)
