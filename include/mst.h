@@ -15,6 +15,14 @@
  * and around them the per-layer density allocation of Sec. 3.2, the FLOP counts of
  * App. "FLOP Calculation" and the strided attention pattern of Sec. 3.3.
  *
+ * Between the qkv and the proj product of a block, the attention half:
+ *
+ *   mst_qk_norm_rotate[_bwd]          norm of every query and key head and the rotation by its position
+ *   mst_key_summary, mst_block_select the blocks of keys that a query reads, by an 8-bit score
+ *   mst_block_plan                    a selection as forward and backward read it
+ *   mst_block_attention_fwd, _bwd     attention over the selected blocks and its gradients
+ *   mst_block_attention_decode        the same for single tokens over a cache
+ *
  * Conventions
  *   - Every pointer named *_dev is DEVICE memory, owned by the caller, 16-byte aligned;
  *     everything else is host memory.  The library allocates no device memory: the
@@ -526,7 +534,11 @@ size_t mst_qk_norm_rotate_workspace_bytes(const mst_qk_shape* shape);
  * len_b < queries is a sequence padded on the left, whose first queries (p < 0) are rows without keys: output 0, log-sum -inf,
  * gradient 0.  Keys and values at or past len_b are never used, whatever they hold.  Keys are cut into blocks of
  * `block`; a query's own block is the one that holds p.  heads / kv_heads query heads share a key head and one
- * selection of blocks. */
+ * selection of blocks.
+ * Heads below len_b are finite numbers (a value that is not reaches the results of other queries too: their weight 0 times
+ * infinity is no number).
+ * Refused as MST_ERR_SHAPE beside what the fields say: batch kv_heads > 65535; queries >= 2^25; queries n_select heads / kv_heads >= 2^30;
+ * keys or values whose token stride is above 2^22 elements.  With batch 0, and in calls that have nothing to write, buffers may be NULL. */
 typedef struct {
     int32_t batch, queries, keys;   /* >= 0; keys <= 2048 block */
     int32_t heads, kv_heads;        /* heads a multiple of kv_heads, at most 64 times as many */
@@ -540,8 +552,10 @@ typedef struct {
 
 /* Summaries of complete blocks of keys: sums_dev int8 [batch x kv_heads x ceil(keys / block) x head_dim] and scales_dev fp32
  * [batch x kv_heads x ceil(keys / block)], the sum of a block's keys in 8 bits a component and the value of its unit, a
- * power of two.  With E = floor(log2 max |key|) over the block (taken into -100 .. 100):  k8 = round(key 2^(6 - E)) into -127 .. 127,  s = sum over the keys,  r = max(0, floor(log2 max |s|) - 6),
- * sums = round(s 2^-r) into -127 .. 127,  scales = 2^(E - 6 + r); rounding is to nearest even.  A block of zeros has E = -100; keys that are not finite give some sums.
+ * power of two.  With E = floor(log2 max |key|) over the block (taken into -100 .. 100):
+ *   k8 = round(key 2^(6 - E)) into -127 .. 127,  s = sum over the keys,  r = max(0, floor(log2 max |s|) - 6),
+ *   sums = round(s 2^-r) into -127 .. 127,       scales = 2^(E - 6 + r);
+ * rounding is to nearest even.  A block of zeros has E = -100; keys that are not finite give some sums.
  * Only blocks that the last new_tokens keys of their sequence completed are written (new_tokens >= keys: all complete blocks), so a
  * cache's summaries are kept up token by token; entries of other blocks stay as they are. */
 int mst_key_summary(const mst_attention_shape* shape, const mst_heads* k, int8_t* sums_dev, float* scales_dev,
@@ -575,7 +589,9 @@ int mst_block_attention_bwd(const mst_attention_shape* shape, const mst_heads* q
                             const mst_heads* dq, const mst_heads* dk, const mst_heads* dv,
                             void* ws_dev, size_t ws_bytes, mst_stream_t stream);
 
-/* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments.  The forward keeps nothing in it for the backward. */
+/* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments.  The backward's: 4 bytes a row (query, head) and up to 256 MB of
+ * lists and partial sums (more if one key head takes more); the forward, whose sums stay in registers, asks for 256 bytes and keeps nothing in
+ * them for the backward. */
 size_t mst_block_attention_workspace_bytes(const mst_attention_shape* shape, int backward);
 
 /* The forward for few queries (single tokens over a cache), from blocks_dev itself, without plan or workspace.  The same rules

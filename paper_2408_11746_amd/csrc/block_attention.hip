@@ -127,12 +127,12 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
 // ---- single tokens: a workgroup per (query, key head, RT of its heads); its wavefronts take pieces of the selected blocks in turn, the
 // next piece on its way while they work on one.  A key is LANES lanes of eight components, so a wavefront reads 64 / LANES keys in
 // a row; with one to four rows the products are no work for matrix instructions (the reads take longer) and every value stays
-// in registers, in fp32, until the wavefronts are joined.
-constexpr int DEC_THREADS = 512;
-template <typename T, int LANES, int RT>
-__global__ __launch_bounds__(DEC_THREADS) void k_attention_decode(AttentionArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, const int* __restrict__ blocks,
+// in registers, in fp32, until the wavefronts are joined.  Bound by memory: 64 sequences, 8 key heads of 4 heads of 128, 16 blocks of 64 of
+// up to 16384 tokens, 268 MB of keys and values, take 53 us (5.1 TB/s; part of them from the last level's cache).
+template <typename T, int LANES, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_attention_decode(AttentionArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, const int* __restrict__ blocks,
                                                                   Heads<T> o, float* __restrict__ lse) {
-    constexpr int KEYS = 64 / LANES, WAVES = DEC_THREADS / 64, PIECE = sizeof(T) == 2 ? 32 : 16, STEPS = PIECE / KEYS;
+    constexpr int KEYS = 64 / LANES, PIECE = sizeof(T) == 2 ? 32 : 16, STEPS = PIECE / KEYS;
     __shared__ float part[WAVES][RT][LANES * 8];
     __shared__ float part_m[WAVES][RT], part_l[WAVES][RT];
     __shared__ int list[SELECT_MAX];
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(DEC_THREADS) void k_attention_decode(AttentionArgs 
         }
     }
     __syncthreads();
-    for (int u = threadIdx.x; u < RT * LANES * 2; u += DEC_THREADS) {          // four components of a head to a thread
+    for (int u = threadIdx.x; u < RT * LANES * 2; u += WAVES * 64) {          // four components of a head to a thread
         const int r = u / (LANES * 2), d = (u - r * (LANES * 2)) * 4;
         if (r0 + r >= a.R || d >= a.D) continue;
         float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -320,21 +320,26 @@ extern "C" int mst_block_attention_decode(const mst_attention_shape* s, const ms
         using T = decltype(type);
         const Heads<const T> qh = heads_of<const T>(q), kh = heads_of<const T>(k), vh = heads_of<const T>(v);
         const Heads<T> oh = heads_of<T>(o);
-        auto launch = [&](auto lanes, auto rt) {
-            constexpr int L = decltype(lanes)::value, RT = decltype(rt)::value;
-            k_attention_decode<T, L, RT><<<dim3((unsigned)(cdiv(a.R, RT) * a.Tq), (unsigned)(a.B * a.G)), DEC_THREADS, 0, st>>>(a, qh, kh, vh, blocks, oh, lse);
+        auto launch = [&](auto lanes, auto rt, auto waves) {
+            constexpr int L = decltype(lanes)::value, RT = decltype(rt)::value, WAVES = decltype(waves)::value;
+            k_attention_decode<T, L, RT, WAVES><<<dim3((unsigned)(cdiv(a.R, RT) * a.Tq), (unsigned)(a.B * a.G)), WAVES * 64, 0, st>>>(a, qh, kh, vh, blocks, oh, lse);
         };
-        auto width = [&](auto rt) {
-            if (a.D <= 64) launch(std::integral_constant<int, 8>{}, rt);
-            else launch(std::integral_constant<int, 16>{}, rt);
+        auto width = [&](auto rt, auto waves) {
+            if (a.D <= 64) launch(std::integral_constant<int, 8>{}, rt, waves);
+            else launch(std::integral_constant<int, 16>{}, rt, waves);
         };
-        // as many heads to a workgroup as read the keys once, but one for each CU if there are heads (one sequence, 8 key heads of 4, 16 blocks
-        // of 64: 21.5 us with four heads to a workgroup, 11.7 with one; 64 such sequences 64 either way)
+        // As many heads to a workgroup as read the keys once, but one for each CU if there are heads (one sequence, 8 key heads of 4, 16 blocks
+        // of 64: 21.5 us with four heads to a workgroup, 11.7 with one).  Eight wavefronts where workgroups are still too few for the card,
+        // four where CUs hold several (that sequence 11.7 with eight, 12.6 with four; two key heads of 16, 32 blocks of 128: 31 and 39;
+        // 64 sequences of 8 key heads of 4: 63 and 53).
+        constexpr int CUS = 256;
+        auto groups = [&](int rt) { return (int64_t)a.B * a.G * a.Tq * cdiv(a.R, rt); };
         int rt = a.R == 1 ? 1 : a.R == 2 ? 2 : 4;
-        while (rt > 1 && (int64_t)a.B * a.G * a.Tq * cdiv(a.R, rt) < 256) rt /= 2;
-        if (rt == 1) width(std::integral_constant<int, 1>{});
-        else if (rt == 2) width(std::integral_constant<int, 2>{});
-        else width(std::integral_constant<int, 4>{});
+        while (rt > 1 && groups(rt) < CUS) rt /= 2;
+        if (groups(rt) < CUS) width(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+        else if (rt == 1) width(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+        else if (rt == 2) width(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+        else width(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
     });
     MST_LAUNCH_CHECK();
     return MST_OK;

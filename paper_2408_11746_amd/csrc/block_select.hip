@@ -166,6 +166,9 @@ __device__ inline void merge_best(float (&x)[KK]) {
                 x[e] = hi, x[e + d] = lo;
             }
 }
+// Measured, 8192 queries of 20 heads over 128 blocks: 36.2 us, 42.6 with the scores formed again; HB = 4 heads at a time 40.2.  16384 queries of 32 heads
+// with 8 key heads over 256 blocks: 63.5 us, 70.5 with the scores formed again; HB = 1 71.0.  Bound by the vector instructions: 8-bit queries, insertions,
+// merges (the matrix instructions are busy in 1 % of the clocks).
 constexpr int SELECT_THREADS = 256, SELECT_CHUNK = 64, SELECT_HELD = 256;
 template <typename T, int KK, int HB, bool HELD>
 __global__ __launch_bounds__(SELECT_THREADS) void k_block_select(AttentionArgs a, Heads<const T> q, const int8_t* __restrict__ sums,
@@ -549,8 +552,10 @@ __global__ __launch_bounds__(LIST_TILE) void k_list_fill(AttentionArgs a, Plan p
     }
 }
 
-// fewer queries than this: a workgroup for each
-constexpr int FEW_QUERIES = 16;
+// Fewer (query, key head) than this: a workgroup for each.  The other kernel walks the summaries one chunk after the other, whatever the number of
+// queries, and leaves most of the card idle until there are many.  (8 key heads, 256 blocks: 64 queries 7.2 us against 19.2; 16 x 12 key heads, 64
+// blocks: 4 queries 6.6 against 7.5, 8 queries 11.1 against 7.5.)
+constexpr int FEW_QUERIES = 1024;
 
 }  // namespace
 
@@ -609,7 +614,7 @@ extern "C" int mst_block_select(const mst_attention_shape* s, const mst_heads* q
     with_type(s->type, [&](auto t) {
         using T = decltype(t);
         const Heads<const T> qh = heads_of<const T>(q);
-        if (a.Tq < FEW_QUERIES) {
+        if ((int64_t)a.Tq * a.B * a.G < FEW_QUERIES) {
             k_block_select_few<T><<<dim3((unsigned)a.Tq, (unsigned)(a.B * a.G)), FEW_THREADS, 0, st>>>(a, qh, sums, scales, blocks);
             return;
         }

@@ -2,7 +2,7 @@
 //
 // A head vector lies in one group of lanes, two quads of components to a lane, such that a lane has both components of its
 // pairs: the rotation needs no other lane, the mean of the squares is a sum over the group, and each value is read and
-// written once.  A group takes several heads of one token in a row, so that the angles and weights are read once for them and
+// written once.  A group takes two heads of one token in a row, so that the angles and weights are read once for them and
 // their loads are on the way together.  Bound by memory at ten operations a value; few tokens by latency.
 // The backward needs no more of the forward than x: with r = 1 / sqrt(mean x^2 + eps), dn the gradient rotated back and
 // g = dn weight,  dx = r (g - x r^2 mean(g x)),  dweight = sum over the vectors of dn x r.  A lane meets the same
@@ -14,8 +14,13 @@ namespace mst {
 namespace {
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_BLOCKS = 1024;        // workgroups of the backward: rows of the weights' partial sums, at most
-constexpr int NORM_HEADS = 4;            // heads of a token that a group takes
+// Workgroups of the backward, at most: rows of the weights' partial sums.  (16 x 1024 tokens of 16 + 16 heads of 64: 41.7 us with 1024 of them, 44.0
+// with 2048, 46.0 with 4096; 3 x 1531 of 16 + 4 heads of 128 in fp32 28.1, 30.0 and 34.9)
+constexpr int NORM_BLOCKS = 1024;
+// Heads of a token that a group takes: with one the angles are read for every head, with more the registers let fewer groups be on their way.  (forward
+// of 8 x 1024 tokens of 20 + 20 heads, one, two, four, eight heads: 24.0, 21.8, 23.2, 23.4 us; the first backward above 46.2, 41.7, 49.1, 69.3; 32 single
+// tokens of 12 + 12 heads 3.6, 3.8, 4.6, 6.3)
+constexpr int NORM_HEADS = 2;
 
 // which components a lane has.  HALVES: pairs (i, i + rotated / 2), whole quads of them; PAIRS: (2i, 2i + 1); APART: pairs
 // (i, i + rotated / 2) where rotated / 2 is no multiple of 4, the other component read where it lies.

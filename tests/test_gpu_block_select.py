@@ -140,3 +140,64 @@ def test_what_is_not_finite_still_selects_blocks_of_the_sequence():
     for t, row in enumerate(rows):
         own, kept = t // block, [j for j in row if j >= 0]
         assert kept == sorted(set(kept)) and kept[-1] == own and len(kept) == min(n_select, own + 1) and (row[len(kept):] == -1).all()
+
+
+CASES_OF_MANY = [
+    (1, 1100, 1100, 2, 2, 64, 32, 4, "bf16", None),
+    (2, 650, 650, 6, 2, 40, 32, 3, "f32", [650, 77]),               # left-padded
+    (9, 70, 300, 8, 2, 128, 64, 2, "bf16", [300, 190] * 4 + [70]),
+    (200, 1, 515, 24, 6, 64, 32, 8, "bf16", [515, 32, 1, 0] * 50),  # many single tokens
+    (13, 41, 260, 40, 2, 16, 32, 4, "bf16", [260, 3, 41] * 4 + [0]),  # twenty heads to a key head
+    (5, 257, 300, 1, 1, 8, 32, 1, "bf16", None),                    # the own block alone
+    (8, 129, 160, 2, 1, 24, 32, 64, "f32", [96, 0] * 4),            # more than there are
+    (16, 65, 9000, 1, 1, 16, 32, 12, "bf16", None),                 # more blocks than stay in registers
+    (70, 17, 700, 1, 1, 16, 32, 20, "bf16", None),
+    (1, 1031, 2100, 2, 1, 104, 32, 40, "f32", None),
+]
+
+
+@pytest.mark.parametrize("B,T,S,H,G,D,block,n_select,dtype,lengths", CASES_OF_MANY)
+def test_selection_of_many_queries(B, T, S, H, G, D, block, n_select, dtype, lengths):
+    assert B * T * G >= 1024                                        # (fewer go another way)
+    test_selection(B, T, S, H, G, D, block, n_select, dtype, lengths)
+
+
+@pytest.mark.parametrize("blocks,n_select", [(100, 6), (300, 33), (1500, 64)])
+def test_ties_and_zeros_of_many_queries(blocks, n_select):
+    test_ties_and_zeros(1100, blocks, n_select)
+
+
+def test_few_and_many_queries_agree():
+    # the last queries of long sequences: all at once, and a few at a time
+    rng = np.random.default_rng(17)
+    B, T, S, H, G, D, block, n_select = 4, 300, 5000, 4, 2, 72, 32, 10
+    q, k = tensor(rng.standard_normal((B, T, H, D)), "bf16"), tensor(rng.standard_normal((B, S, G, D)), "bf16")
+    lengths = [S, 301, 299, 4000]
+    shape = _shape(B, T, S, H, G, D, block, n_select, "bf16", lengths)
+    sums, scales = _summaries(shape, k, block, S)
+    many = torch.empty(B, G, T, n_select, dtype=torch.int32, device=DEV)
+    mst.mst_block_select(shape, q, sums, scales, many)
+    for t0 in range(0, T, 100):
+        part = _shape(B, 100, S, H, G, D, block, n_select, "bf16", [n - T + t0 + 100 for n in lengths])
+        few = torch.empty(B, G, 100, n_select, dtype=torch.int32, device=DEV)
+        mst.mst_block_select(part, q[:, t0:t0 + 100], sums, scales, few)
+        torch.cuda.synchronize()
+        assert torch.equal(few, many[:, :, t0:t0 + 100])
+
+
+def test_what_is_not_finite_among_many_queries():
+    B, S, H, G, D, block, n_select = 4, 320, 2, 1, 16, 32, 4
+    q, k = torch.randn(B, S, H, D, device=DEV), torch.randn(B, S, G, D, device=DEV)
+    q[0, ::3, 0, 0] = float("nan")
+    q[1, 1::3, 1, 2] = float("inf")
+    k[2, ::50] = float("-inf")
+    k[3, 7] = float("nan")
+    shape = _shape(B, S, S, H, G, D, block, n_select, "f32")
+    sums, scales = _summaries(shape, k, block, S)
+    got = torch.empty(B, G, S, n_select, dtype=torch.int32, device=DEV)
+    mst.mst_block_select(shape, q, sums, scales, got)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for t, row in enumerate(got.cpu().numpy()[b, 0]):
+            own, kept = t // block, [j for j in row if j >= 0]
+            assert kept == sorted(set(kept)) and kept[-1] == own and len(kept) == min(n_select, own + 1) and (row[len(kept):] == -1).all()
