@@ -7,11 +7,16 @@
 // sum.  A block with one item is written as it is; the sums of several items are left in fp32 and added in the order of the list.
 // The second works like the forward: rows that own their dQ walk the union of their blocks.
 //
+// Measured, 8192 queries of 20 heads of 64, 8 blocks of 64: lists 29 us, dK and dV 145 (270 TFLOP/s of the rows' own pairs), their sums 12, delta 19, dQ 213 (the union:
+// three and a half times the blocks of a row).  2 x 4099 of 24 heads of 128 with 8 key heads: dK and dV 323 us (one wavefront a SIMD, bound by the time from a
+// load to its use), dQ 225.
+//
 // dQ is a difference: the rows of dS add up to zero, and what the keys have in common falls out.  An error in delta, or one in
 // dS that does not add up to zero, brings it back.  delta from the rounded O is off by a bfloat16 rounding of O, and a bfloat16 dS by its own:
 // with keys of a common direction dQ was 3.5e-3 off (2-norm; its own rounding makes 1.7e-3).  So the first kernel, which has
 // dS with that delta in fp32, also leaves the sum of each of its rows, which is what delta lacks; a small launch adds them; and
-// the second takes dS as two bfloat16 numbers, high and low: 1.7e-3.
+// the second takes dS as two bfloat16 numbers, high and low: 1.7e-3.  The first takes dS and P so too: rounded once, they put dK 2.4e-3 to 3.0e-3 off
+// and dV 2.4e-3, as two numbers 1.9e-3 and 1.7e-3, for 14 us of 131 (8192 queries of 20 heads of 64; 35 of 288 for 2 x 4099 of 24 of 128).  (What dK still has is delta's error.)
 #include "block_rows.h"
 
 namespace mst {
@@ -54,7 +59,7 @@ struct DkvTiles {
 };
 
 // (128 components take more registers than two wavefronts a SIMD have: so bound, it spills 170 bytes a lane, and 4099 queries of 24 heads
-// with 8 key heads take 368 us, not 281)
+// with 8 key heads take 368 us, not 281, P and dS rounded once)
 template <typename T, int DP, int KP>
 __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 256 ? 1 : 2)) void k_attention_dkv(AttentionArgs a, Lists lists, Heads<const T> q, Heads<const T> k, Heads<const T> v,
                                                                                Heads<const T> d_o, int bg0, int group, BwdArgs w, Heads<T> dk_out, Heads<T> dv_out) {
@@ -197,14 +202,20 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
                         if (kp * 32 + i32 > i4[r]) p[e + r] = ds[e + r] = 0.f;
                 }
             }
-            Operand<T> pf, sf;           // columns = keys, contraction over the rows
+            Operand<T> pf, sf, p_low, s_low;       // columns = keys, contraction over the rows
             set_operand(pf, p);
             set_operand(sf, ds);
+            set_operand_rest(p_low, pf, p);
+            set_operand_rest(s_low, sf, ds);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 if (!worth<T>(d * 32, a.D)) continue;
-                dv[d] = product32(across_rows<T, DP>(ot, rg * 32 + u * 16, d * 32, lane), pf, dv[d]);
-                dk[d] = product32(across_rows<T, DP>(qt, rg * 32 + u * 16, d * 32, lane), sf, dk[d]);
+                const Operand<T> grads = across_rows<T, DP>(ot, rg * 32 + u * 16, d * 32, lane);
+                dv[d] = product32(grads, pf, dv[d]);
+                if (sizeof(T) == 2) dv[d] = product32(grads, p_low, dv[d]);
+                const Operand<T> queries = across_rows<T, DP>(qt, rg * 32 + u * 16, d * 32, lane);
+                dk[d] = product32(queries, sf, dk[d]);
+                if (sizeof(T) == 2) dk[d] = product32(queries, s_low, dk[d]);
             }
             if (LACKS)
 #pragma unroll
@@ -372,7 +383,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : sizeof(T)
                     for (int e = 0; e < 8; ++e) y[e] = exp2_fast(__builtin_fmaf(s[u * 8 + e], scale2, -less)) * (dp[u * 8 + e] - dl);
                     Operand<T> sf, low;
                     set_operand(sf, y);
-                    if (sizeof(T) == 2) set_operand_rest(low, sf, y);
+                    set_operand_rest(low, sf, y);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
                         if (!worth<T>(d * 32, a.D)) continue;

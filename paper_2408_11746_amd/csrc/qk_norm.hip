@@ -4,6 +4,8 @@
 // pairs: the rotation needs no other lane, the mean of the squares is a sum over the group, and each value is read and
 // written once.  A group takes two heads of one token in a row, so that the angles and weights are read once for them and
 // their loads are on the way together.  Bound by memory at ten operations a value; few tokens by latency.
+// Measured: 8 x 1024 tokens of 20 + 20 heads of 64, fp32 to bfloat16, 126 MB, 22 us back to back (some of it from the last level's cache; a copy
+// of 1 GiB runs at 5.1 TB/s, 25 us for as much).
 // The backward needs no more of the forward than x: with r = 1 / sqrt(mean x^2 + eps), dn the gradient rotated back and
 // g = dn weight,  dx = r (g - x r^2 mean(g x)),  dweight = sum over the vectors of dn x r.  A lane meets the same
 // components in all its vectors and keeps their sums in registers; a workgroup adds its lanes and writes one row, and a
