@@ -2,8 +2,8 @@
 
 Bounds are taken element by element from sums of absolute values, before anything is run: a sum of n fp32 products is off by at
 most n 2^-24 of the sum of their sizes (here twice that, for the sum's own order and the exponentials), a value rounded
-to bfloat16 (8 significant bits, half a unit of the last) by 2^-8 of its size, and the kernels round to bfloat16 the weights P and (for dK)
-dS and each output.
+to bfloat16 (8 significant bits, half a unit of the last) by 2^-8 of its size.  A kernel may round to bfloat16 the weights P, (for dK)
+dS and each output; the gradients in fact carry P and dS as two numbers and stay well inside.
 """
 import numpy as np
 import torch
