@@ -36,18 +36,19 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
     const int p = len - a.Tq + t;
     // a positive factor, so that the highest product is the highest score: its sign goes to the query
     const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, 1.17549435e-38f);
+    Cursor cursor(a, rows, tok, there);
+    const bool sees = there && cursor.next < a.nb;             // (the vector of a row that sees nothing may hold anything)
     Operand<T> qf[QC];
     const T* qp = q.at(b, there ? t : 0, there ? h : 0);
 #pragma unroll
     for (int c = 0; c < QC; ++c) {
-        qf[c] = there && c * 16 + half * 8 < a.D ? load_operand(qp + c * 16 + half * 8) : zero_operand<T>();
+        qf[c] = sees && c * 16 + half * 8 < a.D ? load_operand(qp + c * 16 + half * 8) : zero_operand<T>();
         if (a.scale < 0.f) qf[c] = negated(qf[c]);
     }
     floatx16 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zero16();
     float m = -INFINITY, l = 0.f;
-    Cursor cursor(a, rows, tok, there);
     const Tiles tiles_in(a, k, v, b, g, wave, lds);
     const int parts = a.BK / KW, all = n * parts;
     auto entry_of = [&](int i) { return (uint32_t)__builtin_amdgcn_readfirstlane(list[i]); };
@@ -98,6 +99,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
                     for (int r = 0; r < 16; ++r) acc[d][r] *= f;
             }
             const float less = limit < 0 ? INFINITY : m;       // a row that sees nothing here: weights 2^-inf
+            const float before = l;
             Operand<T> pf[2 * ST];
 #pragma unroll
             for (int u = 0; u < 2 * ST; ++u) {
@@ -109,6 +111,13 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
                 }
                 set_operand(pf[u], w);
             }
+            // ... which are 0 but where a product that the row has nothing to do with left fp32: then its sum is no number
+            if (__any(limit < 0 && l != l))
+                if (limit < 0) {
+                    l = before;
+#pragma unroll
+                    for (int u = 0; u < 2 * ST; ++u) pf[u] = zero_operand<T>();
+                }
 #pragma unroll
             for (int d = 0; d < DT; ++d)
                 if (worth<T>(d * 32, a.D))
