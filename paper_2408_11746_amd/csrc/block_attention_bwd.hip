@@ -24,6 +24,9 @@ namespace {
 
 constexpr size_t PARTIAL_BYTES = size_t(256) << 20;
 
+// x y, and 0 if either is 0, whatever the other is (one instruction, as an ordinary product)
+__device__ float product_or_zero(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+
 struct BwdArgs {
     const float* lse;                    // [B][H][Tq]
     const float* delta;                  // [B][H][Tq]
@@ -380,7 +383,10 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : sizeof(T)
                 for (int u = 0; u < 2; ++u) {
                     float y[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = exp2_fast(__builtin_fmaf(s[u * 8 + e], scale2, -less)) * (dp[u * 8 + e] - dl);
+                    for (int e = 0; e < 8; ++e) {          // (0 for what a row does not see, also where s or dp left fp32: the median of no number is 0)
+                        const float weight = __builtin_amdgcn_fmed3f(exp2_fast(__builtin_fmaf(s[u * 8 + e], scale2, -less)), 0.f, 1.f);
+                        y[e] = product_or_zero(weight, dp[u * 8 + e] - dl);
+                    }
                     Operand<T> sf, low;
                     set_operand(sf, y);
                     set_operand_rest(low, sf, y);
@@ -397,13 +403,14 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : sizeof(T)
         if (block_ends) cursor.pass(a, (int)(now & 0xFFFF));
     }
     if (!there) return;
+    const float scale = lse2 == lse2 ? a.scale : lse2;             // (a row whose scores are no numbers: the weights above were cut to 0)
     T* po = dq.at(b, t, h);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int c = d * 32 + 2 * r + 4 * half;
-            if (c < a.D) store4(po + c, acc[d][r] * a.scale, acc[d][r + 1] * a.scale, acc[d][r + 2] * a.scale, acc[d][r + 3] * a.scale);
+            if (c < a.D) store4(po + c, acc[d][r] * scale, acc[d][r + 1] * scale, acc[d][r + 2] * scale, acc[d][r + 3] * scale);
         }
 }
 
