@@ -491,11 +491,11 @@ extern "C" int mst_block_attention_bwd(const mst_attention_shape* s, const mst_h
                                        void* ws, size_t ws_bytes, mst_stream_t stream) {
     using namespace mst;
     if (int e = check_attention(s)) return e;
-    if (s->batch == 0) return MST_OK;                          // (empty buffers may be null)
+    if (s->batch == 0 || (s->queries == 0 && s->keys == 0)) return MST_OK;          // (empty buffers may be null)
     const struct { const mst_heads* v; bool key, written; } views[] = {{q, false, false}, {k, true, false}, {v, true, false}, {o, false, false}, {d_o, false, false}, {dq, false, true}, {dk, true, true}, {dv, true, true}};
     for (const auto& x : views)
         if (int e = x.key ? check_keys(s, x.v, x.written) : check_heads(x.v, s->batch, s->queries, s->heads, s->type, x.written)) return e;
-    if (!plan_dev || (s->queries > 0 && !lse) || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
+    if ((s->queries > 0 && (!plan_dev || !lse)) || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
     const BwdSpace sp = bwd_space(s);
     if (ws_bytes < sp.total) return MST_ERR_WORKSPACE;
     const AttentionArgs a = attention_args(s);

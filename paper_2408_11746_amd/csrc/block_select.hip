@@ -589,13 +589,12 @@ extern "C" int mst_key_summary(const mst_attention_shape* s, const mst_heads* k,
     using namespace mst;
     if (int e = check_attention(s)) return e;
     if (new_tokens < 0) return MST_ERR_ARG;
-    if (s->batch == 0 || s->keys == 0) return MST_OK;          // (empty buffers may be null)
+    // blocks that a sequence's last new_tokens keys can complete
+    const int64_t most = new_tokens == 0 ? 0 : std::min<int64_t>(s->keys / s->block, (int64_t)new_tokens / s->block + 1);
+    if (s->batch == 0 || most == 0) return MST_OK;             // (buffers may be null)
     if (!sums || !scales || !aligned16(sums) || !aligned16(scales)) return MST_ERR_ARG;
     if (int e = check_heads(k, s->batch, s->keys, s->kv_heads, s->type, false)) return e;
     const AttentionArgs a = attention_args(s);
-    // blocks that a sequence's last new_tokens keys can complete
-    const int64_t most = std::min<int64_t>(s->keys / s->block, (int64_t)new_tokens / s->block + 1);
-    if (most == 0 || new_tokens == 0) return MST_OK;
     with_type(s->type, [&](auto t) {
         using T = decltype(t);
         k_key_summary<T><<<dim3((unsigned)most, (unsigned)(a.B * a.G)), SUM_THREADS, 0, static_cast<hipStream_t>(stream)>>>(a, heads_of<const T>(k), sums, scales, new_tokens);
@@ -650,12 +649,11 @@ extern "C" size_t mst_block_plan_bytes(const mst_attention_shape* s) {
 extern "C" int mst_block_plan(const mst_attention_shape* s, const int32_t* blocks, void* plan_dev, size_t plan_bytes, mst_stream_t stream) {
     using namespace mst;
     if (int e = check_attention(s)) return e;
-    if (s->batch == 0) return MST_OK;
-    if ((s->queries > 0 && !blocks) || !plan_dev || !aligned16(blocks) || !aligned16(plan_dev)) return MST_ERR_ARG;
+    if (s->batch == 0 || s->queries == 0) return MST_OK;
+    if (!blocks || !plan_dev || !aligned16(blocks) || !aligned16(plan_dev)) return MST_ERR_ARG;
     const AttentionArgs a = attention_args(s);
     const Plan plan = carve_plan(plan_dev, a);
     if (plan_bytes < plan.total) return MST_ERR_WORKSPACE;
-    if (a.Tq == 0) return MST_OK;
     const size_t lds = (size_t)PLAN_ROWS * (a.NS | 1) * 4;      // 65 KB at most
     static uint64_t allowed = 0;
     if (lds > 64 * 1024)
