@@ -590,8 +590,8 @@ int mst_block_attention_bwd(const mst_attention_shape* shape, const mst_heads* q
                             void* ws_dev, size_t ws_bytes, mst_stream_t stream);
 
 /* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments.  The backward's: 4 bytes a row (query, head) and up to 256 MB of
- * lists and partial sums (more if one key head takes more); the forward, whose sums stay in registers, asks for 256 bytes and keeps nothing in
- * them for the backward. */
+ * lists and partial sums (more if one key head takes more).  The forward's sums stay in registers: it takes NULL and 0 bytes as well, and keeps
+ * nothing in a workspace for the backward (its size is 256 bytes, so that 0 says that the arguments are invalid). */
 size_t mst_block_attention_workspace_bytes(const mst_attention_shape* shape, int backward);
 
 /* The forward for few queries (single tokens over a cache), from blocks_dev itself, without plan or workspace.  The same rules

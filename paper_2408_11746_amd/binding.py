@@ -552,10 +552,10 @@ def mst_block_attention_workspace_bytes(shape: BlockAttentionShape, backward: bo
     return int(lib().mst_block_attention_workspace_bytes(shape._ref, int(backward)))
 
 
-def mst_block_attention_fwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, ws, stream=None):
+def mst_block_attention_fwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, ws=None, stream=None):
     _check("mst_block_attention_fwd",
            lib().mst_block_attention_fwd(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(plan), _heads(o), _ptr(lse), _ptr(ws),
-                                         ws.numel(), _stream(stream)))
+                                         0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def mst_block_attention_bwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, d_o, dq, dk, dv, ws, stream=None):

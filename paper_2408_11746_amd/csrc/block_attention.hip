@@ -290,8 +290,8 @@ extern "C" int mst_block_attention_fwd(const mst_attention_shape* s, const mst_h
     if (int e = check_keys(s, k, false)) return e;
     if (int e = check_keys(s, v, false)) return e;
     if (int e = check_heads(o, s->batch, s->queries, s->heads, s->type, true)) return e;
-    if (!plan_dev || !lse || !ws || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws)) return MST_ERR_ARG;
-    if (ws_bytes < mst_block_attention_workspace_bytes(s, 0)) return MST_ERR_WORKSPACE;
+    if (!plan_dev || !lse || !aligned16(plan_dev) || !aligned16(lse) || !aligned16(ws) || (!ws && ws_bytes > 0)) return MST_ERR_ARG;
+    if (ws && ws_bytes < mst_block_attention_workspace_bytes(s, 0)) return MST_ERR_WORKSPACE;          // (nothing is kept there: none will do)
     const AttentionArgs a = attention_args(s);
     const Plan plan = carve_plan(plan_dev, a);
     hipStream_t st = static_cast<hipStream_t>(stream);
