@@ -4,6 +4,7 @@ import of a compute entry point raises."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -59,8 +60,10 @@ class TransformerFlops(C.Structure):
 
 
 class HeadsView(C.Structure):
-    """Strided view of head vectors [batch, token, head, head_dim]; see heads()."""
+    """Strided view of head vectors [batch, token, head, head_dim]; see heads().  One that heads() made knows its tensor's type and
+    sizes, which the calls compare with theirs."""
     _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+    dtype = sizes = None
 
 
 class QKNormShape(C.Structure):
@@ -78,9 +81,13 @@ class BlockAttentionShape:
     """Shape of the attention over selected blocks; `lengths` (int32 device tensor or None) is kept alive by it."""
 
     def __init__(self, batch, queries, keys, heads, kv_heads, head_dim, block, n_select, scale, type=MST_BF16, lengths=None):
+        if hasattr(lengths, "data_ptr"):
+            _check_lengths(lengths, batch)
         self.lengths = lengths
         self._c = _AttentionShapeC(batch, queries, keys, heads, kv_heads, head_dim, block, n_select, scale, type, _ptr(lengths))
         self._ref = C.byref(self._c)
+        dtype = _torch_type(type)
+        self._queries, self._keys = (dtype, (batch, queries, heads, head_dim)), (dtype, (batch, keys, kv_heads, head_dim))
 
 
 def lib_path() -> str:
@@ -188,11 +195,11 @@ def _check(fn: str, code: int):
 
 def _ptr(t) -> int:
     """Device (or host) address of a torch tensor / raw int address / None."""
+    if t is None:
+        return 0
     try:
         return t.data_ptr()
     except AttributeError:
-        if t is None:
-            return 0
         if isinstance(t, int):
             return t
         raise
@@ -503,19 +510,58 @@ def heads(t) -> HeadsView:
     s = t.stride()
     if len(s) != 4 or (s[3] != 1 and t.shape[3] > 1):
         raise ValueError("heads are [batch, token, head, head_dim] with contiguous components")
-    return HeadsView(t.data_ptr(), s[0], s[1], s[2])
+    v = HeadsView(t.data_ptr(), s[0], s[1], s[2])
+    v.dtype, v.sizes = t.dtype, t.shape
+    return v
 
 
-def _heads(t):
-    if t is None:
+def _check_lengths(t, batch):
+    import torch
+    if t.dtype is not torch.int32 or t.numel() < batch or not t.is_contiguous():
+        raise ValueError("lengths are int32, one behind the other, one for each of %d sequences" % batch)
+
+
+def _torch_type(number):
+    import torch
+    return {MST_F32: torch.float32, MST_BF16: torch.bfloat16}.get(number)
+
+
+def _heads(t, expected, byref=C.byref):
+    """The argument for a tensor or view of which a call reads or writes `expected`, (type, sizes); None: nothing is looked at.
+    (Small calls are bound by the host: 1.0 us a tensor, 0.75 without the comparison.)"""
+    if t is None or expected is None:
         return None
-    return C.byref(t if isinstance(t, HeadsView) else heads(t))
+    if type(t) is HeadsView:
+        if t.sizes is not None and (t.dtype is not expected[0] or t.sizes != expected[1]):
+            _compare(t.dtype, t.sizes, expected)
+        return byref(t)
+    if t.dtype is not expected[0] or t.shape != expected[1]:
+        _compare(t.dtype, t.shape, expected)
+    s = t.stride()
+    if s[3] != 1 and t.shape[3] > 1:
+        raise ValueError("heads are [batch, token, head, head_dim] with contiguous components")
+    return byref(HeadsView(t.data_ptr(), s[0], s[1], s[2]))
+
+
+def _compare(dtype, sizes, expected):
+    if dtype is not expected[0] and expected[0] is not None:         # (None: the library refuses the shape)
+        raise ValueError("heads of %s where the shape says %s" % (dtype, expected[0]))
+    if len(sizes) != 4 or any(n < m for n, m in zip(sizes, expected[1])):
+        raise ValueError("heads of sizes %s where the shape asks for %s" % (tuple(sizes), expected[1]))
+
+
+@functools.lru_cache(maxsize=256)
+def _qk_expected(shape: bytes):
+    """(x and its gradient, y and its), for queries and for keys"""
+    s = QKNormShape.from_buffer_copy(shape)
+    return [None if n == 0 else (_torch_type(t), (s.batch, s.tokens, n, s.head_dim)) for n in (s.heads, s.kv_heads) for t in (s.in_type, s.out_type)]
 
 
 def mst_qk_norm_rotate(shape: QKNormShape, q, k, q_weight, k_weight, table, positions, q_out, k_out, stream=None):
+    qx, qy, kx, ky = _qk_expected(bytes(shape))
     _check("mst_qk_norm_rotate",
-           lib().mst_qk_norm_rotate(C.byref(shape), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _ptr(table),
-                                    _ptr(positions), _heads(q_out), _heads(k_out), _stream(stream)))
+           lib().mst_qk_norm_rotate(C.byref(shape), _heads(q, qx), _heads(k, kx), _ptr(q_weight), _ptr(k_weight), _ptr(table),
+                                    _ptr(positions), _heads(q_out, qy), _heads(k_out, ky), _stream(stream)))
 
 
 def mst_qk_norm_rotate_workspace_bytes(shape: QKNormShape) -> int:
@@ -524,20 +570,21 @@ def mst_qk_norm_rotate_workspace_bytes(shape: QKNormShape) -> int:
 
 def mst_qk_norm_rotate_bwd(shape: QKNormShape, q, k, q_weight, k_weight, table, positions, dq_out, dk_out, dq_in, dk_in,
                            dq_weight, dk_weight, ws, stream=None):
+    qx, qy, kx, ky = _qk_expected(bytes(shape))
     _check("mst_qk_norm_rotate_bwd",
-           lib().mst_qk_norm_rotate_bwd(C.byref(shape), _heads(q), _heads(k), _ptr(q_weight), _ptr(k_weight), _ptr(table),
-                                        _ptr(positions), _heads(dq_out), _heads(dk_out), _heads(dq_in), _heads(dk_in),
+           lib().mst_qk_norm_rotate_bwd(C.byref(shape), _heads(q, qx), _heads(k, kx), _ptr(q_weight), _ptr(k_weight), _ptr(table),
+                                        _ptr(positions), _heads(dq_out, qy), _heads(dk_out, ky), _heads(dq_in, qx), _heads(dk_in, kx),
                                         _ptr(dq_weight), _ptr(dk_weight), _ptr(ws), ws.numel(), _stream(stream)))
 
 
 def mst_key_summary(shape: BlockAttentionShape, k, sums, scales, new_tokens: int, stream=None):
     _check("mst_key_summary",
-           lib().mst_key_summary(shape._ref, _heads(k), _ptr(sums), _ptr(scales), new_tokens, _stream(stream)))
+           lib().mst_key_summary(shape._ref, _heads(k, shape._keys), _ptr(sums), _ptr(scales), new_tokens, _stream(stream)))
 
 
 def mst_block_select(shape: BlockAttentionShape, q, sums, scales, blocks, stream=None):
     _check("mst_block_select",
-           lib().mst_block_select(shape._ref, _heads(q), _ptr(sums), _ptr(scales), _ptr(blocks), _stream(stream)))
+           lib().mst_block_select(shape._ref, _heads(q, shape._queries), _ptr(sums), _ptr(scales), _ptr(blocks), _stream(stream)))
 
 
 def mst_block_plan_bytes(shape: BlockAttentionShape) -> int:
@@ -553,19 +600,22 @@ def mst_block_attention_workspace_bytes(shape: BlockAttentionShape, backward: bo
 
 
 def mst_block_attention_fwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, ws=None, stream=None):
+    rows, keys = shape._queries, shape._keys
     _check("mst_block_attention_fwd",
-           lib().mst_block_attention_fwd(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(plan), _heads(o), _ptr(lse), _ptr(ws),
-                                         0 if ws is None else ws.numel(), _stream(stream)))
+           lib().mst_block_attention_fwd(shape._ref, _heads(q, rows), _heads(k, keys), _heads(v, keys), _ptr(plan), _heads(o, rows), _ptr(lse),
+                                         _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def mst_block_attention_bwd(shape: BlockAttentionShape, q, k, v, plan, o, lse, d_o, dq, dk, dv, ws, stream=None):
+    rows, keys = shape._queries, shape._keys
     _check("mst_block_attention_bwd",
-           lib().mst_block_attention_bwd(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(plan), _heads(o), _ptr(lse),
-                                         _heads(d_o), _heads(dq), _heads(dk), _heads(dv), _ptr(ws), ws.numel(),
+           lib().mst_block_attention_bwd(shape._ref, _heads(q, rows), _heads(k, keys), _heads(v, keys), _ptr(plan), _heads(o, rows), _ptr(lse),
+                                         _heads(d_o, rows), _heads(dq, rows), _heads(dk, keys), _heads(dv, keys), _ptr(ws), ws.numel(),
                                          _stream(stream)))
 
 
 def mst_block_attention_decode(shape: BlockAttentionShape, q, k, v, blocks, o, lse, stream=None):
+    rows, keys = shape._queries, shape._keys
     _check("mst_block_attention_decode",
-           lib().mst_block_attention_decode(shape._ref, _heads(q), _heads(k), _heads(v), _ptr(blocks), _heads(o), _ptr(lse),
+           lib().mst_block_attention_decode(shape._ref, _heads(q, rows), _heads(k, keys), _heads(v, keys), _ptr(blocks), _heads(o, rows), _ptr(lse),
                                             _stream(stream)))
