@@ -1,5 +1,5 @@
-// Which blocks of keys a query reads: 8-bit summaries of the blocks, scores in whole numbers, the best of them, and the plan
-// that turns a selection into lists of queries.
+// Which blocks of keys a query reads: 8-bit summaries of the blocks, scores in whole numbers, the best of them, the plan that keeps
+// the entries of a selection that count, and the lists of a block's queries that the gradients make of a plan.
 //
 // Keys and queries are scaled by powers of two and rounded to 8 bits, summed as whole numbers and rounded to 8 bits again; a
 // score is a sum of at most 128 products below 2^14, exact in 32 bits, times the block's power of two.  Nothing here depends on
@@ -553,9 +553,11 @@ __global__ __launch_bounds__(LIST_TILE) void k_list_fill(AttentionArgs a, Plan p
     }
 }
 
-// Fewer (query, key head) than this: a workgroup for each.  The other kernel walks the summaries one chunk after the other, whatever the number of
-// queries, and leaves most of the card idle until there are many.  (8 key heads, 256 blocks: 64 queries 7.2 us against 19.2; 16 x 12 key heads, 64
-// blocks: 4 queries 6.6 against 7.5, 8 queries 11.1 against 7.5.)
+// Single tokens, and fewer (query, key head) than this: a workgroup for each.  The other kernel walks the summaries one chunk after the other, 64 queries of a
+// key head together, and leaves most of the card idle until there are many.  Kernel times, each query's own workgroup against the other, heads of 128 with four to
+// a key head: single tokens of 128 x 8 key heads, 16, 64, 256 and 1024 blocks: 7, 9, 14 and 37 us against 16, 19, 33 and 94; of 512 x 8: 22, 35, 45 and 151
+// against 49, 58, 105 and 353 (one head of 64 each, 4 selected, 384 x 12, 16 blocks, the closest: 28 against 30).  Two queries of 384 x 12 with such heads: 54 against 31.
+// Eight of 16 x 8 (1024), 16, 64, 256 blocks: 7, 10, 13 against 8, 10, 20; sixteen (2048): 12, 17, 23 against 8, 10, 20.
 constexpr int FEW_QUERIES = 1024;
 
 }  // namespace
@@ -614,7 +616,7 @@ extern "C" int mst_block_select(const mst_attention_shape* s, const mst_heads* q
     with_type(s->type, [&](auto t) {
         using T = decltype(t);
         const Heads<const T> qh = heads_of<const T>(q);
-        if ((int64_t)a.Tq * a.B * a.G < FEW_QUERIES) {
+        if (a.Tq == 1 || (int64_t)a.Tq * a.B * a.G < FEW_QUERIES) {
             k_block_select_few<T><<<dim3((unsigned)a.Tq, (unsigned)(a.B * a.G)), FEW_THREADS, 0, st>>>(a, qh, sums, scales, blocks);
             return;
         }
