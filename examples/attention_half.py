@@ -97,6 +97,8 @@ class Generation:
     """Single tokens after a prompt: a cache of keys, values and summaries that each token extends."""
 
     def __init__(self, half, capacity):
+        if not half.tokens <= capacity <= half.table.shape[0]:          # (positions past the table would take the angles of its last row)
+            raise ValueError("a cache of %d tokens: the prompt has %d, the table of angles %d" % (capacity, half.tokens, half.table.shape[0]))
         self.half, self.capacity = half, capacity
         B, H, G, D, dev = half.batch, half.heads, half.kv_heads, half.dim, half.device
         nb = -(-capacity // half.block)
@@ -115,6 +117,8 @@ class Generation:
     def token(self, x):
         """x [batch, 1, width] -> y; every sequence grows by one"""
         half, at = self.half, int(self.lengths[0])
+        if at == self.capacity:
+            raise ValueError("the cache is full: %d tokens" % at)
         H, G, B = half.heads, half.kv_heads, half.batch
         mst.mst_sparse_fc_fwd(half.qkv, x, self.rows, B)
         here = slice(at, at + 1)
