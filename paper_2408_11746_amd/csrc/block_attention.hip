@@ -48,7 +48,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
     floatx16 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zero16();
-    float m = -INFINITY, l = 0.f;
+    float m = LOWEST, l = 0.f;
     const Tiles tiles_in(a, k, v, b, g, wave, lds);
     const int parts = a.BK / KW, all = n * parts;
     auto entry_of = [&](int i) { return (uint32_t)__builtin_amdgcn_readfirstlane(list[i]); };
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(ROW_THREADS, (sizeof(T) * DP == 512 ? 1 : 2)) void 
             top = apart<32>(top, [](float u, float w) { return fmaxf(u, w); }) * scale2;
             if (limit < 0) top = -INFINITY;
             if (__any(top > m + SLACK)) {
-                const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : exp2_fast(m - to);
+                const float to = fmaxf(m, top), f = exp2_fast(m - to);
                 m = to;
                 l *= f;
 #pragma unroll
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_attention_decode(AttentionArgs a
     float qs[RT][8], acc[RT][8], m[RT], l[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        m[r] = -INFINITY, l[r] = 0.f;
+        m[r] = LOWEST, l[r] = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) qs[r][e] = acc[r][e] = 0.f;
         if (c * 8 < a.D && r0 + r < a.R) load8(q.at(b, t, g * a.R + r0 + r) + c * 8, qs[r]);
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_attention_decode(AttentionArgs a
             auto higher = [](float u, float w) { return fmaxf(u, w); };
             if (LANES <= 8) top = higher(top, __shfl_xor(top, 8));
             top = apart<32>(apart<16>(top, higher), higher);
-            const float to = fmaxf(m[r], top), f = exp2_fast(m[r] - to);     // (key0 is visible: `to` is a number)
+            const float to = fmaxf(m[r], top), f = exp2_fast(m[r] - to);
             m[r] = to;
             l[r] *= f;
 #pragma unroll
@@ -263,10 +263,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_attention_decode(AttentionArgs a
     for (int u = threadIdx.x; u < RT * LANES * 2; u += WAVES * 64) {          // four components of a head to a thread
         const int r = u / (LANES * 2), d = (u - r * (LANES * 2)) * 4;
         if (r0 + r >= a.R || d >= a.D) continue;
-        float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+        float top = LOWEST, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < WAVES; ++w) top = fmaxf(top, part_m[w][r]);
         for (int w = 0; w < WAVES; ++w) {
-            if (part_m[w][r] == -INFINITY) continue;
             const float f = exp2f(part_m[w][r] - top);
             sum += part_l[w][r] * f;
 #pragma unroll

@@ -129,7 +129,8 @@ __global__ __launch_bounds__((DkvTiles<T, DP, KP>::THREADS), (sizeof(T) * DP >= 
     auto stat_of = [&](int2 th, int x) {
         const int t = th.x >> SELECT_BITS;
         const int64_t at = ((int64_t)b * a.H + g * a.R + th.y) * a.Tq + t;
-        return Stat{w.lse[at] * LOG2E, w.delta[at], x * RT + (int)threadIdx.x < rows ? len - a.Tq + t - key0 : -1};
+        const float lse = w.lse[at];                           // (-inf: all scores are; weights 2^-inf)
+        return Stat{lse == -INFINITY ? INFINITY : lse * LOG2E, w.delta[at], x * RT + (int)threadIdx.x < rows ? len - a.Tq + t - key0 : -1};
     };
     auto put_stat = [&](const Stat& s, int x) {
         float* p = stats + (x & 1) * 3 * RT + threadIdx.x;

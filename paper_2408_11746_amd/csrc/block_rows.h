@@ -13,6 +13,9 @@
 namespace mst {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// Running maxima begin at the lowest number, not at -inf: scores that are -inf (products below fp32) then have the weight 2^-inf = 0, also before the first
+// number, and a factor 2^(old - new) is one for an unchanged maximum.
+constexpr float LOWEST = -3.402823466e38f;
 constexpr int ROW_THREADS = 256, ROW_WAVES = ROW_THREADS / 64, COLS = ROW_WAVES * 32;
 
 // Two buffers of KW keys and as many values; a load of a wavefront is 1 KB, and a wavefront moves keys or values alone
