@@ -499,7 +499,8 @@ typedef struct {
  * not 0.  The other components are left as they are. */
 typedef struct {
     int32_t batch, tokens;       /* >= 0 */
-    int32_t heads, kv_heads;     /* query and key heads, >= 0: with 0 that side's arguments are not looked at */
+    int32_t heads, kv_heads;     /* query and key heads, >= 0: with 0 that side's views are not looked at, and its
+                                    weight's gradient is 0 */
     int32_t head_dim;            /* a multiple of 8, 8 .. 256 */
     int32_t rotated;             /* even, 0 .. head_dim */
     int32_t interleaved;
@@ -532,11 +533,13 @@ size_t mst_qk_norm_rotate_workspace_bytes(const mst_qk_shape* shape);
  * at position p = len_b - queries + i and sees the keys 0 .. p: with queries = keys = len_b this is causal
  * training, with queries = 1 the next token over a cache of which `keys` is the capacity, in between a piece of a prompt;
  * len_b < queries is a sequence padded on the left, whose first queries (p < 0) are rows without keys: output 0, log-sum -inf,
- * gradient 0.  Keys and values at or past len_b are never used, whatever they hold.  Keys are cut into blocks of
- * `block`; a query's own block is the one that holds p.  heads / kv_heads query heads share a key head and one
- * selection of blocks.
- * Heads below len_b are finite numbers (a value that is not reaches the results of other queries too: their weight 0 times
- * infinity is no number).
+ * gradient 0, whatever their vectors and the gradients of their outputs hold.  Keys and values at or past len_b are
+ * never used, whatever they hold.  Keys are cut into blocks of `block`; a query's own block is the one that holds p.
+ * heads / kv_heads query heads share a key head and one selection of blocks.
+ * Keys and values below len_b, queries with p >= 0 and the gradients of their outputs are finite numbers: a key or value that
+ * is not reaches the results of other queries too (their weight 0 times infinity is no number), a query or gradient that is
+ * not its own results and the gradients of its blocks' keys.  Where only a product leaves fp32: in a block that a row did
+ * not select, the row's results do not change; a score below fp32 weighs 0, and a row with no others is a row without keys.
  * Refused as MST_ERR_SHAPE beside what the fields say: batch kv_heads > 65535; queries >= 2^25; queries n_select heads / kv_heads >= 2^30;
  * keys or values whose token stride is above 2^22 elements.  With batch 0, and in calls that have nothing to write, buffers may be NULL. */
 typedef struct {
@@ -546,7 +549,9 @@ typedef struct {
     int32_t block;                  /* 32, 64 or 128 */
     int32_t n_select;               /* blocks of a query, 1 .. 64 */
     float scale;                    /* of the products q . k, finite */
-    mst_dtype type;                 /* of q, k, v, o and their gradients; products, statistics and sums are fp32 */
+    mst_dtype type;                 /* of q, k, v, o and their gradients.  Products, statistics and sums are fp32; with MST_BF16 the
+                                       weights are rounded to bfloat16 for their product with v (not in single tokens), the gradients
+                                       take them and dS as two bfloat16 numbers each, and dk has the rounding of the o it is given */
     const int32_t* lengths_dev;     /* [batch] or NULL */
 } mst_attention_shape;
 

@@ -5,10 +5,14 @@
 // rows and values across them.  P is rounded to bfloat16 for that product where the heads are (its sum is not): the weights' error is
 // that of the output's own rounding.
 //
-// Measured: 32768 queries of 32 heads of 128 with 8 key heads, 16 blocks of 128 a query, 2.54 ms: 410 TFLOP/s of what the rows
-// selected; 32 rows visit 28.4 blocks where a row has 15.5, so the matrix instructions do 750, of 1255 that a product of 8192 x 8192 x 8192 does
-// on this card.  Their clocks are 35 % of all, the vector instructions' (exponentials, maxima, roundings) about as many, and a SIMD's two
-// wavefronts overlap the two in part.  8192 queries of 20 heads of 64, 8 blocks of 64: 140 us; there 32 rows visit 27.4 blocks for 7.8.
+// A row that does not see a block of the union has the weight 2^-inf there.  That is 0 but where its product with a block that it has nothing to do with
+// left fp32: those weights show as a sum that is no number, and are cleared.
+//
+// Measured: 32768 queries of 32 heads of 128 with 8 key heads, 16 blocks of 128 a query, 2.45 ms: 425 TFLOP/s of what the rows
+// selected; 32 rows visit 28.4 blocks where a row has 15.5, so the matrix instructions do 780, of 1255 that a product of 8192 x 8192 x 8192 does
+// on this card.  (Among passes that follow each other; the first ten after a pause take 2.4 to 3.1, 2.68 on average, as the clock moves.)  Matrix
+// instructions are busy in 34 % of the clocks, the vector instructions (exponentials, maxima, roundings) in about as many, and a SIMD's two
+// wavefronts overlap the two in part.  8192 queries of 20 heads of 64, 8 blocks of 64: 146 us; there 32 rows visit 27.4 blocks for 7.8.
 #include "block_rows.h"
 
 namespace mst {
@@ -343,8 +347,9 @@ extern "C" int mst_block_attention_decode(const mst_attention_shape* s, const ms
             if (a.D <= 64) launch(std::integral_constant<int, 8>{}, rt, waves);
             else launch(std::integral_constant<int, 16>{}, rt, waves);
         };
-        // As many heads to a workgroup as read the keys once, but one for each CU if there are heads (one sequence, 8 key heads of 4, 16 blocks
-        // of 64: 21.5 us with four heads to a workgroup, 11.7 with one).  Eight wavefronts where workgroups are still too few for the card,
+        // Up to four heads to a workgroup, which then reads the keys once for them (of 8 to 64 heads of a key head, 2 to 16 workgroups read
+        // them; of three, a quarter of the work is for nobody), but one for each CU if there are heads (one sequence, 8 key heads of 4, 16 blocks
+        // of 64: 21.5 us with four heads to a workgroup, 11.7 with one; below 256 (query, head) every head reads the keys for itself).  Eight wavefronts where workgroups are still too few for the card,
         // four where CUs hold several (that sequence 11.7 with eight, 12.6 with four; two key heads of 16, 32 blocks of 128: 31 and 39;
         // 64 sequences of 8 key heads of 4: 63 and 53).
         constexpr int CUS = 256;

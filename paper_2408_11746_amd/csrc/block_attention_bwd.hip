@@ -7,9 +7,11 @@
 // sum.  A block with one item is written as it is; the sums of several items are left in fp32 and added in the order of the list.
 // The second works like the forward: rows that own their dQ walk the union of their blocks.
 //
-// Measured, 8192 queries of 20 heads of 64, 8 blocks of 64: lists 29 us, dK and dV 145 (270 TFLOP/s of the rows' own pairs), their sums 12, delta 19, dQ 213 (the union:
+// Measured, 8192 queries of 20 heads of 64, 8 blocks of 64: lists 30 us, dK and dV 147 (270 TFLOP/s of the rows' own pairs), their sums 12, delta 19, dQ 216 (the union:
 // three and a half times the blocks of a row).  2 x 4099 of 24 heads of 128 with 8 key heads: dK and dV 323 us (one wavefront a SIMD, bound by the time from a
-// load to its use), dQ 225.
+// load to its use; matrix instructions busy in 17 % of the clocks), dQ 218.
+// A row's weights are cut into 0 .. 1 and multiplied so that 0 times anything is 0: what a row does not see has no part in its dQ, also where the scores
+// or dP of that left fp32.
 //
 // dQ is a difference: the rows of dS add up to zero, and what the keys have in common falls out.  An error in delta, or one in
 // dS that does not add up to zero, brings it back.  delta from the rounded O is off by a bfloat16 rounding of O, and a bfloat16 dS by its own:

@@ -155,7 +155,9 @@ __device__ inline floatx16 product32(const Operand<float>& a, const Operand<floa
     return c;
 }
 // components from `d` on are there?  fp32 products take eight instructions, each twice the time of bfloat16's one: they are left out where
-// head_dim ends before the padded width does (80 components: 5 of 8 and 3 of 4).  bfloat16 ones are not worth the branch.
+// head_dim ends before the padded width does (80 components: 5 of 8 and 3 of 4; the scores of dQ's walk still go through all).  bfloat16 ones are
+// not worth the branch: with it forward and gradients of 4096 queries take 504 us against 478 at 80 components, 481 against 442 at 96; of 8192 at 40
+// 560 against 550, at 64 563 against 540, and at 32 alone 484 against 522.
 template <typename T>
 __device__ inline bool worth(int d, int D) { return sizeof(T) == 2 || d == 0 || d < D; }
 __device__ inline floatx16 zero16() {
