@@ -23,6 +23,13 @@
  *   mst_block_attention_fwd, _bwd     attention over the selected blocks and its gradients
  *   mst_block_attention_decode        the same for single tokens over a cache
  *
+ * Around the products, for the rest of a training step:
+ *
+ *   mst_layer_norm_fwd, _bwd          sum of a branch and the residual stream, layer norm of it, and the gradients
+ *   mst_gelu_fwd, _bwd                the activation between fc1 and fc2
+ *   mst_checkpoint_write, _read       activations in 8 bits; the two above write and read them too
+ *   mst_vocab_loss_fwd, _bwd          softmax cross entropy over the vocabulary from hidden states and embedding
+ *
  * Conventions
  *   - Every pointer named *_dev is DEVICE memory, owned by the caller, 16-byte aligned;
  *     everything else is host memory.  The library allocates no device memory: the
@@ -603,6 +610,93 @@ size_t mst_block_attention_workspace_bytes(const mst_attention_shape* shape, int
  * for its entries.  lse_dev may be NULL. */
 int mst_block_attention_decode(const mst_attention_shape* shape, const mst_heads* q, const mst_heads* k, const mst_heads* v,
                                const int32_t* blocks_dev, const mst_heads* o, float* lse_dev, mst_stream_t stream);
+
+/* ------------------------------------------- norm, activation and what is kept of them */
+
+/* Rows are dense [rows x width]; widths need no alignment.  All sums and statistics are fp32, an output is rounded once. */
+
+/* Values kept in 8 bits for the backward pass: codes_dev int8 [rows x width] and units_dev fp32 [rows x ceil(width / 128)], a unit for
+ * each 128 consecutive columns of a row (the last may be fewer).  With top the largest |v| of them,
+ *   unit = max(top fl(1/127), 2^-126),  code = round(v fl(1/unit)),  value = code unit
+ * in fp32, rounding to nearest even: a value is off by at most half a unit, and codes depend on nothing but the group's values.  Values that are
+ * not finite make the whole group come back as NaN. */
+typedef struct {
+    int8_t* codes_dev;
+    float* units_dev;
+} mst_checkpoint8;
+
+/* Any activation of `type` into 8 bits, and back.  rows >= 0, 1 <= width <= 2^24, rows width < 2^40, at
+ * most 2^33 groups. */
+int mst_checkpoint_write(int64_t rows, int32_t width, const void* x_dev, mst_dtype type, const mst_checkpoint8* kept, mst_stream_t stream);
+int mst_checkpoint_read(int64_t rows, int32_t width, const mst_checkpoint8* kept, mst_dtype type, void* x_dev, mst_stream_t stream);
+
+/* s = x + residual, in in_type;  n = (s - mean s) / sqrt(mean (s - mean s)^2 + eps);  y = n weight + bias   (means over a row) */
+typedef struct {
+    int64_t rows;                /* 0 .. 2^31 */
+    int32_t width;               /* 1 .. 16384 */
+    float eps;                   /* >= 0 */
+    mst_dtype in_type, out_type; /* of x, the residual, s and the gradients ds and dx; of y */
+    mst_dtype grad_type;         /* of dy */
+} mst_norm_shape;
+
+/* weight, bias: fp32 [width], or NULL for ones and zeros.  residual NULL: s = x.  sum_dev takes s (NULL: not wanted); it may be x or the
+ * residual.  kept (or NULL) takes s in 8 bits. */
+int mst_layer_norm_fwd(const mst_norm_shape* shape, const void* x_dev, const void* residual_dev, const float* weight_dev,
+                       const float* bias_dev, void* sum_dev, void* y_dev, const mst_checkpoint8* kept, mst_stream_t stream);
+
+/* Gradients from s, or from what was kept of it: exactly one of sum_dev and kept is given (the other NULL), and everything is formed from
+ * its values.  dx = the gradient of y through the norm, plus ds_dev, the gradient that reaches s along the residual stream (NULL: none);
+ * it is the gradient of x and of the residual, and may be ds_dev.  dweight_dev, dbias_dev fp32 [width] (NULL: not wanted).  y_dev takes y again
+ * (NULL: not wanted; bias_dev is used for that alone).  Nothing else has to be kept from the forward call.
+ * Workspace: mst_layer_norm_workspace_bytes, 0 on invalid arguments. */
+int mst_layer_norm_bwd(const mst_norm_shape* shape, const void* sum_dev, const mst_checkpoint8* kept, const float* weight_dev,
+                       const float* bias_dev, const void* dy_dev, const void* ds_dev, void* dx_dev, float* dweight_dev, float* dbias_dev,
+                       void* y_dev, void* ws_dev, size_t ws_bytes, mst_stream_t stream);
+size_t mst_layer_norm_workspace_bytes(const mst_norm_shape* shape);
+
+/* y = x / (1 + exp(-2u)), u = sqrt(2 / pi) (x + 0.044715 x^3), GPT-2's form of x Phi(x); with erf not 0: x Phi(x) itself */
+typedef struct {
+    int64_t rows;                /* >= 0, rows width < 2^40, rows ceil(width / 128) <= 2^33 */
+    int32_t width;               /* 1 .. 2^24 */
+    int32_t erf;
+    mst_dtype in_type, out_type;        /* of x; of y */
+    mst_dtype grad_type, in_grad_type;  /* of dy; of dx */
+} mst_gelu_shape;
+
+/* kept (or NULL) takes x in 8 bits. */
+int mst_gelu_fwd(const mst_gelu_shape* shape, const void* x_dev, void* y_dev, const mst_checkpoint8* kept, mst_stream_t stream);
+
+/* dx from x, or from what was kept of it: exactly one of x_dev and kept is given.  dx_dev may be dy_dev (of one type).  y_dev takes y of
+ * the same values again (NULL: not wanted). */
+int mst_gelu_bwd(const mst_gelu_shape* shape, const void* x_dev, const mst_checkpoint8* kept, const void* dy_dev, void* dx_dev, void* y_dev,
+                 mst_stream_t stream);
+
+/* ------------------------------------------- loss over the vocabulary */
+
+/* z = h E^T of hidden states h [tokens x width] and an embedding E [vocab x width], which is never stored whole:
+ *   lse = log sum_v exp z_v,  loss = lse - z_label
+ * for each token.  labels: int32 [tokens]; a token whose label is outside 0 .. vocab - 1 has none: its loss and lse are 0, the gradient of its
+ * hidden state is 0, and its hidden state is used for nothing, whatever it holds. */
+typedef struct {
+    int32_t tokens;              /* 0 .. 2^24 */
+    int32_t width;               /* a multiple of 8, 8 .. 16384 */
+    int32_t vocab;               /* 1 .. 2^24 */
+    mst_dtype type;              /* of h, E and their gradients.  MST_BF16: products of the numbers as they are, fp32 sums; the gradient of z is rounded
+                                    to bfloat16 for its products.  MST_F32: numbers as three bfloat16 parts each, six products (2^-24 of a term) */
+} mst_vocab_loss_shape;
+
+/* loss_dev, lse_dev fp32 [tokens] (loss_dev may be NULL).  Workspace: mst_vocab_loss_workspace_bytes(shape, 0). */
+int mst_vocab_loss_fwd(const mst_vocab_loss_shape* shape, const void* h_dev, const void* E_dev, const int32_t* labels_dev,
+                       float* loss_dev, float* lse_dev, void* ws_dev, size_t ws_bytes, mst_stream_t stream);
+
+/* Gradients of sum_t dloss_t loss_t: dh [tokens x width], dE [vocab x width] (either may be NULL: not wanted) from lse of the forward call and
+ * dloss_dev fp32 [tokens].  z is formed again, in pieces of the vocabulary.  Workspace: mst_vocab_loss_workspace_bytes(shape, 1). */
+int mst_vocab_loss_bwd(const mst_vocab_loss_shape* shape, const void* h_dev, const void* E_dev, const int32_t* labels_dev,
+                       const float* lse_dev, const float* dloss_dev, void* dh_dev, void* dE_dev, void* ws_dev, size_t ws_bytes,
+                       mst_stream_t stream);
+
+/* Workspace of the forward (backward = 0) or of either call; 0 on invalid arguments. */
+size_t mst_vocab_loss_workspace_bytes(const mst_vocab_loss_shape* shape, int backward);
 
 #ifdef __cplusplus
 }

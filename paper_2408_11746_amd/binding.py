@@ -90,6 +90,34 @@ class BlockAttentionShape:
         self._queries, self._keys = (dtype, (batch, queries, heads, head_dim)), (dtype, (batch, keys, kv_heads, head_dim))
 
 
+class LayerNormShape(C.Structure):
+    """rows, width, eps, in_type, out_type, grad_type"""
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("eps", C.c_float), ("in_type", C.c_int), ("out_type", C.c_int), ("grad_type", C.c_int)]
+
+
+class GeluShape(C.Structure):
+    """rows, width, erf, in_type, out_type, grad_type, in_grad_type"""
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("erf", C.c_int32)] + [(k, C.c_int) for k in ("in_type", "out_type", "grad_type", "in_grad_type")]
+
+
+class VocabLossShape(C.Structure):
+    """tokens, width, vocab, type"""
+    _fields_ = [(k, C.c_int32) for k in ("tokens", "width", "vocab")] + [("type", C.c_int)]
+
+
+class _Checkpoint8C(C.Structure):
+    _fields_ = [("codes_dev", C.c_void_p), ("units_dev", C.c_void_p)]
+
+
+class Checkpoint8:
+    """Values kept in 8 bits: codes int8 [rows, width] and units fp32 [rows, ceil(width / 128)], which it keeps alive."""
+
+    def __init__(self, codes, units):
+        self.codes, self.units = codes, units
+        self._c = _Checkpoint8C(_ptr(codes), _ptr(units))
+        self._ref = C.byref(self._c)
+
+
 def lib_path() -> str:
     return os.path.join(HERE, "libmst_hip.so")
 
@@ -164,6 +192,16 @@ def lib() -> C.CDLL:
         "mst_block_attention_bwd": (i32, [vp] * 12 + [sz, vp]),
         "mst_block_attention_workspace_bytes": (sz, [vp, i32]),
         "mst_block_attention_decode": (i32, [vp] * 8),
+        "mst_checkpoint_write": (i32, [i64, i32, vp, i32, vp, vp]),
+        "mst_checkpoint_read": (i32, [i64, i32, vp, i32, vp, vp]),
+        "mst_layer_norm_fwd": (i32, [vp] * 9),
+        "mst_layer_norm_bwd": (i32, [vp] * 12 + [sz, vp]),
+        "mst_layer_norm_workspace_bytes": (sz, [vp]),
+        "mst_gelu_fwd": (i32, [vp] * 5),
+        "mst_gelu_bwd": (i32, [vp] * 7),
+        "mst_vocab_loss_fwd": (i32, [vp] * 7 + [sz, vp]),
+        "mst_vocab_loss_bwd": (i32, [vp] * 9 + [sz, vp]),
+        "mst_vocab_loss_workspace_bytes": (sz, [vp, i32]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -185,7 +223,9 @@ EXPORTS = ["mst_version", "mst_last_hip_error", "mst_layer_device_bytes", "mst_w
            "mst_strided_attention_mask", "mst_strided_attention_count",
            "mst_qk_norm_rotate", "mst_qk_norm_rotate_bwd", "mst_qk_norm_rotate_workspace_bytes", "mst_key_summary",
            "mst_block_select", "mst_block_plan_bytes", "mst_block_plan", "mst_block_attention_fwd", "mst_block_attention_bwd",
-           "mst_block_attention_workspace_bytes", "mst_block_attention_decode"]
+           "mst_block_attention_workspace_bytes", "mst_block_attention_decode",
+           "mst_checkpoint_write", "mst_checkpoint_read", "mst_layer_norm_fwd", "mst_layer_norm_bwd", "mst_layer_norm_workspace_bytes",
+           "mst_gelu_fwd", "mst_gelu_bwd", "mst_vocab_loss_fwd", "mst_vocab_loss_bwd", "mst_vocab_loss_workspace_bytes"]
 
 
 def _check(fn: str, code: int):
@@ -619,3 +659,120 @@ def mst_block_attention_decode(shape: BlockAttentionShape, q, k, v, blocks, o, l
     _check("mst_block_attention_decode",
            lib().mst_block_attention_decode(shape._ref, _heads(q, rows), _heads(k, keys), _heads(v, keys), _ptr(blocks), _heads(o, rows), _ptr(lse),
                                             _stream(stream)))
+
+
+# ------------------------------------------------------------------ norm, activation, checkpoints, loss
+
+_F32 = _INT8 = _INT32 = _BF16 = _FLOATS = None
+
+
+def _types():
+    global _F32, _INT8, _INT32, _BF16, _FLOATS
+    import torch
+    _INT8, _INT32, _BF16, _F32 = torch.int8, torch.int32, torch.bfloat16, torch.float32
+    _FLOATS = (_F32, _BF16)
+
+
+def _dense(t, dtype, numbers):
+    """Address of a tensor of the type, with so many numbers one behind the other on the device that the call runs on; an address as it is;
+    0 for None.  (`dtype` a number of mst_dtype, or a torch type; one that is unknown is the library's to refuse.)"""
+    if t is None or type(t) is int:
+        return t or 0
+    if _FLOATS is None:
+        _types()
+    want = dtype if not isinstance(dtype, int) else _FLOATS[dtype] if 0 <= dtype < 2 else t.dtype
+    if t.dtype is not want or t.numel() < numbers or not t.is_contiguous():
+        raise ValueError("a tensor of %s, %s%s where the call takes %d numbers of %s, one behind the other"
+                         % (t.dtype, tuple(t.shape), "" if t.is_contiguous() else " with strides %s" % (t.stride(),), numbers, want))
+    if t.get_device() != _device():
+        raise ValueError("a tensor on %s where the call runs on the current GPU" % t.device)
+    return t.data_ptr()
+
+
+def _device() -> int:
+    """the calling thread's current GPU, -2 without one"""
+    import torch
+    if not torch.cuda.is_available():
+        return -2
+    global _device
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    torch.cuda.current_stream()                      # (initialises the device)
+    return _device()
+
+
+def _kept(kept, rows, width):
+    """The argument for a checkpoint of rows x width values"""
+    if kept is None:
+        return None
+    _dense(kept.codes, _INT8 or _type_of("int8"), rows * width)
+    _dense(kept.units, MST_F32, rows * -(-width // 128) if width > 0 else 0)
+    return kept._ref
+
+
+def _type_of(name):
+    _types()
+    import torch
+    return getattr(torch, name)
+
+
+def mst_checkpoint_write(rows: int, width: int, x, type: int, kept: Checkpoint8, stream=None):
+    _check("mst_checkpoint_write",
+           lib().mst_checkpoint_write(rows, width, _dense(x, type, rows * width), type, _kept(kept, rows, width), _stream(stream)))
+
+
+def mst_checkpoint_read(rows: int, width: int, kept: Checkpoint8, type: int, x, stream=None):
+    _check("mst_checkpoint_read",
+           lib().mst_checkpoint_read(rows, width, _kept(kept, rows, width), type, _dense(x, type, rows * width), _stream(stream)))
+
+
+def mst_layer_norm_fwd(shape: LayerNormShape, x, residual, weight, bias, sum, y, kept: Optional[Checkpoint8] = None, stream=None):
+    rows, width, t = shape.rows, shape.width, shape.in_type
+    n = rows * width
+    _check("mst_layer_norm_fwd",
+           lib().mst_layer_norm_fwd(C.byref(shape), _dense(x, t, n), _dense(residual, t, n), _dense(weight, MST_F32, width), _dense(bias, MST_F32, width),
+                                    _dense(sum, t, n), _dense(y, shape.out_type, n), _kept(kept, rows, width), _stream(stream)))
+
+
+def mst_layer_norm_workspace_bytes(shape: LayerNormShape) -> int:
+    return int(lib().mst_layer_norm_workspace_bytes(C.byref(shape)))
+
+
+def mst_layer_norm_bwd(shape: LayerNormShape, sum, kept: Optional[Checkpoint8], weight, bias, dy, ds, dx, dweight, dbias, y, ws, stream=None):
+    rows, width, t = shape.rows, shape.width, shape.in_type
+    n = rows * width
+    _check("mst_layer_norm_bwd",
+           lib().mst_layer_norm_bwd(C.byref(shape), _dense(sum, t, n), _kept(kept, rows, width), _dense(weight, MST_F32, width), _dense(bias, MST_F32, width),
+                                    _dense(dy, shape.grad_type, n), _dense(ds, t, n), _dense(dx, t, n), _dense(dweight, MST_F32, width),
+                                    _dense(dbias, MST_F32, width), _dense(y, shape.out_type, n), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def mst_gelu_fwd(shape: GeluShape, x, y, kept: Optional[Checkpoint8] = None, stream=None):
+    n = shape.rows * shape.width
+    _check("mst_gelu_fwd",
+           lib().mst_gelu_fwd(C.byref(shape), _dense(x, shape.in_type, n), _dense(y, shape.out_type, n), _kept(kept, shape.rows, shape.width), _stream(stream)))
+
+
+def mst_gelu_bwd(shape: GeluShape, x, kept: Optional[Checkpoint8], dy, dx, y=None, stream=None):
+    n = shape.rows * shape.width
+    _check("mst_gelu_bwd",
+           lib().mst_gelu_bwd(C.byref(shape), _dense(x, shape.in_type, n), _kept(kept, shape.rows, shape.width), _dense(dy, shape.grad_type, n),
+                              _dense(dx, shape.in_grad_type, n), _dense(y, shape.out_type, n), _stream(stream)))
+
+
+def mst_vocab_loss_workspace_bytes(shape: VocabLossShape, backward: bool) -> int:
+    return int(lib().mst_vocab_loss_workspace_bytes(C.byref(shape), int(backward)))
+
+
+def mst_vocab_loss_fwd(shape: VocabLossShape, h, E, labels, loss, lse, ws, stream=None):
+    T, W, t = shape.tokens, shape.width, shape.type
+    _check("mst_vocab_loss_fwd",
+           lib().mst_vocab_loss_fwd(C.byref(shape), _dense(h, t, T * W), _dense(E, t, shape.vocab * W), _dense(labels, _INT32 or _type_of("int32"), T),
+                                    _dense(loss, MST_F32, T), _dense(lse, MST_F32, T), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def mst_vocab_loss_bwd(shape: VocabLossShape, h, E, labels, lse, dloss, dh, dE, ws, stream=None):
+    T, W, t = shape.tokens, shape.width, shape.type
+    _check("mst_vocab_loss_bwd",
+           lib().mst_vocab_loss_bwd(C.byref(shape), _dense(h, t, T * W), _dense(E, t, shape.vocab * W), _dense(labels, _INT32 or _type_of("int32"), T),
+                                    _dense(lse, MST_F32, T), _dense(dloss, MST_F32, T), _dense(dh, t, T * W), _dense(dE, t, shape.vocab * W),
+                                    _ptr(ws), ws.numel(), _stream(stream)))

@@ -1,0 +1,65 @@
+// What the loss over the vocabulary keeps in its workspace, and its products (vocab_gemm.hip).
+#pragma once
+
+#include "common.h"
+#include "heads.h"
+
+namespace mst {
+
+constexpr int VT = 256;                  // rows and columns of the largest output tile: workspace arrays are padded to it
+constexpr int VK = 32;                   // contraction indices of a step: operands are padded to it
+constexpr int PLANES_MAX = 3;
+
+// A matrix of bfloat16 numbers, or of numbers that are the sum of three (plane p a stride further on).  Along: a row's numbers are
+// contraction indices; across: a row is one contraction index.  Rows past `rows` read as the last one.
+struct VocabOperand {
+    const uint16_t* p;
+    int64_t plane, ld;
+    int rows;
+};
+
+// One of the products of the loss: C[m][n] = sum_k A B
+struct VocabProduct {
+    VocabOperand a, b;
+    const int* m_count;                  // rows of C (device), or null: m
+    const int* k_count;                  // contraction indices (device), or null: k
+    int m, n, k;                         // as the host knows them (the most there are)
+    int planes;                          // of either operand: 1, or 3 and six products a term
+    int splits;                          // of the contraction, each with its own C (sums)
+};
+
+// ---- what becomes of C
+// statistics of the rows' logits: (max, sum of exp(z - max)) per row and STAT_COLUMNS columns
+constexpr int STAT_COLUMNS = 64;
+struct VocabStats {
+    float2* stats;                       // [STAT_COLUMNS columns][row_stride]
+    int64_t row_stride;
+    int first;                           // number of the first of them
+};
+// the gradient of the logits d (exp(z - lse) - [label]), in planes
+struct VocabLogitGrad {
+    uint16_t* ds;
+    int64_t plane, ld;
+    const float *lse, *d;                // per row, padded to VT: infinity and 0 there
+    const int* label;                    // per row, relative to the first column; the value below goes there
+    const float* at_label;
+    int v0;                              // of column 0 in the vocabulary
+};
+struct VocabSums {                       // fp32, split s at sums + s stride; added to what is there
+    float* sums;
+    int64_t stride, ld;
+    int add;
+};
+struct VocabOut {                        // rows of the result times the unit, in its type
+    void* out;
+    int64_t ld;
+    int f32;
+    const float* unit;
+};
+
+int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s);            // a, b along
+int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s);   // a, b along
+int vocab_sums(const VocabProduct& p, const VocabSums& e, hipStream_t s);              // a along, b across
+int vocab_out(const VocabProduct& p, const VocabOut& e, hipStream_t s);                // a, b across
+
+}  // namespace mst
