@@ -7,7 +7,8 @@
 namespace mst {
 
 constexpr int VT = 256;                  // rows and columns of the largest output tile: workspace arrays are padded to it
-constexpr int VK = 32;                   // contraction indices of a step: operands are padded to it
+constexpr int VK = 32;                   // contraction indices of a step
+constexpr int VPAD = 64;                 // operands are padded to so many
 constexpr int PLANES_MAX = 3;
 
 // A matrix of bfloat16 numbers, or of numbers that are the sum of three (plane p a stride further on).  Along: a row's numbers are
@@ -29,18 +30,19 @@ struct VocabProduct {
 };
 
 // ---- what becomes of C
-// statistics of the rows' logits: (max, sum of exp(z - max)) per row and STAT_COLUMNS columns
+// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and STAT_COLUMNS columns
 constexpr int STAT_COLUMNS = 64;
 struct VocabStats {
     float2* stats;                       // [STAT_COLUMNS columns][row_stride]
     int64_t row_stride;
     int first;                           // number of the first of them
+    const float* at_label;               // logit of a row's label, padded to VT
 };
 // the gradient of the logits d (exp(z - lse) - [label]), in planes
 struct VocabLogitGrad {
     uint16_t* ds;
     int64_t plane, ld;
-    const float *lse, *d;                // per row, padded to VT: infinity and 0 there
+    const float *lse, *d;                // per row, padded to VT: infinite and 0 there
     const int* label;                    // per row, relative to the first column; the value below goes there
     const float* at_label;
     int v0;                              // of column 0 in the vocabulary

@@ -1,7 +1,7 @@
 // Softmax cross entropy over the vocabulary from hidden states and embedding, and its gradients (mst_vocab_loss_fwd, _bwd).
 //
 //   z = h E^T,  lse = log sum_v exp z_v,  loss = lse - z_label;   dz = dloss (exp(z - lse) - [v = label]),  dh = dz E,  dE = dz^T h
-// The logits never reach memory.  The forward reduces each tile of them to a maximum and a sum per row; a second kernel joins those.  The backward
+// The logits never reach memory.  The forward reduces each tile of them to a sum per row; a second kernel joins those.  The backward
 // forms them again, a piece of the vocabulary at a time, such that dz of a piece (bfloat16, PIECE_BYTES at most) is read by both products behind it before the next
 // piece replaces it; dE of a piece is complete, dh is summed in fp32 over the pieces.
 // Tokens without a label take no part: the labelled ones are packed side by side first (in order, so that sums do not depend on chance), which also
@@ -127,20 +127,20 @@ __global__ __launch_bounds__(256) void k_vocab_pack(const T* __restrict__ h, con
     }
 }
 
-// rows of a piece of the embedding in parts, padded with zeros
+// rows of a piece of the embedding in parts, padded with zeros to `ld` columns and to whole steps of rows
 template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_parts(const T* __restrict__ E, int rows, int W, uint16_t* __restrict__ to, int64_t plane, int ld, int planes) {
-    const int64_t quads = (int64_t)rows * (ld / 4);
+__global__ __launch_bounds__(256) void k_vocab_parts(const T* __restrict__ E, int rows, int padded, int W, uint16_t* __restrict__ to, int64_t plane, int ld, int planes) {
+    const int64_t quads = (int64_t)padded * (ld / 4);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < quads; q += (int64_t)gridDim.x * 256) {
         const int64_t r = q / (ld / 4);
         const int c = 4 * (int)(q - r * (ld / 4));
         float x[4];
-        load_columns(E + r * W + c, W - c, x);
+        load_columns(E + r * W + c, r < rows ? W - c : 0, x);
         put_parts(to + r * ld + c, plane, planes, x);
     }
 }
 
-// maxima and sums of a row joined: 64 rows a workgroup, a quarter of the statistics a wavefront
+// sums of a row joined: 64 rows a workgroup, a quarter of the statistics a wavefront
 __global__ __launch_bounds__(256) void k_vocab_join(const float2* __restrict__ stats, int64_t stride, int n, const int* __restrict__ count, const int* __restrict__ list,
                                                     const float* __restrict__ at_label, float* __restrict__ loss, float* __restrict__ lse) {
     __shared__ float2 part[4][64];
@@ -148,8 +148,8 @@ __global__ __launch_bounds__(256) void k_vocab_join(const float2* __restrict__ s
     if ((int)blockIdx.x * 64 >= rows) return;
     float top = -INFINITY, sum = 0.f;
     auto add = [&](float2 x) __attribute__((always_inline)) {
-        const float m = fmaxf(top, x.x), base = m == -INFINITY ? 0.f : m;
-        sum = sum * expf(top - base) + x.y * expf(x.x - base);
+        const float m = fmaxf(top, x.x), from = m == -INFINITY ? 0.f : m;
+        sum = sum * exp2_fast(top - from) + x.y * exp2_fast(x.x - from);
         top = m;
     };
 #pragma unroll 8
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void k_vocab_join(const float2* __restrict__ s
     __syncthreads();
     if (wave || row >= rows) return;
     for (int w = 1; w < 4; ++w) add(part[w][lane]);
-    const float l = top + logf(sum);
+    const float l = (top + log2f(sum)) * 0.69314718f;
     const int token = list[row];
     lse[token] = l;
     if (loss) loss[token] = l - at_label[row];
@@ -202,7 +202,7 @@ struct Plan {
 
     Plan(const mst_vocab_loss_shape& s, bool backward) {
         planes = s.type == MST_F32 ? PLANES_MAX : 1;
-        wide = (int)align_up(s.width, VK);
+        wide = (int)align_up(s.width, VPAD);
         rows = (int64_t)align_up(s.tokens, VT);
         split_E = planes > 1 || wide != s.width;
         const int64_t column = 2 * planes * ((backward ? rows : 0) + (split_E ? wide : 0)), whole = (int64_t)align_up(s.vocab, VT);
@@ -260,10 +260,11 @@ struct Run {
             o = {reinterpret_cast<const uint16_t*>(from), 0, s.width, n};
             return MST_OK;
         }
-        const int64_t quads = (int64_t)n * (plan.wide / 4), plane = (int64_t)plan.piece * plan.wide;
-        k_vocab_parts<T><<<(unsigned)std::min<int64_t>(cdiv(quads, 256), 4096), 256, 0, stream>>>(from, n, s.width, at<uint16_t>(plan.E), plane, plan.wide, plan.planes);
+        const int padded = (int)align_up(n, VPAD);
+        const int64_t quads = (int64_t)padded * (plan.wide / 4), plane = (int64_t)plan.piece * plan.wide;
+        k_vocab_parts<T><<<(unsigned)std::min<int64_t>(cdiv(quads, 256), 4096), 256, 0, stream>>>(from, n, padded, s.width, at<uint16_t>(plan.E), plane, plan.wide, plan.planes);
         MST_LAUNCH_CHECK();
-        o = {at<uint16_t>(plan.E), plane, plan.wide, n};
+        o = {at<uint16_t>(plan.E), plane, plan.wide, padded};
         return MST_OK;
     }
     VocabOperand packed() const { return {at<uint16_t>(plan.h), plan.rows * plan.wide, plan.wide, (int)plan.rows}; }
@@ -274,7 +275,7 @@ struct Run {
             VocabOperand e;
             if (int rc = embedding(i, e)) return rc;
             const VocabProduct p = {packed(), e, at<int>(plan.count), nullptr, s.tokens, columns(i), plan.wide, plan.planes, 1};
-            if (int rc = vocab_stats(p, {at<float2>(plan.stat), plan.rows, i * (plan.piece / STAT_COLUMNS)}, stream)) return rc;
+            if (int rc = vocab_stats(p, {at<float2>(plan.stat), plan.rows, i * (plan.piece / STAT_COLUMNS), at<float>(plan.at_label)}, stream)) return rc;
         }
         k_vocab_join<<<(unsigned)cdiv(s.tokens, 64), 256, 0, stream>>>(at<float2>(plan.stat), plan.rows, plan.stats, at<int>(plan.count), at<int>(plan.list),
                                                                       at<float>(plan.at_label), loss, lse);
