@@ -106,21 +106,30 @@ __device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& 
 template <int I, int J, bool ENDS>
 __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
     const int last = p.n - n0 - 4 * (lane >> 4);
-    float base[I], d[I];
+    float base[I], d[I], at_label[I];
+    int label[I];
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         const int m = m0 + 16 * i + (lane & 15);
         base[i] = e.lse[m] * LOG2E;
         d[i] = e.d[m];
+        at_label[i] = e.at_label[m];
+        label[i] = e.label[m] - e.v0 - n0;
     }
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         uint16_t* const row = e.ds + (int64_t)(m0 + 16 * i + (lane & 15)) * e.ld + n0 + 4 * (lane >> 4);
+        const bool some = __any(label[i] >= 0 && label[i] < 16 * J);       // of these sixteen rows has its label among these columns (one in 25)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             float x[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) x[v] = !ENDS || 16 * j + v < last ? d[i] * exp2_fast(fmaf(acc[i][j][v], LOG2E, -base[i])) : 0.f;
+            if (some) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (16 * j + 4 * (lane >> 4) + v == label[i]) x[v] = at_label[i];
+            }
             uint16_t* to = row + 16 * j;
             for (int part = 0;;) {
                 const uint32_t a = pack2(x[0], x[1]), b = pack2(x[2], x[3]);
@@ -132,19 +141,6 @@ __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabP
                 x[2] -= __uint_as_float(b << 16);
                 x[3] -= __uint_as_float(b & 0xFFFF0000u);
             }
-        }
-    }
-    // a label's place, if it is among these columns, behind the stores above
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int r = lane; r < 16 * I; r += 64) {
-        const int m = m0 + r, col = e.label[m] - e.v0 - n0;
-        if (col < 0 || col >= 16 * J) continue;
-        float x = e.at_label[m];
-        for (int part = 0; part < p.planes; ++part) {
-            const uint32_t bits = pack2(x, 0.f);
-            e.ds[part * e.plane + (int64_t)m * e.ld + n0 + col] = (uint16_t)bits;
-            x -= __uint_as_float(bits << 16);
         }
     }
 }
@@ -169,18 +165,27 @@ __device__ __forceinline__ void leave_f32(floatx4 (&acc)[I][J], char* room, int 
         room_done();
     }
 }
+// Sums lie as the wavefronts hold them, a wavefront's 16 x 16 results in 1 KB after another (sum_place): the next piece begins with them.
 template <int I, int J>
-__device__ __forceinline__ void finish(const VocabSums& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane, int m_rows, char* room) {
-    float* const sums = e.sums + split * e.stride;
-    leave_f32(acc, room, lane, [&](int r, int c, float4 x) __attribute__((always_inline)) {
-        if (m0 + r >= m_rows || n0 + c >= p.n) return;              // (p.n a multiple of eight)
-        float4* const to = reinterpret_cast<float4*>(sums + (int64_t)(m0 + r) * e.ld + n0 + c);
-        if (e.add) {
-            const float4 o = *to;
-            x = make_float4(x.x + o.x, x.y + o.y, x.z + o.z, x.w + o.w);
-        }
-        *to = x;
-    });
+__device__ __forceinline__ float4* sums_of(const VocabSums& e, int m0, int n0, int split, int lane) {
+    return reinterpret_cast<float4*>(e.sums + split * e.stride) + sum_place(m0, n0, e.wide) + lane;
+}
+template <int I, int J>
+__device__ __forceinline__ void begin(const VocabSums& e, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane) {
+    if (!e.add) return;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[i][j] = *reinterpret_cast<const floatx4*>(sums_of<I, J>(e, m0 + 16 * i, n0 + 16 * j, split, lane));
+}
+template <int I, int J, typename Args>
+__device__ __forceinline__ void begin(const Args&, floatx4 (&)[I][J], int, int, int, int) {}
+template <int I, int J>
+__device__ __forceinline__ void finish(const VocabSums& e, const VocabProduct&, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane, int, char*) {
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) *reinterpret_cast<floatx4*>(sums_of<I, J>(e, m0 + 16 * i, n0 + 16 * j, split, lane)) = acc[i][j];
 }
 template <int I, int J>
 __device__ __forceinline__ void finish(const VocabOutOf<float>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int m_rows, char* room) {
@@ -253,6 +258,7 @@ __global__ __launch_bounds__(256) void k_vocab_small(const VocabProduct p, const
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    begin(e, acc, m0 + wm, n0 + wn, split, lane);
     for (int term = p.planes == 1 ? 5 : 0; term < 6; ++term)
         for (int t = kb; t < ke; ++t) {
             __syncthreads();
@@ -382,6 +388,7 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    begin(e, acc, m0 + wm, n0 + wn, split, lane);
     bf16x8 a[2][8], b[2][8];
     // products from register set SET; half 1 - SET of the stages sa, sb goes to the other set, a stage's loads to `to`
     auto step = [&](auto set, uint32_t sa, uint32_t sb, uint32_t to) __attribute__((always_inline)) {
@@ -455,9 +462,11 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     finish(e, p, acc, m0 + wm, n0 + wn, split, lane, m_rows, lds + 32768 * wave);
 }
 
+bool small(int m) { return m <= 128; }
+
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipStream_t s) {
-    if (p.m <= 128) {
+    if (small(E == SUMS || E == STATS || E == LOGIT_GRAD ? p.m : p.k)) {
         const int64_t blocks = cdiv(p.m, SM) * cdiv(p.n, SM) * p.splits;
         k_vocab_small<A_ALONG, B_ALONG, E><<<(unsigned)blocks, 256, 0, s>>>(p, e);
     } else {
@@ -471,6 +480,19 @@ int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipSt
 }
 
 }  // namespace
+
+// As many ranges as let the products end first: rounds of 256 workgroups, each as long as its range and what begins and ends it (the time of some eight
+// pairs of steps, the sums of the pieces before and behind among it).
+int vocab_splits(int m, int n, int k) {
+    const int64_t side = small(m) ? SM : VT, tiles = cdiv(m, side) * cdiv(n, side), pairs = cdiv(k, L_PAIR);
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= 64 && s <= pairs; ++s) {
+        const int64_t time = cdiv(tiles * s, 256) * (cdiv(pairs, s) + 8);
+        if (time < least) least = time, best = s;
+    }
+    return best;
+}
 
 int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s) { return launch<true, true, STATS>(p, e, s); }
 int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s) { return launch<true, true, LOGIT_GRAD>(p, e, s); }

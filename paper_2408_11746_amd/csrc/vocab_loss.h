@@ -47,11 +47,15 @@ struct VocabLogitGrad {
     const float* at_label;
     int v0;                              // of column 0 in the vocabulary
 };
-struct VocabSums {                       // fp32, split s at sums + s stride; added to what is there
+// fp32 sums, split s at sums + s stride; with add, added to what is there.  In blocks of 16 x 16 one after another along n, then m, padded to whole tiles: number
+// 4 g + v of row r of a block is component v of its word (four numbers) 16 g + r.
+struct VocabSums {
     float* sums;
-    int64_t stride, ld;
+    int64_t stride;
+    int wide;                            // blocks along n
     int add;
 };
+__device__ inline int64_t sum_place(int m, int n, int wide) { return ((int64_t)(m >> 4) * wide + (n >> 4)) * 64; }      // word of the block that holds m, n
 struct VocabOut {                        // rows of the result times the unit, in its type
     void* out;
     int64_t ld;
@@ -59,6 +63,7 @@ struct VocabOut {                        // rows of the result times the unit, i
     const float* unit;
 };
 
+int vocab_splits(int m, int n, int k);   // ranges of the contraction for vocab_sums
 int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s);            // a, b along
 int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s);   // a, b along
 int vocab_sums(const VocabProduct& p, const VocabSums& e, hipStream_t s);              // a along, b across

@@ -15,7 +15,6 @@ namespace mst {
 namespace {
 
 constexpr int64_t PIECE_BYTES = int64_t(1) << 28;
-constexpr int SPLITS_MAX = 64;
 
 // ---- which tokens have a label
 constexpr int ROWS_THREADS = 1024, ROWS_EACH = 16;
@@ -164,23 +163,32 @@ __global__ __launch_bounds__(256) void k_vocab_join(const float2* __restrict__ s
     if (loss) loss[token] = l - at_label[row];
 }
 
-// gradients of the hidden states: sums of the splits, back to the tokens' places
+// gradients of the hidden states: sums of the splits, back to the tokens' places; a wavefront takes blocks of 16 rows and 16 columns
 template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_dh(const float* __restrict__ sums, int64_t stride, int splits, const int* __restrict__ place, const float* __restrict__ unit, int tokens,
-                                                  int W, T* __restrict__ dh) {
-    const int64_t quads = (int64_t)tokens * (W / 4);
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < quads; q += (int64_t)gridDim.x * 256) {
-        const int64_t token = q / (W / 4);
-        const int c = 4 * (int)(q - token * (W / 4)), row = place[token];
+__global__ __launch_bounds__(256) void k_vocab_dh(const float* __restrict__ sums, int64_t stride, int wide, int splits, const int* __restrict__ count, const int* __restrict__ list,
+                                                  const float* __restrict__ unit, int W, T* __restrict__ dh) {
+    const int rows = *count, lane = threadIdx.x & 63, row = blockIdx.x * 16 + (lane & 15);
+    if ((int)blockIdx.x * 16 >= rows) return;
+    const float u = *unit;
+    const int64_t token = row < rows ? list[row] : 0;
+    for (int c = 16 * (blockIdx.y * 4 + (threadIdx.x >> 6)); c < W; c += 64 * gridDim.y) {
+        const float* const from = sums + 4 * (sum_place(row, c, wide) + lane);
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (row >= 0)
-            for (int s = 0; s < splits; ++s) {
-                const float4 y = *reinterpret_cast<const float4*>(sums + s * stride + (int64_t)row * W + c);
-                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-            }
-        const float u = *unit;
-        store4(dh + token * W + c, u * x.x, u * x.y, u * x.z, u * x.w);
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4 y = *reinterpret_cast<const float4*>(from + s * stride);
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        }
+        const int col = c + 4 * (lane >> 4);
+        if (row < rows && col < W) store4(dh + token * W + col, u * x.x, u * x.y, u * x.z, u * x.w);
     }
+}
+// ... and those of the tokens without a label: 0; a wavefront a token
+template <typename T>
+__global__ __launch_bounds__(256) void k_vocab_dh_others(const int* __restrict__ place, int tokens, int W, T* __restrict__ dh) {
+    const int token = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (token >= tokens || place[token] >= 0) return;
+    for (int c = 4 * (threadIdx.x & 63); c < W; c += 256) store4(dh + (int64_t)token * W + c, 0.f, 0.f, 0.f, 0.f);
 }
 
 int check_shape(const mst_vocab_loss_shape* s) {
@@ -196,10 +204,11 @@ struct Plan {
     int64_t rows;                        // of packed arrays
     bool split_E;                        // the products read the embedding from its parts
     int piece, pieces;                   // columns of the vocabulary, and how often
-    int splits;                          // of the sums for dh
+    int splits, sum_blocks;              // of the sums for dh; blocks along a row
     int stats;
     size_t count, unit, place, list, label, at_label, lse, d, h, E, stat, ds, sums, bytes;
 
+    int64_t sum_stride() const { return rows * sum_blocks * 16; }
     Plan(const mst_vocab_loss_shape& s, bool backward) {
         planes = s.type == MST_F32 ? PLANES_MAX : 1;
         wide = (int)align_up(s.width, VPAD);
@@ -211,8 +220,8 @@ struct Plan {
         piece = (int)align_up(cdiv(s.vocab, pieces), VT);
         pieces = (int)cdiv(s.vocab, piece);
         stats = (int)cdiv(s.vocab, STAT_COLUMNS);
-        const int64_t tiles = cdiv(rows, VT) * cdiv(s.width, VT);
-        splits = (int)std::max<int64_t>(1, std::min({cdiv(512, std::max<int64_t>(tiles, 1)), int64_t(SPLITS_MAX), int64_t(piece / 256)}));
+        sum_blocks = (int)align_up(s.width, VT) / 16;
+        splits = vocab_splits(s.tokens, s.width, piece);
         bytes = 0;
         auto part = [&](size_t n) { const size_t at = bytes; bytes += align_up(n); return at; };
         count = part(4);
@@ -227,7 +236,7 @@ struct Plan {
         E = part(split_E ? 2 * planes * (size_t)piece * wide : 0);
         stat = part(backward ? 0 : 8 * (size_t)rows * stats);
         ds = part(backward ? 2 * planes * (size_t)rows * piece : 0);
-        sums = part(backward ? 4 * (size_t)splits * rows * s.width : 0);
+        sums = part(backward ? 4 * (size_t)splits * sum_stride() : 0);
     }
 };
 
@@ -296,7 +305,7 @@ struct Run {
                                              i * plan.piece}, stream)) return rc;
             if (dh) {
                 const VocabProduct p = {ds_rows, e, at<int>(plan.count), nullptr, s.tokens, s.width, n, plan.planes, plan.splits};
-                if (int rc = vocab_sums(p, {at<float>(plan.sums), plan.rows * s.width, s.width, i > 0}, stream)) return rc;
+                if (int rc = vocab_sums(p, {at<float>(plan.sums), plan.sum_stride(), plan.sum_blocks, i > 0}, stream)) return rc;
             }
             if (dE) {
                 const VocabProduct p = {ds_rows, packed(), nullptr, at<int>(plan.count), n, s.width, s.tokens, plan.planes, 1};
@@ -304,9 +313,10 @@ struct Run {
             }
         }
         if (dh) {
-            const int64_t quads = (int64_t)s.tokens * (s.width / 4);
-            k_vocab_dh<T><<<(unsigned)std::min<int64_t>(cdiv(quads, 256), 8192), 256, 0, stream>>>(at<float>(plan.sums), plan.rows * s.width, plan.splits, at<int>(plan.place), at<float>(plan.unit),
-                                                                                                  s.tokens, s.width, dh);
+            k_vocab_dh<T><<<dim3((unsigned)cdiv(s.tokens, 16), (unsigned)cdiv(s.width, 256)), 256, 0, stream>>>(
+                at<float>(plan.sums), plan.sum_stride(), plan.sum_blocks, plan.splits, at<int>(plan.count), at<int>(plan.list), at<float>(plan.unit), s.width, dh);
+            MST_LAUNCH_CHECK();
+            k_vocab_dh_others<T><<<(unsigned)cdiv(s.tokens, 4), 256, 0, stream>>>(at<int>(plan.place), s.tokens, s.width, dh);
             MST_LAUNCH_CHECK();
         }
         return MST_OK;
