@@ -30,69 +30,75 @@ __device__ __forceinline__ uint32_t along_unit(int m, int u) {
 __device__ __forceinline__ int across_swizzle(int k) { return (k & 3) | ((k >> 1) & 4); }
 
 // ---- 128 x 128 tiles, four wavefronts of 64 x 64
-constexpr int SM = 128, S_OP = SM * 64, S_ROOM = 64 * 128;      // (64 rows of 128 bytes)
+constexpr int SM = 128, S_OP = SM * 64;
 
-enum Epilogue { STATS, LOGIT_GRAD, SUMS, OUT_F32, OUT_BF16 };
+enum Epilogue { STATS, LOGIT_GRAD, LOGIT_GRAD_PARTS, SUMS, OUT_F32, OUT_BF16 };
 template <Epilogue E> struct EpilogueArgs;
 template <> struct EpilogueArgs<STATS> { using type = VocabStats; };
-template <> struct EpilogueArgs<LOGIT_GRAD> { using type = VocabLogitGrad; };
+template <int PLANES> struct VocabLogitGradOf : VocabLogitGrad {};
+template <> struct EpilogueArgs<LOGIT_GRAD> { using type = VocabLogitGradOf<1>; };
+template <> struct EpilogueArgs<LOGIT_GRAD_PARTS> { using type = VocabLogitGradOf<PLANES_MAX>; };
 template <> struct EpilogueArgs<SUMS> { using type = VocabSums; };
 template <typename T> struct VocabOutOf : VocabOut {};
 template <> struct EpilogueArgs<OUT_F32> { using type = VocabOutOf<float>; };
 template <> struct EpilogueArgs<OUT_BF16> { using type = VocabOutOf<bf16>; };
 
 // Results: acc[i][j][v] is row m0 + 16 i + lane % 16, column n0 + 16 j + 4 (lane / 16) + v of C; a wavefront's 16 I rows and 16 J columns.
-// A lane's four columns are 8 or 16 bytes of a row; dh and dE go through `room` (the wavefront's own LDS, 16 I rows of ROW bytes) on their way to memory and leave
-// it in whole lines.  Word u of row r is kept at u ^ r (of as many as a row has).
-template <int ROW>
-__device__ __forceinline__ uint32_t room_at(int r, int byte) { return (uint32_t)(r * ROW + ((((byte >> 4) ^ r) & (ROW / 16 - 1)) << 4 | (byte & 15))); }
-__device__ __forceinline__ void room_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-// f(row, first byte, its word) for the rows r0 .. r0 + ROWS - 1
-template <int ROWS, int ROW, typename F>
-__device__ __forceinline__ void leave(const char* room, int lane, F&& f) {
-    constexpr int EACH = 1024 / ROW;                                // rows of a store
-#pragma unroll 8
-    for (int r = 0; r < ROWS; r += EACH) {
-        const int row = r + lane / (ROW / 16), byte = lane % (ROW / 16) * 16;
-        f(row, byte, *reinterpret_cast<const uint4*>(room + room_at<ROW>(row, byte)));
-    }
+// Results go straight to memory: a store writes 32 or 64 bytes of sixteen rows, and those that fill a line follow one another.  (Through LDS, in whole lines, they
+// waited longer than they saved.)
+// Result v of a 16 x 16 product.  The large tiles' lie in accumulation registers and are read out where they are used (left to the compiler, most of them are read at
+// once, and other registers spill).
+template <bool LARGE>
+__device__ __forceinline__ float result(const floatx4& acc, int v) {
+    if constexpr (!LARGE) return acc[v];
+    float x;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[v]));
+    return x;
 }
 
 // Sums of exp2(z log2 e - base) over 64 columns, those below p.n.  Base is the logit of the row's own label: the sum over all columns is then 1 at least,
 // what is lost below fp32 does not count in it, and no maximum has to be found first (a fifth of the instructions).  A sum that leaves fp32 is formed again
 // from the row's maximum here.
-template <int I, int J, bool ENDS>
-__device__ __forceinline__ void statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int c, int m0, int n0, int lane) {
+template <int I, int J, bool ENDS, bool MAXIMUM>
+__device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int c, int m0, int n0, int lane) {
     const int last = p.n - n0 - 4 * (lane >> 4);
     auto larger = [](float a, float b) { return fmaxf(a, b); };
     auto plus = [](float a, float b) { return a + b; };
+    float2* const to = e.stats + (int64_t)(e.first + n0 / STAT_COLUMNS + c / 4) * e.row_stride + m0 + (lane & 15);
     float base[I];
 #pragma unroll
-    for (int i = 0; i < I; ++i) base[i] = e.at_label[m0 + 16 * i + (lane & 15)] * LOG2E;
+    for (int i = 0; i < I; ++i) base[i] = MAXIMUM ? 0.f : e.at_label[m0 + 16 * i + (lane & 15)] * LOG2E;
+    bool fits = true;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-        auto z = [&](int j, int v) __attribute__((always_inline)) { return !ENDS || 16 * j + v < last ? acc[i][j][v] : -INFINITY; };
-        auto sum_from = [&](float from) __attribute__((always_inline)) {
-            float sum = 0.f;
-#pragma unroll
-            for (int j = c; j < c + 4; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(z(j, v), LOG2E, -from));
-            return apart<32>(apart<16>(sum, plus), plus);
+        auto z = [&](int j, int v) __attribute__((always_inline)) {
+            const float x = result<I == 8>(acc[i][j], v);
+            return !ENDS || 16 * j + v < last ? x : -INFINITY;
         };
-        float from = base[i], sum = sum_from(from);
-        if (__any(!(sum < INFINITY))) {
+        if constexpr (MAXIMUM) {
             float top = z(c, 0);
 #pragma unroll
             for (int j = c; j < c + 4; ++j) top = fmaxf(fmaxf(fmaxf(top, z(j, 0)), fmaxf(z(j, 1), z(j, 2))), z(j, 3));
-            from = apart<32>(apart<16>(top, larger), larger) * LOG2E;
-            sum = sum_from(from);
+            base[i] = apart<32>(apart<16>(top, larger), larger) * LOG2E;
         }
-        if (lane < 16) e.stats[(int64_t)(e.first + n0 / STAT_COLUMNS + c / 4) * e.row_stride + m0 + 16 * i + lane] = make_float2(from, sum);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = c; j < c + 4; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(z(j, v), LOG2E, -base[i]));
+        sum = apart<32>(apart<16>(sum, plus), plus);
+        fits &= sum < INFINITY;
+        if (lane < 16) to[16 * i] = make_float2(base[i], sum);
+        __builtin_amdgcn_sched_barrier(0);                          // (with the results of several rows out of the accumulation registers it spills)
     }
+    return fits;
+}
+template <int I, int J, bool ENDS>
+__device__ __forceinline__ void statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int c, int m0, int n0, int lane) {
+    if (__any(!statistics<I, J, ENDS, false>(e, p, acc, c, m0, n0, lane))) statistics<I, J, ENDS, true>(e, p, acc, c, m0, n0, lane);
 }
 template <int I, int J>
-__device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int, char*) {
+__device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int) {
 #pragma unroll
     for (int c = 0; c < J; c += 4) {
         const int first = n0 + 16 * c;
@@ -101,11 +107,10 @@ __device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& 
     }
 }
 
-// dz, straight to memory: a store writes 32 bytes of sixteen rows, and the four that fill a line follow one another.  (Through LDS, in whole lines, it
-// waited longer than it saved.)
-template <int I, int J, bool ENDS>
+// dz
+template <int I, int J, int PLANES, bool ENDS>
 __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
-    const int last = p.n - n0 - 4 * (lane >> 4);
+    const int g = lane >> 4, last = p.n - n0 - 4 * g;
     float base[I], d[I], at_label[I];
     int label[I];
 #pragma unroll
@@ -118,53 +123,40 @@ __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabP
     }
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-        uint16_t* const row = e.ds + (int64_t)(m0 + 16 * i + (lane & 15)) * e.ld + n0 + 4 * (lane >> 4);
-        const bool some = __any(label[i] >= 0 && label[i] < 16 * J);       // of these sixteen rows has its label among these columns (one in 25)
+        uint16_t* const row = e.ds + (int64_t)(m0 + 16 * i + (lane & 15)) * e.ld + n0 + 4 * g;
+        auto put = [&](auto labels) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            float x[4];
+            for (int j = 0; j < J; ++j) {
+                float x[4];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) x[v] = !ENDS || 16 * j + v < last ? d[i] * exp2_fast(fmaf(acc[i][j][v], LOG2E, -base[i])) : 0.f;
-            if (some) {
+                for (int v = 0; v < 4; ++v) {
+                    x[v] = d[i] * exp2_fast(fmaf(result<I == 8>(acc[i][j], v), LOG2E, -base[i]));
+                    if (ENDS) x[v] = 16 * j + v < last ? x[v] : 0.f;
+                    if (decltype(labels)::value && 16 * j + 4 * g + v == label[i]) x[v] = at_label[i];
+                }
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (16 * j + 4 * (lane >> 4) + v == label[i]) x[v] = at_label[i];
+                for (int part = 0; part < PLANES; ++part) {
+                    const uint32_t a = pack2(x[0], x[1]), b = pack2(x[2], x[3]);
+                    *reinterpret_cast<uint2*>(row + part * e.plane + 16 * j) = make_uint2(a, b);
+                    x[0] -= __uint_as_float(a << 16);
+                    x[1] -= __uint_as_float(a & 0xFFFF0000u);
+                    x[2] -= __uint_as_float(b << 16);
+                    x[3] -= __uint_as_float(b & 0xFFFF0000u);
+                }
             }
-            uint16_t* to = row + 16 * j;
-            for (int part = 0;;) {
-                const uint32_t a = pack2(x[0], x[1]), b = pack2(x[2], x[3]);
-                *reinterpret_cast<uint2*>(to) = make_uint2(a, b);
-                if (++part == p.planes) break;
-                to += e.plane;
-                x[0] -= __uint_as_float(a << 16);
-                x[1] -= __uint_as_float(a & 0xFFFF0000u);
-                x[2] -= __uint_as_float(b << 16);
-                x[3] -= __uint_as_float(b & 0xFFFF0000u);
-            }
-        }
+        };
+        // (one in 25 has a label of its sixteen rows among these columns)
+        if (__any(label[i] >= 0 && label[i] < 16 * J)) put(std::true_type{});
+        else put(std::false_type{});
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
-template <int I, int J>
-__device__ __forceinline__ void finish(const VocabLogitGrad& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int, char*) {
-    if (n0 + 16 * J <= p.n) logit_grad<I, J, false>(e, p, acc, m0, n0, lane);
-    else logit_grad<I, J, true>(e, p, acc, m0, n0, lane);
+template <int I, int J, int PLANES>
+__device__ __forceinline__ void finish(const VocabLogitGradOf<PLANES>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int) {
+    if (n0 + 16 * J <= p.n) logit_grad<I, J, PLANES, false>(e, p, acc, m0, n0, lane);
+    else logit_grad<I, J, PLANES, true>(e, p, acc, m0, n0, lane);
 }
 
-// fp32 results, half the columns at a time: f(row, column, four results)
-template <int I, int J, typename F>
-__device__ __forceinline__ void leave_f32(floatx4 (&acc)[I][J], char* room, int lane, F&& f) {
-    constexpr int ROW = 32 * J;
-#pragma unroll
-    for (int c = 0; c < J; c += J / 2) {
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-            for (int j = c; j < c + J / 2; ++j) *reinterpret_cast<floatx4*>(room + room_at<ROW>(16 * i + (lane & 15), 64 * (j - c) + 16 * (lane >> 4))) = acc[i][j];
-        room_done();
-        leave<16 * I, ROW>(room, lane, [&](int r, int byte, uint4 x) { f(r, 16 * c + byte / 4, __builtin_bit_cast(float4, x)); });
-        room_done();
-    }
-}
 // Sums lie as the wavefronts hold them, a wavefront's 16 x 16 results in 1 KB after another (sum_place): the next piece begins with them.
 template <int I, int J>
 __device__ __forceinline__ float4* sums_of(const VocabSums& e, int m0, int n0, int split, int lane) {
@@ -181,39 +173,38 @@ __device__ __forceinline__ void begin(const VocabSums& e, floatx4 (&acc)[I][J], 
 template <int I, int J, typename Args>
 __device__ __forceinline__ void begin(const Args&, floatx4 (&)[I][J], int, int, int, int) {}
 template <int I, int J>
-__device__ __forceinline__ void finish(const VocabSums& e, const VocabProduct&, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane, int, char*) {
+__device__ __forceinline__ void finish(const VocabSums& e, const VocabProduct&, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane, int) {
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) *reinterpret_cast<floatx4*>(sums_of<I, J>(e, m0 + 16 * i, n0 + 16 * j, split, lane)) = acc[i][j];
 }
-template <int I, int J>
-__device__ __forceinline__ void finish(const VocabOutOf<float>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int m_rows, char* room) {
+template <int I, int J, typename T>
+__device__ __forceinline__ void finish(const VocabOutOf<T>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int m_rows) {
     const float u = *e.unit;
-    leave_f32(acc, room, lane, [&](int r, int c, float4 x) __attribute__((always_inline)) {
-        if (m0 + r < m_rows && n0 + c < p.n)
-            *reinterpret_cast<float4*>(static_cast<float*>(e.out) + (int64_t)(m0 + r) * e.ld + n0 + c) = make_float4(u * x.x, u * x.y, u * x.z, u * x.w);
-    });
-}
-template <int I, int J>
-__device__ __forceinline__ void finish(const VocabOutOf<bf16>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int m_rows, char* room) {
-    constexpr int ROW = 32 * J;
-    const float u = *e.unit;
+    const int m = m0 + (lane & 15), n = n0 + 4 * (lane >> 4);
+    T* const first = static_cast<T*>(e.out) + (int64_t)m * e.ld + n;
+    auto put = [&](auto ends) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i) {
+            T* const row = first + (int64_t)(16 * i) * e.ld;
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-            *reinterpret_cast<uint2*>(room + room_at<ROW>(16 * i + (lane & 15), 32 * j + 8 * (lane >> 4))) =
-                make_uint2(pack2(u * acc[i][j][0], u * acc[i][j][1]), pack2(u * acc[i][j][2], u * acc[i][j][3]));
-    room_done();
-    leave<16 * I, ROW>(room, lane, [&](int r, int byte, uint4 x) __attribute__((always_inline)) {
-        if (m0 + r < m_rows && n0 + byte / 2 < p.n) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.out) + (int64_t)(m0 + r) * e.ld + n0 + byte / 2) = x;
-    });
+            for (int j = 0; j < J; ++j)
+                if (!decltype(ends)::value || (m + 16 * i < m_rows && n + 16 * j < p.n))       // (p.n a multiple of eight)
+                    store4(row + 16 * j, u * result<I == 8>(acc[i][j], 0), u * result<I == 8>(acc[i][j], 1), u * result<I == 8>(acc[i][j], 2), u * result<I == 8>(acc[i][j], 3));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (m0 + 16 * I <= m_rows && n0 + 16 * J <= p.n) put(std::false_type{});
+    else put(std::true_type{});
 }
+
+// Of the stores of a unit's results, so many are issued whatever the unit holds (dz: 64 or more, as many as the counter of outstanding accesses can tell apart)
+constexpr int stores_behind(Epilogue E) { return E == LOGIT_GRAD || E == LOGIT_GRAD_PARTS ? 52 : 0; }
 
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 __global__ __launch_bounds__(256) void k_vocab_small(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
-    __shared__ __attribute__((aligned(16))) char lds[4 * S_ROOM];        // two operands, then results
+    __shared__ __attribute__((aligned(16))) char lds[2 * S_OP];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m_rows = p.m_count ? *p.m_count : p.m, k_all = ((p.k_count ? *p.k_count : p.k) + VK - 1) / VK;
     const int gm = (int)((m_rows + SM - 1) / SM), gn = (p.n + SM - 1) / SM, ntiles = gm * gn;
@@ -277,8 +268,7 @@ __global__ __launch_bounds__(256) void k_vocab_small(const VocabProduct p, const
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
         }
-    __syncthreads();
-    finish(e, p, acc, m0 + wm, n0 + wn, split, lane, m_rows, lds + S_ROOM * wave);
+    finish(e, p, acc, m0 + wm, n0 + wn, split, lane, m_rows);
 }
 
 // ---- 256 x 256 tiles, four wavefronts of 128 x 128, the sums in the accumulation half of the registers
@@ -351,55 +341,85 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m_rows = p.m_count ? *p.m_count : p.m, k_rows = p.k_count ? *p.k_count : p.k;
-    // Workgroup -> (tile, range of the contraction): XCD x takes a contiguous share of them, range by range, so that what runs there at a time
-    // reads the same operands
+    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
+    // Units are (tile, range of the contraction), range by range.  XCD x takes a contiguous share of them, its workgroups in turn, so that what runs there
+    // at a time reads the same operands.
     const int gm = (m_rows + VT - 1) / VT, gn = (p.n + VT - 1) / VT, ntiles = gm * gn, units = ntiles * p.splits, Q = (units + 7) >> 3;
-    const int slot = blockIdx.x >> 3, unit = (blockIdx.x & 7) * Q + slot;
-    if (slot >= Q || unit >= units) return;
-    const int split = unit / ntiles;
-    int mi, ni;
-    tile_coords(unit - split * ntiles, gm, gn, mi, ni);
-    const int m0 = mi * VT, n0 = ni * VT, wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
-    const int k_all = (k_rows + L_PAIR - 1) / L_PAIR, per = (k_all + p.splits - 1) / p.splits, kb = min(split * per, k_all), ke = min(kb + per, k_all);
-    const int first_term = p.planes == 1 ? 5 : 0, pairs = (ke - kb) * (6 - first_term);
+    const int end = min(((int)(blockIdx.x & 7) + 1) * Q, units), each = gridDim.x >> 3;
+    int unit = (blockIdx.x & 7) * Q + (blockIdx.x >> 3);
+    if (unit >= end) return;
+    const int k_all = (k_rows + L_PAIR - 1) / L_PAIR, first_term = p.planes == 1 ? 5 : 0;
+    struct Unit { int m0, n0, split, kb, ke; };
+    auto decode = [&](int u) __attribute__((always_inline)) {
+        const int split = u / ntiles;
+        int mi, ni;
+        tile_coords(u - split * ntiles, gm, gn, mi, ni);
+        auto uniform = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+        return Unit{uniform(mi * VT), uniform(ni * VT), uniform(split), uniform((int)((int64_t)split * k_all / p.splits)), uniform((int)((int64_t)(split + 1) * k_all / p.splits))};
+    };
+    floatx4 acc[8][8];
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    };
+    if (k_all == 0) {                     // a batch without labels
+        clear();
+        for (; unit < end; unit += each) {
+            const Unit x = decode(unit);
+            finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
+        }
+        return;
+    }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
+    // The loads run two pairs ahead of the products, into the next unit where the present one ends, so that only the first has to wait for them
     LargeLoads<A_ALONG> la;
     LargeLoads<B_ALONG> lb;
-    la.aim_rows(p.a, m0, wave, lane, L_PAIR);
-    lb.aim_rows(p.b, n0, wave, lane, L_PAIR);
     // An operand that is read across ends inside its last pair only where it is the caller's own embedding (one part): rows past its end are its last
     const int tail = B_ALONG ? L_PAIR : p.b.rows - (k_all - 1) * L_PAIR;
-    int at_t = kb, at_term = first_term;  // of the pair that is loaded next; past the end it stays the last
+    Unit ahead;
+    int ahead_unit = unit, at_t, at_term;
+    bool enter = true;
     auto aim = [&]() __attribute__((always_inline)) {
-        if (!B_ALONG && at_t == k_all - 1 && tail < L_PAIR) lb.aim_rows(p.b, n0, wave, lane, tail);
-        la.aim_pair(p.a, m0, PART_A[at_term], at_t);
-        lb.aim_pair(p.b, n0, PART_B[at_term], at_t);
-        if (at_t + 1 < ke) ++at_t;
-        else if (at_term < 5) ++at_term, at_t = kb;
+        if (enter) {
+            ahead = decode(ahead_unit);
+            la.aim_rows(p.a, ahead.m0, wave, lane, L_PAIR);
+            lb.aim_rows(p.b, ahead.n0, wave, lane, L_PAIR);
+            at_t = ahead.kb;
+            at_term = first_term;
+        }
+        if (!B_ALONG && at_t == k_all - 1 && tail < L_PAIR) lb.aim_rows(p.b, ahead.n0, wave, lane, tail);
+        la.aim_pair(p.a, ahead.m0, PART_A[at_term], at_t);
+        lb.aim_pair(p.b, ahead.n0, PART_B[at_term], at_t);
+        enter = false;
+        if (at_t + 1 < ahead.ke) {
+            ++at_t;
+        } else if (at_term < 5) {
+            ++at_term;
+            at_t = ahead.kb;
+        } else if (ahead_unit + each < end) {
+            ahead_unit += each;
+            enter = true;
+        }                                 // (behind the last pair of all: that again, for nobody)
     };
     const uint32_t mine = 8192u * wave;
     auto next = [&](uint32_t stage) __attribute__((always_inline)) { return stage == (L_STAGES - 1) * L_STAGE ? 0u : stage + L_STAGE; };
     const LargeReads<A_ALONG> ra(wm, lane);
     const LargeReads<B_ALONG> rb(wn, lane);
-
-    floatx4 acc[8][8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    begin(e, acc, m0 + wm, n0 + wn, split, lane);
     bf16x8 a[2][8], b[2][8];
-    // products from register set SET; half 1 - SET of the stages sa, sb goes to the other set, a stage's loads to `to`
-    auto step = [&](auto set, uint32_t sa, uint32_t sb, uint32_t to) __attribute__((always_inline)) {
+    // products from register set SET; half 1 - SET of the stages sa, sb goes to the other set, a stage's loads to `to`.  (The products by hand: the compiler would keep
+    // some of the sums outside the accumulation registers and spill.)
+    auto step = [&](auto set, auto fresh, uint32_t sa, uint32_t sb, uint32_t to) __attribute__((always_inline)) {
         constexpr int P = decltype(set)::value;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             shortx4 pa[2], pb[2];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                // (by hand: the compiler would keep some of the sums outside the accumulation registers and spill)
-                asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b[P][j]), "v"(a[P][i]));
+                if constexpr (decltype(fresh)::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b[P][j]), "v"(a[P][i]));
+                else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b[P][j]), "v"(a[P][i]));
                 if (j == 0) rb.template half<1 - P>(sb, i, 0, b[P ^ 1][i], pb);
                 if (j == 1) rb.template half<1 - P>(sb, i, 1, b[P ^ 1][i], pb);
                 if (j == 3) ra.template half<1 - P>(sa, i, 0, a[P ^ 1][i], pa);
@@ -413,67 +433,88 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
         }
     };
 
-    if (pairs > 0) {
-        uint32_t sa = lds0, sb = lds0 + L_STAGE, to = mine;         // (of the present pair; of the loads, from lds0 on)
-        for (int d = 0; d < 2; ++d) {
-            aim();
+    uint32_t sa = lds0, sb = lds0 + L_STAGE, to = lds0 + mine;      // of the present pair; of the loads
+    for (int d = 0; d < 2; ++d) {
+        aim();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) la.piece(j, lds0 + to);
-            to += L_STAGE;
+        for (int j = 0; j < 8; ++j) la.piece(j, to);
+        to += L_STAGE;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) lb.piece(j, lds0 + to);
-            to += L_STAGE;
+        for (int j = 0; j < 8; ++j) lb.piece(j, to);
+        to += L_STAGE;
+    }
+    wait_loads<16>();
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        shortx4 pa[2], pb[2];
+        rb.template half<0>(sb, i, 0, b[0][i], pb);
+        rb.template half<0>(sb, i, 1, b[0][i], pb);
+        ra.template half<0>(sa, i, 0, a[0][i], pa);
+        ra.template half<0>(sa, i, 1, a[0][i], pa);
+    }
+    uint32_t at = 4 * L_STAGE, na = 2 * L_STAGE, nb = 3 * L_STAGE;  // stage that is loaded next, and those of the next pair
+    auto first = [&](auto fresh) __attribute__((always_inline)) {
+        aim();
+        step(std::integral_constant<int, 0>{}, fresh, sa, sb, lds0 + at + mine);
+        at = next(at);
+    };
+    auto second = [&]() __attribute__((always_inline)) {
+        sa = lds0 + na;
+        sb = lds0 + nb;
+        step(std::integral_constant<int, 1>{}, std::false_type{}, sa, sb, lds0 + at + mine);
+        at = next(at);
+        na = next(nb);
+        nb = next(na);
+    };
+    bool stored = false;
+    for (; unit < end; unit += each) {
+        const Unit x = decode(unit);
+        const int pairs = (x.ke - x.kb) * (6 - first_term);
+        if constexpr (E == SUMS) {
+            clear();
+            begin(e, acc, x.m0 + wm, x.n0 + wn, x.split, lane);
+            first(std::false_type{});
+        } else {
+            first(std::true_type{});
         }
-        wait_loads<16>();
+        // The next pair is in LDS, and everyone has read this one.  Behind its loads only the stage above may be on its way; behind a unit also the stores of
+        // its results, which were issued after them.
+        if (stores_behind(E) > 0 && stored) wait_loads<8 + stores_behind(E)>();
+        else wait_loads<8>();
+        stored = true;
         lds_barrier();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            shortx4 pa[2], pb[2];
-            rb.template half<0>(sb, i, 0, b[0][i], pb);
-            rb.template half<0>(sb, i, 1, b[0][i], pb);
-            ra.template half<0>(sa, i, 0, a[0][i], pa);
-            ra.template half<0>(sa, i, 1, a[0][i], pa);
-        }
-        uint32_t at = 4 * L_STAGE;                                  // stage that is loaded next, and those of the next pair
-        uint32_t na = 2 * L_STAGE, nb = 3 * L_STAGE;
+        second();
 #pragma unroll 1
-        for (int d = 0; d < pairs; ++d) {
-            aim();
-            step(std::integral_constant<int, 0>{}, sa, sb, lds0 + at + mine);
-            at = next(at);
-            // the next pair is in LDS, and everyone has read this one
+        for (int d = 1; d < pairs; ++d) {
+            first(std::false_type{});
             wait_loads<8>();
             lds_barrier();
-            sa = lds0 + na;
-            sb = lds0 + nb;
-            step(std::integral_constant<int, 1>{}, sa, sb, lds0 + at + mine);
-            at = next(at);
-            na = next(nb);
-            nb = next(na);
+            second();
         }
+        // the last product is 18 wait states from its result
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+        finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
     }
-    // nothing may arrive in LDS that is not ours any more; and the last product is 18 wait states from its result
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
-    __syncthreads();
-    finish(e, p, acc, m0 + wm, n0 + wn, split, lane, m_rows, lds + 32768 * wave);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
 }
 
 bool small(int m) { return m <= 128; }
 
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipStream_t s) {
-    if (small(E == SUMS || E == STATS || E == LOGIT_GRAD ? p.m : p.k)) {
+    if (small(E == OUT_F32 || E == OUT_BF16 ? p.k : p.m)) {
         const int64_t blocks = cdiv(p.m, SM) * cdiv(p.n, SM) * p.splits;
         k_vocab_small<A_ALONG, B_ALONG, E><<<(unsigned)blocks, 256, 0, s>>>(p, e);
     } else {
         static uint64_t done = 0;
         const auto kernel = k_vocab_large<A_ALONG, B_ALONG, E>;
         if (int rc = allow_lds(reinterpret_cast<const void*>(kernel), (int)L_LDS, done)) return rc;
-        kernel<<<(unsigned)(8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8)), 256, L_LDS, s>>>(p, e);
+        kernel<<<(unsigned)std::min<int64_t>(256, 8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8)), 256, L_LDS, s>>>(p, e);      // (one to a CU)
     }
     MST_LAUNCH_CHECK();
     return MST_OK;
@@ -495,7 +536,10 @@ int vocab_splits(int m, int n, int k) {
 }
 
 int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s) { return launch<true, true, STATS>(p, e, s); }
-int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s) { return launch<true, true, LOGIT_GRAD>(p, e, s); }
+int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s) {
+    if (p.planes > 1) return launch<true, true, LOGIT_GRAD_PARTS>(p, {e}, s);
+    return launch<true, true, LOGIT_GRAD>(p, {e}, s);
+}
 int vocab_sums(const VocabProduct& p, const VocabSums& e, hipStream_t s) { return launch<true, false, SUMS>(p, e, s); }
 int vocab_out(const VocabProduct& p, const VocabOut& e, hipStream_t s) {
     if (e.f32) return launch<false, false, OUT_F32>(p, {e}, s);

@@ -221,7 +221,7 @@ struct Plan {
         pieces = (int)cdiv(s.vocab, piece);
         stats = (int)cdiv(s.vocab, STAT_COLUMNS);
         sum_blocks = (int)align_up(s.width, VT) / 16;
-        splits = vocab_splits(s.tokens, s.width, piece);
+        splits = vocab_splits(s.tokens, s.width, std::min(piece, s.vocab));
         bytes = 0;
         auto part = [&](size_t n) { const size_t at = bytes; bytes += align_up(n); return at; };
         count = part(4);
@@ -304,7 +304,7 @@ struct Run {
             if (int rc = vocab_logit_grad(z, {at<uint16_t>(plan.ds), plane, plan.piece, at<float>(plan.lse), at<float>(plan.d), at<int>(plan.label), at<float>(plan.at_label),
                                              i * plan.piece}, stream)) return rc;
             if (dh) {
-                const VocabProduct p = {ds_rows, e, at<int>(plan.count), nullptr, s.tokens, s.width, n, plan.planes, plan.splits};
+                const VocabProduct p = {ds_rows, e, at<int>(plan.count), nullptr, s.tokens, s.width, n, plan.planes, (int)std::min<int64_t>(plan.splits, cdiv(n, VPAD))};      // (a last piece may be short)
                 if (int rc = vocab_sums(p, {at<float>(plan.sums), plan.sum_stride(), plan.sum_blocks, i > 0}, stream)) return rc;
             }
             if (dE) {
