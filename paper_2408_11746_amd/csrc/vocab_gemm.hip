@@ -56,15 +56,15 @@ __device__ __forceinline__ float result(const floatx4& acc, int v) {
     return x;
 }
 
-// Sums of exp2(z log2 e - base) over 64 columns, those below p.n.  Base is the logit of the row's own label: the sum over all columns is then 1 at least,
+// Sums of exp2(z log2 e - base) over a wavefront's columns, those below p.n.  Base is the logit of the row's own label: the sum over all columns is then 1 at least,
 // what is lost below fp32 does not count in it, and no maximum has to be found first (a fifth of the instructions).  A sum that leaves fp32 is formed again
 // from the row's maximum here.
 template <int I, int J, bool ENDS, bool MAXIMUM>
-__device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int c, int m0, int n0, int lane) {
+__device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
     const int last = p.n - n0 - 4 * (lane >> 4);
     auto larger = [](float a, float b) { return fmaxf(a, b); };
     auto plus = [](float a, float b) { return a + b; };
-    float2* const to = e.stats + (int64_t)(e.first + n0 / STAT_COLUMNS + c / 4) * e.row_stride + m0 + (lane & 15);
+    float2* const to = e.stats + (int64_t)(e.first + n0 / (16 * J)) * e.row_stride + m0 + (lane & 15);
     float base[I];
 #pragma unroll
     for (int i = 0; i < I; ++i) base[i] = MAXIMUM ? 0.f : e.at_label[m0 + 16 * i + (lane & 15)] * LOG2E;
@@ -76,14 +76,14 @@ __device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProdu
             return !ENDS || 16 * j + v < last ? x : -INFINITY;
         };
         if constexpr (MAXIMUM) {
-            float top = z(c, 0);
+            float top = z(0, 0);
 #pragma unroll
-            for (int j = c; j < c + 4; ++j) top = fmaxf(fmaxf(fmaxf(top, z(j, 0)), fmaxf(z(j, 1), z(j, 2))), z(j, 3));
+            for (int j = 0; j < J; ++j) top = fmaxf(fmaxf(fmaxf(top, z(j, 0)), fmaxf(z(j, 1), z(j, 2))), z(j, 3));
             base[i] = apart<32>(apart<16>(top, larger), larger) * LOG2E;
         }
         float sum = 0.f;
 #pragma unroll
-        for (int j = c; j < c + 4; ++j)
+        for (int j = 0; j < J; ++j)
 #pragma unroll
             for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(z(j, v), LOG2E, -base[i]));
         sum = apart<32>(apart<16>(sum, plus), plus);
@@ -94,17 +94,13 @@ __device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProdu
     return fits;
 }
 template <int I, int J, bool ENDS>
-__device__ __forceinline__ void statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int c, int m0, int n0, int lane) {
-    if (__any(!statistics<I, J, ENDS, false>(e, p, acc, c, m0, n0, lane))) statistics<I, J, ENDS, true>(e, p, acc, c, m0, n0, lane);
+__device__ __forceinline__ void statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
+    if (__any(!statistics<I, J, ENDS, false>(e, p, acc, m0, n0, lane))) statistics<I, J, ENDS, true>(e, p, acc, m0, n0, lane);
 }
 template <int I, int J>
 __device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int) {
-#pragma unroll
-    for (int c = 0; c < J; c += 4) {
-        const int first = n0 + 16 * c;
-        if (first + STAT_COLUMNS <= p.n) statistics<I, J, false>(e, p, acc, c, m0, n0, lane);
-        else if (first < p.n) statistics<I, J, true>(e, p, acc, c, m0, n0, lane);
-    }
+    if (n0 + 16 * J <= p.n) statistics<I, J, false>(e, p, acc, m0, n0, lane);
+    else if (n0 < p.n) statistics<I, J, true>(e, p, acc, m0, n0, lane);
 }
 
 // dz
@@ -503,6 +499,112 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
 }
 
+// ---- few tokens: the embedding is read once, straight into registers, and that bounds it
+// A wavefront takes sixteen rows of the embedding and 16 TT tokens; both operands come as the product wants them, eight consecutive numbers of a row to a lane (the
+// tokens' out of the first cache).  fp32 numbers are split on the way.
+template <typename T> struct Parts;                                 // of eight numbers, as operands
+template <> struct Parts<bf16> {
+    bf16x8 v[1];
+    __device__ __forceinline__ Parts(const bf16* p, bool there) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (there) w = *reinterpret_cast<const uint4*>(p);
+        v[0] = __builtin_bit_cast(bf16x8, w);
+    }
+};
+template <> struct Parts<float> {
+    bf16x8 v[PLANES_MAX];
+    __device__ __forceinline__ Parts(const float* p, bool there) {
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (there) load8(p, x);
+#pragma unroll
+        for (int part = 0; part < PLANES_MAX; ++part) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = pack2(x[2 * e], x[2 * e + 1]);
+                x[2 * e] -= __uint_as_float(w[e] << 16);
+                x[2 * e + 1] -= __uint_as_float(w[e] & 0xFFFF0000u);
+            }
+            v[part] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+    }
+};
+__device__ __forceinline__ void terms(const Parts<bf16>& a, const Parts<bf16>& b, floatx4& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[0], b.v[0], c, 0, 0, 0); }
+__device__ __forceinline__ void terms(const Parts<float>& a, const Parts<float>& b, floatx4& c) {
+    constexpr int A[6] = {0, 2, 1, 0, 1, 0}, B[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+    for (int t = 0; t < 6; ++t) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[A[t]], b.v[B[t]], c, 0, 0, 0);
+}
+
+template <typename T, int TT>
+__global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, const T* __restrict__ E, const int* __restrict__ labels, int tokens, int W, int V,
+                                                   float2* __restrict__ stats, float* __restrict__ at_label) {
+    __shared__ float2 part[4][16 * TT];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+    const int v0 = blockIdx.x * VOCAB_FEW_COLUMNS + 16 * wave, t0 = blockIdx.y * 16 * TT;
+    const T* const e = E + (int64_t)min(v0 + r, V - 1) * W + 8 * g;
+    const T* x[TT];
+#pragma unroll
+    for (int i = 0; i < TT; ++i) x[i] = h + (int64_t)min(t0 + 16 * i + r, tokens - 1) * W + 8 * g;
+    floatx4 acc[TT];
+#pragma unroll
+    for (int i = 0; i < TT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int whole = W & ~31;
+    constexpr int U = sizeof(T) == 2 ? 8 : 4;                       // steps whose loads are on the way together
+    int k = 0;
+    for (; k + 32 * U <= whole; k += 32 * U) {
+        uint4 raw[U][sizeof(T) / 2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q) raw[u][q] = reinterpret_cast<const uint4*>(e + k + 32 * u)[q];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const Parts<T> b(reinterpret_cast<const T*>(raw[u]), true);
+#pragma unroll
+            for (int i = 0; i < TT; ++i) terms(b, Parts<T>(x[i] + k + 32 * u, true), acc[i]);
+        }
+    }
+    for (; k < W; k += 32) {                                        // (a last step may be short: W is a multiple of eight)
+        const bool there = k + 8 * g < W;
+        const Parts<T> b(e + k, there);
+#pragma unroll
+        for (int i = 0; i < TT; ++i) terms(b, Parts<T>(x[i] + k, there), acc[i]);
+    }
+    // acc[i][v]: column v0 + 4 g + v, token t0 + 16 i + r
+    auto larger = [](float a, float b) { return fmaxf(a, b); };
+    auto plus = [](float a, float b) { return a + b; };
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+        const int token = t0 + 16 * i + r, label = token < tokens ? labels[token] : -1;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int col = v0 + 4 * g + v;
+            if (col == label && col < V) at_label[token] = acc[i][v];
+            if (col >= V) acc[i][v] = -INFINITY;
+            top = fmaxf(top, acc[i][v]);
+        }
+        top = apart<32>(apart<16>(top, larger), larger);
+        const float base = top == -INFINITY ? 0.f : top * LOG2E;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(acc[i][v], LOG2E, -base));
+        sum = apart<32>(apart<16>(sum, plus), plus);
+        if (g == 0) part[wave][16 * i + r] = make_float2(top == -INFINITY ? -INFINITY : base, sum);
+    }
+    __syncthreads();
+    const int mine = threadIdx.x;
+    if (mine >= 16 * TT || t0 + mine >= tokens) return;
+    float2 all = part[0][mine];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float2 o = part[w][mine];
+        const float m = fmaxf(all.x, o.x), from = m == -INFINITY ? 0.f : m;
+        all = make_float2(m, all.y * exp2_fast(all.x - from) + o.y * exp2_fast(o.x - from));
+    }
+    stats[(int64_t)blockIdx.x * tokens + t0 + mine] = all;
+}
+
 bool small(int m) { return m <= 128; }
 
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
@@ -522,6 +624,8 @@ int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipSt
 
 }  // namespace
 
+int vocab_stat_columns(int m) { return small(m) ? SM / 2 : VT / 2; }
+
 // As many ranges as let the products end first: rounds of 256 workgroups, each as long as its range and what begins and ends it (the time of some eight
 // pairs of steps, the sums of the pieces before and behind among it).
 int vocab_splits(int m, int n, int k) {
@@ -533,6 +637,24 @@ int vocab_splits(int m, int n, int k) {
         if (time < least) least = time, best = s;
     }
     return best;
+}
+
+int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream) {
+    auto launch = [&](auto type, auto tt) {
+        using T = decltype(type);
+        constexpr int TT = decltype(tt)::value;
+        k_vocab_few<T, TT><<<dim3((unsigned)cdiv(s.vocab, VOCAB_FEW_COLUMNS), (unsigned)cdiv(s.tokens, 16 * TT)), 256, 0, stream>>>(
+            static_cast<const T*>(h), static_cast<const T*>(E), labels, s.tokens, s.width, s.vocab, stats, at_label);
+    };
+    auto typed = [&](auto type) {
+        if (s.tokens <= 16) launch(type, std::integral_constant<int, 1>{});
+        else if (s.tokens <= 32) launch(type, std::integral_constant<int, 2>{});
+        else launch(type, std::integral_constant<int, 4>{});
+    };
+    if (s.type == MST_F32) typed(float{});
+    else typed(bf16{});
+    MST_LAUNCH_CHECK();
+    return MST_OK;
 }
 
 int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s) { return launch<true, true, STATS>(p, e, s); }

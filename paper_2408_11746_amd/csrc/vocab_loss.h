@@ -30,10 +30,9 @@ struct VocabProduct {
 };
 
 // ---- what becomes of C
-// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and STAT_COLUMNS columns
-constexpr int STAT_COLUMNS = 64;
+// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and vocab_stat_columns columns
 struct VocabStats {
-    float2* stats;                       // [STAT_COLUMNS columns][row_stride]
+    float2* stats;                       // [vocab_stat_columns columns][row_stride]
     int64_t row_stride;
     int first;                           // number of the first of them
     const float* at_label;               // logit of a row's label, padded to VT
@@ -63,7 +62,11 @@ struct VocabOut {                        // rows of the result times the unit, i
     const float* unit;
 };
 
+int vocab_stat_columns(int m);
 int vocab_splits(int m, int n, int k);   // ranges of the contraction for vocab_sums
+// The forward for few tokens, from the hidden states as they are: statistics per VOCAB_FEW_COLUMNS columns, [columns][tokens], and each label's logit
+constexpr int VOCAB_FEW = 128, VOCAB_FEW_COLUMNS = 64;
+int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream);
 int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s);            // a, b along
 int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s);   // a, b along
 int vocab_sums(const VocabProduct& p, const VocabSums& e, hipStream_t s);              // a along, b across

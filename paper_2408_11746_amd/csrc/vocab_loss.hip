@@ -17,7 +17,7 @@ namespace {
 constexpr int64_t PIECE_BYTES = int64_t(1) << 28;
 
 // ---- which tokens have a label
-constexpr int ROWS_THREADS = 1024, ROWS_EACH = 16;
+constexpr int ROWS_THREADS = 1024, ROWS_EACH = 8;
 // One workgroup: place[token] = its row or -1, list[row] = token, label[row], count.  In order.  Rows behind the last, up to a whole tile: label -1.
 // Outputs of tokens without one: 0.  unit: the largest size of the rows' dloss (1 if all are 0).
 __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restrict__ labels, int T, int V, int* __restrict__ count, int* __restrict__ place,
@@ -29,10 +29,26 @@ __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restri
     int before = 0;                                                 // rows of the tokens before this round's
     for (int t0 = 0; t0 < T; t0 += ROWS_THREADS * ROWS_EACH) {
         int mine[ROWS_EACH], n = 0;
+        float d[ROWS_EACH];
         const int first = t0 + tid * ROWS_EACH;
+        if (first + ROWS_EACH <= T) {
+#pragma unroll
+            for (int e = 0; e < ROWS_EACH; e += 4) {
+                const int4 x = *reinterpret_cast<const int4*>(labels + first + e);
+                mine[e] = x.x, mine[e + 1] = x.y, mine[e + 2] = x.z, mine[e + 3] = x.w;
+                if (!dloss) continue;
+                const float4 y = *reinterpret_cast<const float4*>(dloss + first + e);
+                d[e] = y.x, d[e + 1] = y.y, d[e + 2] = y.z, d[e + 3] = y.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < ROWS_EACH; ++e) {
+                mine[e] = first + e < T ? labels[first + e] : -1;
+                d[e] = dloss && first + e < T ? dloss[first + e] : 0.f;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < ROWS_EACH; ++e) {
-            mine[e] = first + e < T ? labels[first + e] : -1;
             if (mine[e] < 0 || mine[e] >= V) mine[e] = -1;
             n += mine[e] >= 0;
         }
@@ -56,7 +72,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restri
                 const bool has = mine[e] >= 0;
                 place[first + e] = has ? row : -1;
                 if (has) list[row] = first + e, label[row] = mine[e], ++row;
-                if (has && dloss) top = max(top, __float_as_int(dloss[first + e]) & 0x7FFFFFFF);
+                if (has && dloss) top = max(top, __float_as_int(d[e]) & 0x7FFFFFFF);
                 if (!has && loss) loss[first + e] = 0.f;
                 if (!has && lse) lse[first + e] = 0.f;
             }
@@ -139,11 +155,14 @@ __global__ __launch_bounds__(256) void k_vocab_parts(const T* __restrict__ E, in
     }
 }
 
-// sums of a row joined: 64 rows a workgroup, a quarter of the statistics a wavefront
-__global__ __launch_bounds__(256) void k_vocab_join(const float2* __restrict__ stats, int64_t stride, int n, const int* __restrict__ count, const int* __restrict__ list,
-                                                    const float* __restrict__ at_label, float* __restrict__ loss, float* __restrict__ lse) {
-    __shared__ float2 part[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 64 + lane, rows = *count;
+// sums of a row joined: 64 rows a workgroup, a sixteenth of the statistics a wavefront.  Rows are tokens (count and list null; `vocab` says which have a label), or
+// the packed ones.
+constexpr int JOIN_WAVES = 16;
+__global__ __launch_bounds__(64 * JOIN_WAVES) void k_vocab_join(const float2* __restrict__ stats, int64_t stride, int n, int tokens, const int* __restrict__ count,
+                                                                const int* __restrict__ list, const int* __restrict__ labels, int vocab, const float* __restrict__ at_label,
+                                                                float* __restrict__ loss, float* __restrict__ lse) {
+    __shared__ float2 part[JOIN_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 64 + lane, rows = count ? *count : tokens;
     if ((int)blockIdx.x * 64 >= rows) return;
     float top = -INFINITY, sum = 0.f;
     auto add = [&](float2 x) __attribute__((always_inline)) {
@@ -151,16 +170,18 @@ __global__ __launch_bounds__(256) void k_vocab_join(const float2* __restrict__ s
         sum = sum * exp2_fast(top - from) + x.y * exp2_fast(x.x - from);
         top = m;
     };
+    if (row < rows)
 #pragma unroll 8
-    for (int i = wave; i < n; i += 4) add(stats[(int64_t)i * stride + row]);
+        for (int i = wave; i < n; i += JOIN_WAVES) add(stats[(int64_t)i * stride + row]);
     part[wave][lane] = make_float2(top, sum);
     __syncthreads();
     if (wave || row >= rows) return;
-    for (int w = 1; w < 4; ++w) add(part[w][lane]);
+    for (int w = 1; w < JOIN_WAVES; ++w) add(part[w][lane]);
     const float l = (top + log2f(sum)) * 0.69314718f;
-    const int token = list[row];
-    lse[token] = l;
-    if (loss) loss[token] = l - at_label[row];
+    const int token = list ? list[row] : row;
+    const bool has = !labels || (labels[token] >= 0 && labels[token] < vocab);
+    lse[token] = has ? l : 0.f;
+    if (loss) loss[token] = has ? l - at_label[row] : 0.f;
 }
 
 // gradients of the hidden states: sums of the splits, back to the tokens' places; a wavefront takes blocks of 16 rows and 16 columns
@@ -205,7 +226,8 @@ struct Plan {
     bool split_E;                        // the products read the embedding from its parts
     int piece, pieces;                   // columns of the vocabulary, and how often
     int splits, sum_blocks;              // of the sums for dh; blocks along a row
-    int stats;
+    bool few;                            // tokens, of which none is packed
+    int stats, stat_columns;
     size_t count, unit, place, list, label, at_label, lse, d, h, E, stat, ds, sums, bytes;
 
     int64_t sum_stride() const { return rows * sum_blocks * 16; }
@@ -219,7 +241,9 @@ struct Plan {
         pieces = (int)cdiv(s.vocab, most);
         piece = (int)align_up(cdiv(s.vocab, pieces), VT);
         pieces = (int)cdiv(s.vocab, piece);
-        stats = (int)cdiv(s.vocab, STAT_COLUMNS);
+        few = !backward && s.tokens <= VOCAB_FEW;
+        stat_columns = few ? VOCAB_FEW_COLUMNS : vocab_stat_columns(s.tokens);
+        stats = (int)cdiv(s.vocab, stat_columns);
         sum_blocks = (int)align_up(s.width, VT) / 16;
         splits = vocab_splits(s.tokens, s.width, std::min(piece, s.vocab));
         bytes = 0;
@@ -232,8 +256,8 @@ struct Plan {
         at_label = part(4 * (size_t)rows);
         lse = part(backward ? 4 * (size_t)rows : 0);
         d = part(backward ? 4 * (size_t)rows : 0);
-        h = part(2 * planes * (size_t)rows * wide);
-        E = part(split_E ? 2 * planes * (size_t)piece * wide : 0);
+        h = part(few ? 0 : 2 * planes * (size_t)rows * wide);
+        E = part(split_E && !few ? 2 * planes * (size_t)piece * wide : 0);
         stat = part(backward ? 0 : 8 * (size_t)rows * stats);
         ds = part(backward ? 2 * planes * (size_t)rows * piece : 0);
         sums = part(backward ? 4 * (size_t)splits * sum_stride() : 0);
@@ -279,15 +303,22 @@ struct Run {
     VocabOperand packed() const { return {at<uint16_t>(plan.h), plan.rows * plan.wide, plan.wide, (int)plan.rows}; }
 
     int forward(const int* labels, float* loss, float* lse) const {
+        if (plan.few) {
+            if (int e = vocab_few(s, h, E, labels, at<float2>(plan.stat), at<float>(plan.at_label), stream)) return e;
+            return join(labels, s.tokens, loss, lse);
+        }
         if (int e = rows(labels, loss, lse, nullptr, nullptr)) return e;
         for (int i = 0; i < plan.pieces; ++i) {
             VocabOperand e;
             if (int rc = embedding(i, e)) return rc;
             const VocabProduct p = {packed(), e, at<int>(plan.count), nullptr, s.tokens, columns(i), plan.wide, plan.planes, 1};
-            if (int rc = vocab_stats(p, {at<float2>(plan.stat), plan.rows, i * (plan.piece / STAT_COLUMNS), at<float>(plan.at_label)}, stream)) return rc;
+            if (int rc = vocab_stats(p, {at<float2>(plan.stat), plan.rows, i * (plan.piece / plan.stat_columns), at<float>(plan.at_label)}, stream)) return rc;
         }
-        k_vocab_join<<<(unsigned)cdiv(s.tokens, 64), 256, 0, stream>>>(at<float2>(plan.stat), plan.rows, plan.stats, at<int>(plan.count), at<int>(plan.list),
-                                                                      at<float>(plan.at_label), loss, lse);
+        return join(nullptr, plan.rows, loss, lse);
+    }
+    int join(const int* labels, int64_t stride, float* loss, float* lse) const {
+        k_vocab_join<<<(unsigned)cdiv(s.tokens, 64), 64 * JOIN_WAVES, 0, stream>>>(at<float2>(plan.stat), stride, plan.stats, s.tokens, labels ? nullptr : at<int>(plan.count),
+                                                                                  labels ? nullptr : at<int>(plan.list), labels, s.vocab, at<float>(plan.at_label), loss, lse);
         MST_LAUNCH_CHECK();
         return MST_OK;
     }
