@@ -284,11 +284,11 @@ template <bool ALONG>
 struct LargeLoads {
     uint32_t v[8];
     const char* base;                    // of the pair
-    __device__ __forceinline__ void aim_rows(const VocabOperand& o, int first, int wave, int lane, int left) {
+    __device__ __forceinline__ void aim_rows(const VocabOperand& o, int first, int wave, int lane, int left, int turn) {
         const uint32_t row_bytes = 2u * (uint32_t)o.ld;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int piece = 8 * wave + j;
+            const int piece = 8 * wave + (j ^ turn);
             if constexpr (ALONG) {
                 const int row = 8 * piece + (lane >> 3), u = (lane & 7) ^ pair_mix(row);
                 v[j] = (uint32_t)min(row, o.rows - 1 - first) * row_bytes + 16u * u;
@@ -302,7 +302,8 @@ struct LargeLoads {
         const uint16_t* const from = o.p + part * o.plane;
         base = reinterpret_cast<const char*>(ALONG ? from + (int64_t)first * o.ld + t * L_PAIR : from + (int64_t)t * L_PAIR * o.ld + first);
     }
-    __device__ __forceinline__ void piece(int j, uint32_t to) const { load_to_lds(base, v[j], to + 1024u * j); }
+    // to: the wavefront's 8 KB of the stage (a multiple of that) ^ 1024 turn; the j-th load is of piece j ^ turn
+    __device__ __forceinline__ void piece(int j, uint32_t to) const { load_to_lds(base, v[j], to ^ 1024u * j); }
 };
 // ... and of its reads: eight operands of sixteen rows (or columns) a step, of half `step` of a stage
 template <bool ALONG>
@@ -370,6 +371,9 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
+    // Workgroups that share rows of an operand begin with different pieces of them, so that each meets what another has fetched already.  Loss and gradients of 8192 tokens,
+    // width 1280, vocabulary 50257: 4.21 -> 3.9 ms; of 768 tokens, width 768, where three share what they read from memory: 366 -> 378 us.
+    auto turn = [&](int first) __attribute__((always_inline)) { return first / VT & 7; };
     // The loads run two pairs ahead of the products, into the next unit where the present one ends, so that only the first has to wait for them
     LargeLoads<A_ALONG> la;
     LargeLoads<B_ALONG> lb;
@@ -381,12 +385,12 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     auto aim = [&]() __attribute__((always_inline)) {
         if (enter) {
             ahead = decode(ahead_unit);
-            la.aim_rows(p.a, ahead.m0, wave, lane, L_PAIR);
-            lb.aim_rows(p.b, ahead.n0, wave, lane, L_PAIR);
+            la.aim_rows(p.a, ahead.m0, wave, lane, L_PAIR, turn(ahead.n0));
+            lb.aim_rows(p.b, ahead.n0, wave, lane, L_PAIR, turn(ahead.m0));
             at_t = ahead.kb;
             at_term = first_term;
         }
-        if (!B_ALONG && at_t == k_all - 1 && tail < L_PAIR) lb.aim_rows(p.b, ahead.n0, wave, lane, tail);
+        if (!B_ALONG && at_t == k_all - 1 && tail < L_PAIR) lb.aim_rows(p.b, ahead.n0, wave, lane, tail, turn(ahead.m0));
         la.aim_pair(p.a, ahead.m0, PART_A[at_term], at_t);
         lb.aim_pair(p.b, ahead.n0, PART_B[at_term], at_t);
         enter = false;
@@ -433,10 +437,10 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     for (int d = 0; d < 2; ++d) {
         aim();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) la.piece(j, to);
+        for (int j = 0; j < 8; ++j) la.piece(j, to ^ 1024 * turn(ahead.n0));
         to += L_STAGE;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) lb.piece(j, to);
+        for (int j = 0; j < 8; ++j) lb.piece(j, to ^ 1024 * turn(ahead.m0));
         to += L_STAGE;
     }
     wait_loads<16>();
@@ -452,13 +456,13 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     uint32_t at = 4 * L_STAGE, na = 2 * L_STAGE, nb = 3 * L_STAGE;  // stage that is loaded next, and those of the next pair
     auto first = [&](auto fresh) __attribute__((always_inline)) {
         aim();
-        step(std::integral_constant<int, 0>{}, fresh, sa, sb, lds0 + at + mine);
+        step(std::integral_constant<int, 0>{}, fresh, sa, sb, (lds0 + at + mine) ^ 1024 * turn(ahead.n0));
         at = next(at);
     };
     auto second = [&]() __attribute__((always_inline)) {
         sa = lds0 + na;
         sb = lds0 + nb;
-        step(std::integral_constant<int, 1>{}, std::false_type{}, sa, sb, lds0 + at + mine);
+        step(std::integral_constant<int, 1>{}, std::false_type{}, sa, sb, (lds0 + at + mine) ^ 1024 * turn(ahead.m0));
         at = next(at);
         na = next(nb);
         nb = next(na);
