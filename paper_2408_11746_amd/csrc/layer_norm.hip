@@ -15,7 +15,9 @@ namespace {
 
 constexpr int ROWS_A_BLOCK = 4;          // wavefronts of a workgroup whose rows are one wavefront's
 constexpr int WIDTH_MAX = 16384;
-constexpr int BWD_BLOCKS = 1024;         // workgroups of the backward, at most: rows of the weights' sums
+constexpr int BWD_BLOCKS = 768;          // workgroups of the backward, at most: rows of the weights' sums
+
+__host__ __device__ constexpr int pitch_of(int width) { return (width + 3) & ~3; }      // of a row of the weights' sums
 
 struct NormRows {
     int64_t rows;
@@ -47,15 +49,21 @@ struct Span {
     __device__ Span(int width_) : thread(WAVES == 1 ? threadIdx.x & 63 : threadIdx.x), width(width_) {}
     __device__ int column(int c) const { return 4 * (c * LANES + thread); }
     __device__ int count(int c) const { return c < CH - ENDS ? 4 : width - column(c); }          // (0 or less: none)
+    // The row's address stays in scalar registers and the lane's offset is one of 32 bits: left to itself the compiler keeps a 64-bit address for each quad of each
+    // operand, which take more registers than the numbers.
     template <typename T>
     __device__ void load(const T* row, float (&x)[CH][4]) const {
+        auto at = (__attribute__((address_space(1))) const char*)row;
+        asm("" : "+s"(at));
 #pragma unroll
-        for (int c = 0; c < CH; ++c) load_columns(row + column(c), count(c), x[c]);
+        for (int c = 0; c < CH; ++c) load_columns((const T*)(at + (uint32_t)(thread * 4 * (int)sizeof(T)) + c * LANES * 4 * (int)sizeof(T)), count(c), x[c]);
     }
     template <typename T>
     __device__ void store(T* row, const float (&x)[CH][4]) const {
+        auto at = (__attribute__((address_space(1))) char*)row;
+        asm("" : "+s"(at));
 #pragma unroll
-        for (int c = 0; c < CH; ++c) store_columns(row + column(c), count(c), x[c]);
+        for (int c = 0; c < CH; ++c) store_columns((T*)(at + (uint32_t)(thread * 4 * (int)sizeof(T)) + c * LANES * 4 * (int)sizeof(T)), count(c), x[c]);
     }
     // x - mean where there are columns, 0 elsewhere, and r
     __device__ float center(const NormRows& n, float (&x)[CH][4], float* room) const {
@@ -81,7 +89,7 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
                                                                                          int8_t* __restrict__ codes, float* __restrict__ units) {
     __shared__ float room[WAVES];
     const Span<CH, WAVES, ENDS> span(n.width);
-    const int64_t first = WAVES == 1 ? (int64_t)blockIdx.x * ROWS_A_BLOCK + (threadIdx.x >> 6) : blockIdx.x, step = (int64_t)gridDim.x * (WAVES == 1 ? ROWS_A_BLOCK : 1);
+    const int64_t first = WAVES == 1 ? (int64_t)blockIdx.x * ROWS_A_BLOCK + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x, step = (int64_t)gridDim.x * (WAVES == 1 ? ROWS_A_BLOCK : 1);
     const int per_row = (n.width + KEPT_GROUP - 1) / KEPT_GROUP;
     for (int64_t row = first; row < n.rows; row += step) {
         const int64_t at = row * n.width;
@@ -99,10 +107,12 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
         for (int c = 0; c < CH; ++c) round_columns(x, s[c]);         // what is normed is what the backward pass will find
         if (sum) span.store(sum + at, s);
         if (codes) {
+            auto code_row = (__attribute__((address_space(1))) int8_t*)(codes + at);
+            asm("" : "+s"(code_row));
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const float unit = kept_unit(s[c]);
-                store_codes(codes + at + span.column(c), span.count(c), s[c], unit);
+                store_codes((int8_t*)(code_row + (uint32_t)(span.thread * 4) + c * span.LANES * 4), span.count(c), s[c], unit);
                 const int group = span.column(c) / KEPT_GROUP;
                 if ((threadIdx.x & 31) == 0 && group < per_row) units[row * per_row + group] = unit;
             }
@@ -119,9 +129,11 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
     }
 }
 
+// wavefronts of a SIMD that the registers have to suffice for
+constexpr int bwd_waves(int ch, int waves) { return ch <= 3 ? 4 : waves == 1 && ch <= 5 ? 3 : 2; }
 // TS int8_t: from what was kept
 template <int CH, int WAVES, int ENDS, typename TS, typename TX, typename TG>
-__global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_layer_norm_bwd(NormRows n, const TS* __restrict__ sum, const float* __restrict__ units,
+__global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) __attribute__((amdgpu_waves_per_eu(bwd_waves(CH, WAVES)))) void k_layer_norm_bwd(NormRows n, const TS* __restrict__ sum, const float* __restrict__ units,
                                                                                              const float* __restrict__ weight, const float* __restrict__ bias,
                                                                                              const TG* __restrict__ dy, const TX* ds, TX* dx, void* __restrict__ y, int y_f32,
                                                                                              float* __restrict__ partial) {
@@ -129,31 +141,36 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
     __shared__ float room[WAVES];
     __shared__ float4 sums[SHARED][CH * 64 + 1];
     const Span<CH, WAVES, ENDS> span(n.width);
-    const int64_t first = WAVES == 1 ? (int64_t)blockIdx.x * ROWS_A_BLOCK + (threadIdx.x >> 6) : blockIdx.x, step = (int64_t)gridDim.x * (WAVES == 1 ? ROWS_A_BLOCK : 1);
+    const int64_t first = WAVES == 1 ? (int64_t)blockIdx.x * ROWS_A_BLOCK + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x, step = (int64_t)gridDim.x * (WAVES == 1 ? ROWS_A_BLOCK : 1);
     const int per_row = (n.width + KEPT_GROUP - 1) / KEPT_GROUP;
-    float w[CH][4], dw[CH][4], db[CH][4];
-    if (weight) span.load(weight, w);
+    float dw[CH][4], db[CH][4];
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            dw[c][e] = db[c][e] = 0.f;
-            if (!weight) w[c][e] = 1.f;
-        }
+        for (int e = 0; e < 4; ++e) dw[c][e] = db[c][e] = 0.f;
     for (int64_t row = first; row < n.rows; row += step) {
         const int64_t at = row * n.width;
         float s[CH][4], g[CH][4];
         if constexpr (sizeof(TS) == 1) {
+            auto code_row = (__attribute__((address_space(1))) const int8_t*)(sum + at);
+            auto unit_row = (__attribute__((address_space(1))) const float*)(units + row * per_row);
+            asm("" : "+s"(code_row), "+s"(unit_row));
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int group = min(span.column(c) / KEPT_GROUP, per_row - 1);
-                load_codes(sum + at + span.column(c), span.count(c), units[row * per_row + group], s[c]);
+                const uint32_t group = min(span.column(c) / KEPT_GROUP, per_row - 1);
+                load_codes((const int8_t*)(code_row + (uint32_t)(span.thread * 4) + c * span.LANES * 4), span.count(c), unit_row[group], s[c]);
             }
         } else {
             span.load(sum + at, s);
         }
         span.load(dy + at, g);
         const float r = span.center(n, s, room);
+        float w[CH][4];                                             // (from the first cache, row by row: there are no registers for it)
+        if (weight) span.load(weight, w);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[c][e] = weight ? w[c][e] : 1.f;
         float c1 = 0.f, c2 = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
@@ -187,7 +204,8 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
         }
     }
     if (!partial) return;
-    float* const out = partial + (int64_t)blockIdx.x * 2 * n.width;
+    const int pitch = pitch_of(n.width);
+    float* const out = partial + (int64_t)blockIdx.x * 2 * pitch;
     auto write = [&](const float (&v)[CH][4], float* to) __attribute__((always_inline)) {
         if constexpr (WAVES == 1) {
             const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -210,27 +228,34 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
         }
     };
     write(dw, out);
-    write(db, out + n.width);
+    write(db, out + pitch);
 }
 
-// rows of the partial sums added: workgroup (eight columns, which of the two), 32 rows at a time
-__global__ __launch_bounds__(256) void k_layer_norm_sums(const float* __restrict__ partial, int width, int rows, float* __restrict__ dweight, float* __restrict__ dbias) {
-    __shared__ float part[32][8];
+// rows of the partial sums added: workgroup (sixteen columns, which of the two), 128 rows at a time
+__global__ __launch_bounds__(512) void k_layer_norm_sums(const float* __restrict__ partial, int width, int rows, float* __restrict__ dweight, float* __restrict__ dbias) {
+    __shared__ float part[8][16];
     float* const out = blockIdx.y ? dbias : dweight;
     if (!out) return;
-    const int c = threadIdx.x & 7, g = threadIdx.x >> 3, col = blockIdx.x * 8 + c;
-    float s = 0.f;
-    if (col < width)
-#pragma unroll 8
-        for (int r = g; r < rows; r += 32) s += partial[((int64_t)r * 2 + blockIdx.y) * width + col];
-    part[g][c] = s;
-    __syncthreads();
-    if (g == 0 && col < width) {
-        s = 0.f;
+    const int pitch = pitch_of(width), q = threadIdx.x & 3, g = threadIdx.x >> 2, col = blockIdx.x * 16 + 4 * q;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 6
+    for (int r = g; r < rows; r += 128) {
+        float x[4];
+        load_columns(partial + ((int64_t)r * 2 + blockIdx.y) * pitch + col, width - col, x);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) s += part[i][c];
-        out[col] = s;
+        for (int e = 0; e < 4; ++e) s[e] += x[e];
     }
+    // over the sixteen rows of a wavefront, then the wavefronts
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int d = 4; d < 64; d *= 2) s[e] += __shfl_xor(s[e], d);
+        if ((threadIdx.x & 63) < 4) part[threadIdx.x >> 6][4 * q + e] = s[e];
+    }
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c < 16 && blockIdx.x * 16 + c < width)
+        out[blockIdx.x * 16 + c] = ((part[0][c] + part[1][c]) + (part[2][c] + part[3][c])) + ((part[4][c] + part[5][c]) + (part[6][c] + part[7][c]));
 }
 
 int check_shape(const mst_norm_shape* s) {
@@ -263,13 +288,11 @@ void with_span(int width, F&& f) {
         default: break;
     }
     if (width <= 4096) return call(c4, c4, c2);
-    if (width <= 6144) return call(c6, c4, c2);
-    if (width <= 8192) return call(c8, c4, c2);
+    if (width <= 8192) return call(c4, c8, c2);
     if (width <= 12288) return call(c6, c8, c2);
     call(c8, c8, c2);
 }
-int rows_a_block(int width) { return width <= 2048 ? ROWS_A_BLOCK : 1; }
-unsigned blocks_of(const mst_norm_shape* s, int most) { return (unsigned)std::min<int64_t>(cdiv(s->rows, rows_a_block(s->width)), most); }
+unsigned blocks_of(const mst_norm_shape* s, int rows_a_block, int most) { return (unsigned)std::min<int64_t>(cdiv(s->rows, s->width <= 2048 ? rows_a_block : 1), most); }
 
 // f(numbers of the types)
 template <typename F>
@@ -296,7 +319,7 @@ extern "C" int mst_layer_norm_fwd(const mst_norm_shape* s, const void* x, const 
                 using TX = decltype(tx);
                 using TY = decltype(ty);
                 constexpr int WAVES = decltype(waves)::value;
-                k_layer_norm<decltype(ch)::value, WAVES, decltype(ends)::value, TX, TY><<<blocks_of(s, 1 << 20), 64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES), 0, static_cast<hipStream_t>(stream)>>>(
+                k_layer_norm<decltype(ch)::value, WAVES, decltype(ends)::value, TX, TY><<<blocks_of(s, ROWS_A_BLOCK, 1 << 20), 64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES), 0, static_cast<hipStream_t>(stream)>>>(
                     n, static_cast<const TX*>(x), static_cast<const TX*>(residual), weight, bias, static_cast<TX*>(sum), static_cast<TY*>(y),
                     kept ? kept->codes_dev : nullptr, kept ? kept->units_dev : nullptr);
             });
@@ -309,7 +332,7 @@ extern "C" int mst_layer_norm_fwd(const mst_norm_shape* s, const void* x, const 
 extern "C" size_t mst_layer_norm_workspace_bytes(const mst_norm_shape* s) {
     using namespace mst;
     if (check_shape(s)) return 0;
-    return align_up(std::max<size_t>(1, blocks_of(s, BWD_BLOCKS)) * 2 * s->width * sizeof(float));
+    return align_up(std::max<size_t>(1, blocks_of(s, ROWS_A_BLOCK, BWD_BLOCKS)) * 2 * pitch_of(s->width) * sizeof(float));
 }
 
 extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, const mst_checkpoint8* kept, const float* weight, const float* bias, const void* dy,
@@ -325,7 +348,7 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
     }
     if (ws_bytes < mst_layer_norm_workspace_bytes(s)) return MST_ERR_WORKSPACE;
     const NormRows n = {s->rows, s->width, s->eps, 1.f / (float)s->width};
-    const unsigned blocks = blocks_of(s, BWD_BLOCKS);
+    const unsigned blocks = blocks_of(s, ROWS_A_BLOCK, BWD_BLOCKS);
     float* const partial = static_cast<float*>(ws);
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto launch = [&](const auto* from, const float* units, auto tx) {
@@ -353,7 +376,7 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
         MST_LAUNCH_CHECK();
     }
     if (dweight || dbias) {               // (no rows: zeros)
-        k_layer_norm_sums<<<dim3((unsigned)cdiv(s->width, 8), 2), 256, 0, st>>>(partial, s->width, (int)blocks, dweight, dbias);
+        k_layer_norm_sums<<<dim3((unsigned)cdiv(s->width, 16), 2), 512, 0, st>>>(partial, s->width, (int)blocks, dweight, dbias);
         MST_LAUNCH_CHECK();
     }
     return MST_OK;

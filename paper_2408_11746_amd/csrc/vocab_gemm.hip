@@ -553,22 +553,34 @@ __global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, cons
     floatx4 acc[TT];
 #pragma unroll
     for (int i = 0; i < TT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const int whole = W & ~31;
-    constexpr int U = sizeof(T) == 2 ? 8 : 4;                       // steps whose loads are on the way together
-    int k = 0;
-    for (; k + 32 * U <= whole; k += 32 * U) {
-        uint4 raw[U][sizeof(T) / 2];
+    // U steps' loads of the embedding are on the way while U others are worked on
+    constexpr int U = sizeof(T) == 2 ? 8 : 4, WORDS = sizeof(T) / 2;
+    uint4 raw[2][U][WORDS];
+    const int batches = W / (32 * U);
+    auto load = [&](uint4 (&to)[U][WORDS], int batch) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int q = 0; q < (int)sizeof(T) / 2; ++q) raw[u][q] = reinterpret_cast<const uint4*>(e + k + 32 * u)[q];
+            for (int q = 0; q < WORDS; ++q) to[u][q] = reinterpret_cast<const uint4*>(e + 32 * (batch * U + u))[q];
+    };
+    auto work = [&](const uint4 (&from)[U][WORDS], int batch) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const Parts<T> b(reinterpret_cast<const T*>(raw[u]), true);
+            const Parts<T> b(reinterpret_cast<const T*>(from[u]), true);
 #pragma unroll
-            for (int i = 0; i < TT; ++i) terms(b, Parts<T>(x[i] + k + 32 * u, true), acc[i]);
+            for (int i = 0; i < TT; ++i) terms(b, Parts<T>(x[i] + 32 * (batch * U + u), true), acc[i]);
         }
+    };
+    if (batches > 0) load(raw[0], 0);
+    int batch = 0;
+    for (; batch + 2 <= batches; batch += 2) {
+        load(raw[1], batch + 1);
+        work(raw[0], batch);
+        if (batch + 2 < batches) load(raw[0], batch + 2);
+        work(raw[1], batch + 1);
     }
+    if (batch < batches) work(raw[0], batch);
+    int k = 32 * U * batches;
     for (; k < W; k += 32) {                                        // (a last step may be short: W is a multiple of eight)
         const bool there = k + 8 * g < W;
         const Parts<T> b(e + k, there);

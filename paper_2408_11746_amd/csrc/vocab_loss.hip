@@ -155,15 +155,17 @@ __global__ __launch_bounds__(256) void k_vocab_parts(const T* __restrict__ E, in
     }
 }
 
-// sums of a row joined: 64 rows a workgroup, a sixteenth of the statistics a wavefront.  Rows are tokens (count and list null; `vocab` says which have a label), or
-// the packed ones.
-constexpr int JOIN_WAVES = 16;
-__global__ __launch_bounds__(64 * JOIN_WAVES) void k_vocab_join(const float2* __restrict__ stats, int64_t stride, int n, int tokens, const int* __restrict__ count,
-                                                                const int* __restrict__ list, const int* __restrict__ labels, int vocab, const float* __restrict__ at_label,
-                                                                float* __restrict__ loss, float* __restrict__ lse) {
-    __shared__ float2 part[JOIN_WAVES][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 64 + lane, rows = count ? *count : tokens;
-    if ((int)blockIdx.x * 64 >= rows) return;
+// sums of a row joined: ROWS rows a workgroup, a share of the statistics to each of its lanes of a row.  Rows are tokens (count and list null; `vocab` says which have a
+// label), or the packed ones.
+constexpr int JOIN_THREADS = 1024;
+template <int ROWS>
+__global__ __launch_bounds__(JOIN_THREADS) void k_vocab_join(const float2* __restrict__ stats, int64_t stride, int n, int tokens, const int* __restrict__ count,
+                                                             const int* __restrict__ list, const int* __restrict__ labels, int vocab, const float* __restrict__ at_label,
+                                                             float* __restrict__ loss, float* __restrict__ lse) {
+    constexpr int SHARES = JOIN_THREADS / ROWS;
+    __shared__ float2 part[SHARES][ROWS];
+    const int r = threadIdx.x % ROWS, share = threadIdx.x / ROWS, row = blockIdx.x * ROWS + r, rows = count ? *count : tokens;
+    if ((int)blockIdx.x * ROWS >= rows) return;
     float top = -INFINITY, sum = 0.f;
     auto add = [&](float2 x) __attribute__((always_inline)) {
         const float m = fmaxf(top, x.x), from = m == -INFINITY ? 0.f : m;
@@ -172,11 +174,17 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_vocab_join(const float2* __
     };
     if (row < rows)
 #pragma unroll 8
-        for (int i = wave; i < n; i += JOIN_WAVES) add(stats[(int64_t)i * stride + row]);
-    part[wave][lane] = make_float2(top, sum);
+        for (int i = share; i < n; i += SHARES) add(stats[(int64_t)i * stride + row]);
+    part[share][r] = make_float2(top, sum);
     __syncthreads();
-    if (wave || row >= rows) return;
-    for (int w = 1; w < JOIN_WAVES; ++w) add(part[w][lane]);
+    for (int half = SHARES / 2; half > 0; half /= 2) {
+        if (share < half) {
+            add(part[share + half][r]);
+            part[share][r] = make_float2(top, sum);
+        }
+        __syncthreads();
+    }
+    if (share || row >= rows) return;
     const float l = (top + log2f(sum)) * 0.69314718f;
     const int token = list ? list[row] : row;
     const bool has = !labels || (labels[token] >= 0 && labels[token] < vocab);
@@ -317,8 +325,9 @@ struct Run {
         return join(nullptr, plan.rows, loss, lse);
     }
     int join(const int* labels, int64_t stride, float* loss, float* lse) const {
-        k_vocab_join<<<(unsigned)cdiv(s.tokens, 64), 64 * JOIN_WAVES, 0, stream>>>(at<float2>(plan.stat), stride, plan.stats, s.tokens, labels ? nullptr : at<int>(plan.count),
-                                                                                  labels ? nullptr : at<int>(plan.list), labels, s.vocab, at<float>(plan.at_label), loss, lse);
+        const auto kernel = plan.few ? k_vocab_join<8> : k_vocab_join<64>;
+        kernel<<<(unsigned)cdiv(s.tokens, plan.few ? 8 : 64), JOIN_THREADS, 0, stream>>>(at<float2>(plan.stat), stride, plan.stats, s.tokens, labels ? nullptr : at<int>(plan.count),
+                                                                                        labels ? nullptr : at<int>(plan.list), labels, s.vocab, at<float>(plan.at_label), loss, lse);
         MST_LAUNCH_CHECK();
         return MST_OK;
     }
