@@ -646,7 +646,7 @@ int mst_layer_norm_fwd(const mst_norm_shape* shape, const void* x_dev, const voi
 
 /* Gradients from s, or from what was kept of it: exactly one of sum_dev and kept is given (the other NULL), and everything is formed from
  * its values.  dx = the gradient of y through the norm, plus ds_dev, the gradient that reaches s along the residual stream (NULL: none);
- * it is the gradient of x and of the residual, and may be ds_dev.  dweight_dev, dbias_dev fp32 [width] (NULL: not wanted).  y_dev takes y again
+ * it is the gradient of x and of the residual, and may be ds_dev or, of one type, dy_dev.  dweight_dev, dbias_dev fp32 [width] (NULL: not wanted).  y_dev takes y again
  * (NULL: not wanted; bias_dev is used for that alone).  Nothing else has to be kept from the forward call.
  * Workspace: mst_layer_norm_workspace_bytes, 0 on invalid arguments. */
 int mst_layer_norm_bwd(const mst_norm_shape* shape, const void* sum_dev, const mst_checkpoint8* kept, const float* weight_dev,

@@ -561,6 +561,7 @@ def _check_lengths(t, batch):
         raise ValueError("lengths are int32, one behind the other, one for each of %d sequences" % batch)
 
 
+@functools.lru_cache(maxsize=None)
 def _torch_type(number):
     import torch
     return {MST_F32: torch.float32, MST_BF16: torch.bfloat16}.get(number)
@@ -663,74 +664,93 @@ def mst_block_attention_decode(shape: BlockAttentionShape, q, k, v, blocks, o, l
 
 # ------------------------------------------------------------------ norm, activation, checkpoints, loss
 
-_F32 = _INT8 = _INT32 = _BF16 = _FLOATS = None
-
-
-def _types():
-    global _F32, _INT8, _INT32, _BF16, _FLOATS
-    import torch
-    _INT8, _INT32, _BF16, _F32 = torch.int8, torch.int32, torch.bfloat16, torch.float32
-    _FLOATS = (_F32, _BF16)
-
-
-def _dense(t, dtype, numbers):
-    """Address of a tensor of the type, with so many numbers one behind the other on the device that the call runs on; an address as it is;
-    0 for None.  (`dtype` a number of mst_dtype, or a torch type; one that is unknown is the library's to refuse.)"""
-    if t is None or type(t) is int:
-        return t or 0
-    if _FLOATS is None:
-        _types()
-    want = dtype if not isinstance(dtype, int) else _FLOATS[dtype] if 0 <= dtype < 2 else t.dtype
-    if t.dtype is not want or t.numel() < numbers or not t.is_contiguous():
+def _dense(t, dtype, numbers, device):
+    """Address of a tensor of the type (None: the library refuses the shape), with so many numbers one behind the other on the device that the call runs on; an address
+    as it is; 0 for None.  (Small calls are bound by the host: 0.4 us a tensor.)"""
+    try:
+        if t.dtype is dtype and t.numel() >= numbers and t.is_contiguous() and t.get_device() == device:
+            return t.data_ptr()
+    except AttributeError:
+        if t is None:
+            return 0
+        if isinstance(t, int):
+            return t
+        raise
+    if (t.dtype is not dtype and dtype is not None) or t.numel() < numbers or not t.is_contiguous():
         raise ValueError("a tensor of %s, %s%s where the call takes %d numbers of %s, one behind the other"
-                         % (t.dtype, tuple(t.shape), "" if t.is_contiguous() else " with strides %s" % (t.stride(),), numbers, want))
-    if t.get_device() != _device():
+                         % (t.dtype, tuple(t.shape), "" if t.is_contiguous() else " with strides %s" % (t.stride(),), numbers, dtype))
+    if t.get_device() != device:
         raise ValueError("a tensor on %s where the call runs on the current GPU" % t.device)
     return t.data_ptr()
 
 
+_device_function = None
+
+
 def _device() -> int:
     """the calling thread's current GPU, -2 without one"""
+    global _device_function
+    if _device_function is None:
+        import torch
+        if not torch.cuda.is_available():
+            return -2
+        torch.cuda.current_stream()                  # (initialises the device)
+        _device_function = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device_function()
+
+
+@functools.lru_cache(maxsize=None)
+def _small_types():
     import torch
-    if not torch.cuda.is_available():
-        return -2
-    global _device
-    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    torch.cuda.current_stream()                      # (initialises the device)
-    return _device()
+    return torch.float32, torch.int8, torch.int32
 
 
-def _kept(kept, rows, width):
+def _kept(kept, rows, width, device):
     """The argument for a checkpoint of rows x width values"""
     if kept is None:
         return None
-    _dense(kept.codes, _INT8 or _type_of("int8"), rows * width)
-    _dense(kept.units, MST_F32, rows * -(-width // 128) if width > 0 else 0)
+    f32, int8, _ = _small_types()
+    _dense(kept.codes, int8, rows * width, device)
+    _dense(kept.units, f32, rows * -(-width // 128) if width > 0 else 0, device)
     return kept._ref
 
 
-def _type_of(name):
-    _types()
-    import torch
-    return getattr(torch, name)
+@functools.lru_cache(maxsize=256)
+def _norm_expected(shape: bytes):
+    s = LayerNormShape.from_buffer_copy(shape)
+    return s.rows, s.width, s.rows * s.width, _torch_type(s.in_type), _torch_type(s.out_type), _torch_type(s.grad_type), _small_types()[0]
+
+
+@functools.lru_cache(maxsize=256)
+def _gelu_expected(shape: bytes):
+    s = GeluShape.from_buffer_copy(shape)
+    return (s.rows, s.width, s.rows * s.width) + tuple(_torch_type(t) for t in (s.in_type, s.out_type, s.grad_type, s.in_grad_type))
+
+
+@functools.lru_cache(maxsize=256)
+def _loss_expected(shape: bytes):
+    s = VocabLossShape.from_buffer_copy(shape)
+    return (s.tokens, s.tokens * s.width, s.vocab * s.width, _torch_type(s.type)) + _small_types()
 
 
 def mst_checkpoint_write(rows: int, width: int, x, type: int, kept: Checkpoint8, stream=None):
+    dev = _device()
     _check("mst_checkpoint_write",
-           lib().mst_checkpoint_write(rows, width, _dense(x, type, rows * width), type, _kept(kept, rows, width), _stream(stream)))
+           lib().mst_checkpoint_write(rows, width, _dense(x, _torch_type(type), rows * width, dev), type, _kept(kept, rows, width, dev), _stream(stream)))
 
 
 def mst_checkpoint_read(rows: int, width: int, kept: Checkpoint8, type: int, x, stream=None):
+    dev = _device()
     _check("mst_checkpoint_read",
-           lib().mst_checkpoint_read(rows, width, _kept(kept, rows, width), type, _dense(x, type, rows * width), _stream(stream)))
+           lib().mst_checkpoint_read(rows, width, _kept(kept, rows, width, dev), type, _dense(x, _torch_type(type), rows * width, dev), _stream(stream)))
 
 
 def mst_layer_norm_fwd(shape: LayerNormShape, x, residual, weight, bias, sum, y, kept: Optional[Checkpoint8] = None, stream=None):
-    rows, width, t = shape.rows, shape.width, shape.in_type
-    n = rows * width
+    rows, width, n, tx, ty, _, f32 = _norm_expected(bytes(shape))
+    dev = _device()
     _check("mst_layer_norm_fwd",
-           lib().mst_layer_norm_fwd(C.byref(shape), _dense(x, t, n), _dense(residual, t, n), _dense(weight, MST_F32, width), _dense(bias, MST_F32, width),
-                                    _dense(sum, t, n), _dense(y, shape.out_type, n), _kept(kept, rows, width), _stream(stream)))
+           lib().mst_layer_norm_fwd(C.byref(shape), _dense(x, tx, n, dev), _dense(residual, tx, n, dev), _dense(weight, f32, width, dev), _dense(bias, f32, width, dev),
+                                    _dense(sum, tx, n, dev), _dense(y, ty, n, dev), _kept(kept, rows, width, dev), _stream(stream)))
 
 
 def mst_layer_norm_workspace_bytes(shape: LayerNormShape) -> int:
@@ -738,25 +758,26 @@ def mst_layer_norm_workspace_bytes(shape: LayerNormShape) -> int:
 
 
 def mst_layer_norm_bwd(shape: LayerNormShape, sum, kept: Optional[Checkpoint8], weight, bias, dy, ds, dx, dweight, dbias, y, ws, stream=None):
-    rows, width, t = shape.rows, shape.width, shape.in_type
-    n = rows * width
+    rows, width, n, tx, ty, tg, f32 = _norm_expected(bytes(shape))
+    dev = _device()
     _check("mst_layer_norm_bwd",
-           lib().mst_layer_norm_bwd(C.byref(shape), _dense(sum, t, n), _kept(kept, rows, width), _dense(weight, MST_F32, width), _dense(bias, MST_F32, width),
-                                    _dense(dy, shape.grad_type, n), _dense(ds, t, n), _dense(dx, t, n), _dense(dweight, MST_F32, width),
-                                    _dense(dbias, MST_F32, width), _dense(y, shape.out_type, n), _ptr(ws), ws.numel(), _stream(stream)))
+           lib().mst_layer_norm_bwd(C.byref(shape), _dense(sum, tx, n, dev), _kept(kept, rows, width, dev), _dense(weight, f32, width, dev), _dense(bias, f32, width, dev),
+                                    _dense(dy, tg, n, dev), _dense(ds, tx, n, dev), _dense(dx, tx, n, dev), _dense(dweight, f32, width, dev),
+                                    _dense(dbias, f32, width, dev), _dense(y, ty, n, dev), _ptr(ws), ws.numel(), _stream(stream)))
 
 
 def mst_gelu_fwd(shape: GeluShape, x, y, kept: Optional[Checkpoint8] = None, stream=None):
-    n = shape.rows * shape.width
-    _check("mst_gelu_fwd",
-           lib().mst_gelu_fwd(C.byref(shape), _dense(x, shape.in_type, n), _dense(y, shape.out_type, n), _kept(kept, shape.rows, shape.width), _stream(stream)))
+    rows, width, n, tx, ty, _, _ = _gelu_expected(bytes(shape))
+    dev = _device()
+    _check("mst_gelu_fwd", lib().mst_gelu_fwd(C.byref(shape), _dense(x, tx, n, dev), _dense(y, ty, n, dev), _kept(kept, rows, width, dev), _stream(stream)))
 
 
 def mst_gelu_bwd(shape: GeluShape, x, kept: Optional[Checkpoint8], dy, dx, y=None, stream=None):
-    n = shape.rows * shape.width
+    rows, width, n, tx, ty, tg, td = _gelu_expected(bytes(shape))
+    dev = _device()
     _check("mst_gelu_bwd",
-           lib().mst_gelu_bwd(C.byref(shape), _dense(x, shape.in_type, n), _kept(kept, shape.rows, shape.width), _dense(dy, shape.grad_type, n),
-                              _dense(dx, shape.in_grad_type, n), _dense(y, shape.out_type, n), _stream(stream)))
+           lib().mst_gelu_bwd(C.byref(shape), _dense(x, tx, n, dev), _kept(kept, rows, width, dev), _dense(dy, tg, n, dev), _dense(dx, td, n, dev), _dense(y, ty, n, dev),
+                              _stream(stream)))
 
 
 def mst_vocab_loss_workspace_bytes(shape: VocabLossShape, backward: bool) -> int:
@@ -764,15 +785,16 @@ def mst_vocab_loss_workspace_bytes(shape: VocabLossShape, backward: bool) -> int
 
 
 def mst_vocab_loss_fwd(shape: VocabLossShape, h, E, labels, loss, lse, ws, stream=None):
-    T, W, t = shape.tokens, shape.width, shape.type
+    T, nh, nE, t, f32, _, int32 = _loss_expected(bytes(shape))
+    dev = _device()
     _check("mst_vocab_loss_fwd",
-           lib().mst_vocab_loss_fwd(C.byref(shape), _dense(h, t, T * W), _dense(E, t, shape.vocab * W), _dense(labels, _INT32 or _type_of("int32"), T),
-                                    _dense(loss, MST_F32, T), _dense(lse, MST_F32, T), _ptr(ws), ws.numel(), _stream(stream)))
+           lib().mst_vocab_loss_fwd(C.byref(shape), _dense(h, t, nh, dev), _dense(E, t, nE, dev), _dense(labels, int32, T, dev), _dense(loss, f32, T, dev),
+                                    _dense(lse, f32, T, dev), _ptr(ws), ws.numel(), _stream(stream)))
 
 
 def mst_vocab_loss_bwd(shape: VocabLossShape, h, E, labels, lse, dloss, dh, dE, ws, stream=None):
-    T, W, t = shape.tokens, shape.width, shape.type
+    T, nh, nE, t, f32, _, int32 = _loss_expected(bytes(shape))
+    dev = _device()
     _check("mst_vocab_loss_bwd",
-           lib().mst_vocab_loss_bwd(C.byref(shape), _dense(h, t, T * W), _dense(E, t, shape.vocab * W), _dense(labels, _INT32 or _type_of("int32"), T),
-                                    _dense(lse, MST_F32, T), _dense(dloss, MST_F32, T), _dense(dh, t, T * W), _dense(dE, t, shape.vocab * W),
-                                    _ptr(ws), ws.numel(), _stream(stream)))
+           lib().mst_vocab_loss_bwd(C.byref(shape), _dense(h, t, nh, dev), _dense(E, t, nE, dev), _dense(labels, int32, T, dev), _dense(lse, f32, T, dev),
+                                    _dense(dloss, f32, T, dev), _dense(dh, t, nh, dev), _dense(dE, t, nE, dev), _ptr(ws), ws.numel(), _stream(stream)))

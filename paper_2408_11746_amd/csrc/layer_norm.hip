@@ -131,11 +131,11 @@ __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) void k_la
 
 // wavefronts of a SIMD that the registers have to suffice for
 constexpr int bwd_waves(int ch, int waves) { return ch <= 3 ? 4 : waves == 1 && ch <= 5 ? 3 : 2; }
-// TS int8_t: from what was kept
+// TS int8_t: from what was kept.  (dx may be dy or ds: a row has been read before it is written.)
 template <int CH, int WAVES, int ENDS, typename TS, typename TX, typename TG>
 __global__ __launch_bounds__(64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES)) __attribute__((amdgpu_waves_per_eu(bwd_waves(CH, WAVES)))) void k_layer_norm_bwd(NormRows n, const TS* __restrict__ sum, const float* __restrict__ units,
                                                                                              const float* __restrict__ weight, const float* __restrict__ bias,
-                                                                                             const TG* __restrict__ dy, const TX* ds, TX* dx, void* __restrict__ y, int y_f32,
+                                                                                             const TG* dy, const TX* ds, TX* dx, void* __restrict__ y, int y_f32,
                                                                                              float* __restrict__ partial) {
     constexpr int SHARED = WAVES == 1 ? ROWS_A_BLOCK : 1;
     __shared__ float room[WAVES];
@@ -346,6 +346,7 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
         if (kept)
             if (int e = check_kept(kept)) return e;
     }
+    if (dx == dy && dy && s->grad_type != s->in_type) return MST_ERR_ARG;
     if (ws_bytes < mst_layer_norm_workspace_bytes(s)) return MST_ERR_WORKSPACE;
     const NormRows n = {s->rows, s->width, s->eps, 1.f / (float)s->width};
     const unsigned blocks = blocks_of(s, ROWS_A_BLOCK, BWD_BLOCKS);

@@ -81,6 +81,7 @@ def test_norm_refuses_arguments():
             assert _code(lambda: _norm_bwd(s, **{name: bad})) == -1
     for name in ("total", "w", "b", "ds", "dw", "db", "y"):
         assert _code(lambda: _norm_bwd(s, **{name: FAKE + 8})) == -1
+    assert _code(lambda: _norm_bwd(_norm(grad_type=1))) == -1         # in place of dy, of another type
     assert _code(lambda: _norm_bwd(s, total=None)) == -1            # neither the sum nor what was kept of it
     assert _code(lambda: _norm_bwd(s, kept=KEPT)) == -1             # both
     need = mst.mst_layer_norm_workspace_bytes(s)
