@@ -298,9 +298,8 @@ struct LargeLoads {
             }
         }
     }
-    __device__ __forceinline__ void aim_pair(const VocabOperand& o, int first, int part, int t) {
-        const uint16_t* const from = o.p + part * o.plane;
-        base = reinterpret_cast<const char*>(ALONG ? from + (int64_t)first * o.ld + t * L_PAIR : from + (int64_t)t * L_PAIR * o.ld + first);
+    __device__ __forceinline__ void aim_pair(const VocabOperand& o, int first, int t) {
+        base = reinterpret_cast<const char*>(ALONG ? o.p + (int64_t)first * o.ld + t * L_PAIR : o.p + (int64_t)t * L_PAIR * o.ld + first);
     }
     // to: the wavefront's 8 KB of the stage (a multiple of that) ^ 1024 turn; the j-th load is of piece j ^ turn
     __device__ __forceinline__ void piece(int j, uint32_t to) const { load_to_lds(base, v[j], to ^ 1024u * j); }
@@ -332,28 +331,43 @@ struct LargeReads {
     }
 };
 
+// Units are (tile, range of the contraction), range by range.  XCD x takes a contiguous share of them, its workgroups in turn, so that what runs there at a time
+// reads the same operands.
+struct Unit { int m0, n0, split, kb, ke; };      // (range in pairs of steps)
+struct Units {
+    int m_rows, gm, gn, ntiles, k_all, splits, next, end, each;
+    __device__ __forceinline__ Units(const VocabProduct& p) {
+        m_rows = p.m_count ? *p.m_count : p.m;
+        k_all = ((p.k_count ? *p.k_count : p.k) + L_PAIR - 1) / L_PAIR;
+        gm = (m_rows + VT - 1) / VT;
+        gn = (p.n + VT - 1) / VT;
+        ntiles = gm * gn;
+        splits = p.splits;
+        const int units = ntiles * splits, Q = (units + 7) >> 3;
+        next = (blockIdx.x & 7) * Q + (blockIdx.x >> 3);
+        end = min(((int)(blockIdx.x & 7) + 1) * Q, units);
+        each = gridDim.x >> 3;
+    }
+    __device__ __forceinline__ Unit decode(int u) const {
+        const int split = u / ntiles;
+        int mi, ni;
+        tile_coords(u - split * ntiles, gm, gn, mi, ni);
+        auto uniform = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+        return Unit{uniform(mi * VT), uniform(ni * VT), uniform(split), uniform((int)((int64_t)split * k_all / splits)), uniform((int)((int64_t)(split + 1) * k_all / splits))};
+    }
+};
+
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m_rows = p.m_count ? *p.m_count : p.m, k_rows = p.k_count ? *p.k_count : p.k;
     const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
-    // Units are (tile, range of the contraction), range by range.  XCD x takes a contiguous share of them, its workgroups in turn, so that what runs there
-    // at a time reads the same operands.
-    const int gm = (m_rows + VT - 1) / VT, gn = (p.n + VT - 1) / VT, ntiles = gm * gn, units = ntiles * p.splits, Q = (units + 7) >> 3;
-    const int end = min(((int)(blockIdx.x & 7) + 1) * Q, units), each = gridDim.x >> 3;
-    int unit = (blockIdx.x & 7) * Q + (blockIdx.x >> 3);
+    const Units units(p);
+    const int m_rows = units.m_rows, k_all = units.k_all, end = units.end, each = units.each;
+    int unit = units.next;
     if (unit >= end) return;
-    const int k_all = (k_rows + L_PAIR - 1) / L_PAIR, first_term = p.planes == 1 ? 5 : 0;
-    struct Unit { int m0, n0, split, kb, ke; };
-    auto decode = [&](int u) __attribute__((always_inline)) {
-        const int split = u / ntiles;
-        int mi, ni;
-        tile_coords(u - split * ntiles, gm, gn, mi, ni);
-        auto uniform = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
-        return Unit{uniform(mi * VT), uniform(ni * VT), uniform(split), uniform((int)((int64_t)split * k_all / p.splits)), uniform((int)((int64_t)(split + 1) * k_all / p.splits))};
-    };
+    auto decode = [&](int u) __attribute__((always_inline)) { return units.decode(u); };
     floatx4 acc[8][8];
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -377,10 +391,10 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     // The loads run two pairs ahead of the products, into the next unit where the present one ends, so that only the first has to wait for them
     LargeLoads<A_ALONG> la;
     LargeLoads<B_ALONG> lb;
-    // An operand that is read across ends inside its last pair only where it is the caller's own embedding (one part): rows past its end are its last
+    // An operand that is read across ends inside its last pair only where it is the caller's own embedding: rows past its end are its last
     const int tail = B_ALONG ? L_PAIR : p.b.rows - (k_all - 1) * L_PAIR;
     Unit ahead;
-    int ahead_unit = unit, at_t, at_term;
+    int ahead_unit = unit, at_t;
     bool enter = true;
     auto aim = [&]() __attribute__((always_inline)) {
         if (enter) {
@@ -388,17 +402,13 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
             la.aim_rows(p.a, ahead.m0, wave, lane, L_PAIR, turn(ahead.n0));
             lb.aim_rows(p.b, ahead.n0, wave, lane, L_PAIR, turn(ahead.m0));
             at_t = ahead.kb;
-            at_term = first_term;
         }
         if (!B_ALONG && at_t == k_all - 1 && tail < L_PAIR) lb.aim_rows(p.b, ahead.n0, wave, lane, tail, turn(ahead.m0));
-        la.aim_pair(p.a, ahead.m0, PART_A[at_term], at_t);
-        lb.aim_pair(p.b, ahead.n0, PART_B[at_term], at_t);
+        la.aim_pair(p.a, ahead.m0, at_t);
+        lb.aim_pair(p.b, ahead.n0, at_t);
         enter = false;
         if (at_t + 1 < ahead.ke) {
             ++at_t;
-        } else if (at_term < 5) {
-            ++at_term;
-            at_t = ahead.kb;
         } else if (ahead_unit + each < end) {
             ahead_unit += each;
             enter = true;
@@ -470,7 +480,7 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
     bool stored = false;
     for (; unit < end; unit += each) {
         const Unit x = decode(unit);
-        const int pairs = (x.ke - x.kb) * (6 - first_term);
+        const int pairs = x.ke - x.kb;
         if constexpr (E == SUMS) {
             clear();
             begin(e, acc, x.m0 + wm, x.n0 + wn, x.split, lane);
@@ -491,6 +501,231 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
             wait_loads<8>();
             lds_barrier();
             second();
+        }
+        // the last product is 18 wait states from its result
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+        finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
+}
+
+// ---- the same tiles for numbers of three parts: six products of each step of 32 indices
+// The parts of a step are in LDS once, 16 KB each, and a part stays in registers for the products that follow one another with it: seven reads of operands instead of
+// twelve, and half of the bytes from memory that six separate products would take, which bound them (1378 tokens, width 648, vocabulary 32003: statistics 317 us).
+//   product   a2 b0   a1 b0   a0 b0   a0 b2   a0 b1   a1 b1        register set of a, of b:  0 Q   1 Q   0 Q   0 1-Q   0 Q   1 Q
+//   reads     a1      a0      b2      b1      a1      b0, a2 of the next step
+//   loads     b0      a2      a1      a0      b2      b1  of the next step
+// Ten stages: a part is loaded six products before the one that has its number in this order, and waited for every other product.
+constexpr int Q_STAGE = VT * VK * 2, Q_STAGES = 10;
+constexpr unsigned Q_LDS = Q_STAGES * Q_STAGE;
+
+template <bool ALONG>
+struct PartLoads {
+    uint32_t v[4];
+    const char* base;                    // of part 0 of the step
+    __device__ __forceinline__ void aim_rows(const VocabOperand& o, int first, int wave, int lane, int turn) {
+        const uint32_t row_bytes = 2u * (uint32_t)o.ld;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int piece = 4 * wave + (j ^ turn);
+            if constexpr (ALONG) {
+                const int rho = lane >> 2, row = 16 * piece + (((rho & 3) << 2) | (rho >> 2)), u = ((lane & 3) ^ (rho >> 2)) & 3;
+                v[j] = (uint32_t)min(row, o.rows - 1 - first) * row_bytes + 16u * u;
+            } else {
+                const int k = 2 * piece + (lane >> 5), col = 16 * (((lane & 31) >> 1) ^ across_swizzle(k)) + 8 * (lane & 1);
+                v[j] = (uint32_t)k * row_bytes + 2u * (uint32_t)min((int64_t)col, o.ld - 8 - first);
+            }
+        }
+    }
+    __device__ __forceinline__ void aim_step(const VocabOperand& o, int first, int t) {
+        base = reinterpret_cast<const char*>(ALONG ? o.p + (int64_t)first * o.ld + t * VK : o.p + (int64_t)t * VK * o.ld + first);
+    }
+    // to: the wavefront's 4 KB of the stage ^ 1024 turn
+    __device__ __forceinline__ void piece(int j, int64_t part_bytes, uint32_t to) const { load_to_lds(base + part_bytes, v[j], to ^ 1024u * j); }
+};
+template <bool ALONG>
+struct PartReads {
+    uint32_t at[ALONG ? 1 : 8];
+    __device__ __forceinline__ PartReads(int first, int lane) {
+        if constexpr (ALONG) {
+            at[0] = along_unit(first + (lane & 15), lane >> 4);
+        } else {
+            const int k = 8 * (lane >> 4) + ((lane >> 2) & 3);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) at[i] = (uint32_t)(k * 512 + (((first / 16 + i) ^ across_swizzle(k)) << 5) + (lane & 3) * 8);
+        }
+    }
+    __device__ __forceinline__ void half(uint32_t stage, int i, int h, bf16x8& whole, shortx4 (&part)[2]) const {
+        if constexpr (ALONG) {
+            if (h == 0) whole = *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)(stage + at[0] + 1024u * i));
+        } else {
+            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)(stage + at[i] + 2048u * h));
+            if (h == 1) whole = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+template <bool A_ALONG, bool B_ALONG, Epilogue E>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
+    const Units units(p);
+    const int m_rows = units.m_rows, end = units.end, each = units.each;
+    int unit = units.next;
+    if (unit >= end) return;
+    floatx4 acc[8][8];
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    };
+    if (units.k_all == 0) {               // a batch without labels
+        clear();
+        for (; unit < end; unit += each) {
+            const Unit x = units.decode(unit);
+            finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
+        }
+        return;
+    }
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+
+    // The loads run a step ahead of the products, into the next unit where the present one ends.  (Every operand is in the workspace, padded to whole pairs of steps.)
+    PartLoads<A_ALONG> la;
+    PartLoads<B_ALONG> lb;
+    Unit ahead;
+    int ahead_unit = unit, at_t;
+    bool enter = true;
+    auto turn = [&](int first) __attribute__((always_inline)) { return first / VT & 3; };
+    auto aim = [&]() __attribute__((always_inline)) {
+        if (enter) {
+            ahead = units.decode(ahead_unit);
+            la.aim_rows(p.a, ahead.m0, wave, lane, turn(ahead.n0));
+            lb.aim_rows(p.b, ahead.n0, wave, lane, turn(ahead.m0));
+            at_t = 2 * ahead.kb;
+        }
+        la.aim_step(p.a, ahead.m0, at_t);
+        lb.aim_step(p.b, ahead.n0, at_t);
+        enter = false;
+        if (at_t + 1 < 2 * ahead.ke) {
+            ++at_t;
+        } else if (ahead_unit + each < end) {
+            ahead_unit += each;
+            enter = true;
+        }                                 // (behind the last step of all: that again, for nobody)
+    };
+    const int64_t plane_a = 2 * p.a.plane, plane_b = 2 * p.b.plane;
+    const uint32_t mine = 4096u * wave;
+    int base = 0;                                                   // stage of the present step's first part
+    auto stage = [&](int n) __attribute__((always_inline)) {        // of part n from there on
+        const int x = base + n;
+        return lds0 + (uint32_t)(x >= Q_STAGES ? x - Q_STAGES : x) * Q_STAGE;
+    };
+    // where the wavefront's loads of part n (of the next step: n + 6) go
+    auto to_a = [&](int n) __attribute__((always_inline)) { return (stage(n) + mine) ^ 1024 * turn(ahead.n0); };
+    auto to_b = [&](int n) __attribute__((always_inline)) { return (stage(n) + mine) ^ 1024 * turn(ahead.m0); };
+    const PartReads<A_ALONG> ra(wm, lane);
+    const PartReads<B_ALONG> rb(wn, lane);
+    bf16x8 a[2][8], b[2][8];
+    // products of sets AS and BS; what stage sa (sb) holds goes to set RA (RB; -1: nothing is read), part `part` of an operand to `to`
+    auto product = [&](auto as, auto bs, auto fresh, auto ra_set, uint32_t sa, auto rb_set, uint32_t sb, auto of_a, int part, uint32_t to) __attribute__((always_inline)) {
+        constexpr int AS = decltype(as)::value, BS = decltype(bs)::value, RA = decltype(ra_set)::value, RB = decltype(rb_set)::value;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            shortx4 pa[2], pb[2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (decltype(fresh)::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b[BS][j]), "v"(a[AS][i]));
+                else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b[BS][j]), "v"(a[AS][i]));
+                if constexpr (RB >= 0) {
+                    if (j == 0) rb.half(sb, i, 0, b[RB][i], pb);
+                    if (j == 1) rb.half(sb, i, 1, b[RB][i], pb);
+                }
+                if constexpr (RA >= 0) {
+                    if (j == 3) ra.half(sa, i, 0, a[RA][i], pa);
+                    if (j == 4) ra.half(sa, i, 1, a[RA][i], pa);
+                }
+                if (j == 6 && (i & 1)) {
+                    if constexpr (decltype(of_a)::value) la.piece(i >> 1, part * plane_a, to);
+                    else lb.piece(i >> 1, part * plane_b, to);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    constexpr std::integral_constant<int, -1> none;
+    constexpr std::integral_constant<int, 0> zero;
+    constexpr std::integral_constant<int, 1> one;
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    auto meet = [&](bool stored) __attribute__((always_inline)) {   // the parts of this product and the next are in LDS, and everyone is done with the last two
+        if (stores_behind(E) > 0 && stored) wait_loads<8 + stores_behind(E)>();
+        else wait_loads<8>();
+        lds_barrier();
+    };
+    auto step = [&](auto q, auto fresh, bool stored) __attribute__((always_inline)) {
+        constexpr std::integral_constant<int, decltype(q)::value> Q;
+        constexpr std::integral_constant<int, 1 - decltype(q)::value> R;
+        meet(stored);
+        aim();
+        product(zero, Q, fresh, one, stage(2), none, 0, no, 0, to_b(6));
+        product(one, Q, no, zero, stage(3), none, 0, yes, 2, to_a(7));
+        meet(false);
+        product(zero, Q, no, none, 0, R, stage(4), yes, 1, to_a(8));
+        product(zero, R, no, none, 0, Q, stage(5), yes, 0, to_a(9));
+        meet(false);
+        product(zero, Q, no, one, stage(2), none, 0, no, 2, to_b(10));
+        const uint32_t load = to_b(11);
+        base = base + 6 >= Q_STAGES ? base + 6 - Q_STAGES : base + 6;
+        product(one, Q, no, zero, stage(1), R, stage(0), no, 1, load);
+    };
+
+    aim();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lb.piece(j, 0, to_b(0));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) la.piece(j, 2 * plane_a, to_a(1));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) la.piece(j, plane_a, to_a(2));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) la.piece(j, 0, to_a(3));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lb.piece(j, 2 * plane_b, to_b(4));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lb.piece(j, plane_b, to_b(5));
+    wait_loads<16>();
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        shortx4 pa[2], pb[2];
+        rb.half(stage(0), i, 0, b[0][i], pb);
+        rb.half(stage(0), i, 1, b[0][i], pb);
+        ra.half(stage(1), i, 0, a[0][i], pa);
+        ra.half(stage(1), i, 1, a[0][i], pa);
+    }
+    bool stored = false;
+    for (; unit < end; unit += each) {
+        const Unit x = units.decode(unit);
+        const int pairs = x.ke - x.kb;
+        if constexpr (E == SUMS) {
+            clear();
+            begin(e, acc, x.m0 + wm, x.n0 + wn, x.split, lane);
+            step(zero, no, stored);
+        } else {
+            step(zero, yes, stored);
+        }
+        stored = true;
+        step(one, no, false);
+#pragma unroll 1
+        for (int d = 1; d < pairs; ++d) {
+            step(zero, no, false);
+            step(one, no, false);
         }
         // the last product is 18 wait states from its result
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -629,10 +864,22 @@ int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipSt
         const int64_t blocks = cdiv(p.m, SM) * cdiv(p.n, SM) * p.splits;
         k_vocab_small<A_ALONG, B_ALONG, E><<<(unsigned)blocks, 256, 0, s>>>(p, e);
     } else {
-        static uint64_t done = 0;
-        const auto kernel = k_vocab_large<A_ALONG, B_ALONG, E>;
-        if (int rc = allow_lds(reinterpret_cast<const void*>(kernel), (int)L_LDS, done)) return rc;
-        kernel<<<(unsigned)std::min<int64_t>(256, 8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8)), 256, L_LDS, s>>>(p, e);      // (one to a CU)
+        // (one to a CU)
+        const unsigned grid = (unsigned)std::min<int64_t>(256, 8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8));
+        auto run = [&](auto kernel, unsigned bytes, uint64_t& done) {
+            if (int rc = allow_lds(reinterpret_cast<const void*>(kernel), (int)bytes, done)) return rc;
+            kernel<<<grid, 256, bytes, s>>>(p, e);
+            return (int)MST_OK;
+        };
+        static uint64_t done[2] = {0, 0};
+        int rc = MST_ERR_ARG;
+        if constexpr (E != LOGIT_GRAD && E != OUT_BF16) {
+            if (p.planes > 1) rc = run(k_vocab_large_parts<A_ALONG, B_ALONG, E>, Q_LDS, done[1]);
+        }
+        if constexpr (E != LOGIT_GRAD_PARTS && E != OUT_F32) {
+            if (p.planes == 1) rc = run(k_vocab_large<A_ALONG, B_ALONG, E>, L_LDS, done[0]);
+        }
+        if (rc) return rc;
     }
     MST_LAUNCH_CHECK();
     return MST_OK;
