@@ -14,7 +14,7 @@
 namespace mst {
 namespace {
 
-constexpr int64_t PIECE_BYTES = int64_t(1) << 28;
+constexpr int64_t PIECE_BYTES = int64_t(1) << 29;
 
 // ---- which tokens have a label
 constexpr int ROWS_THREADS = 1024, ROWS_EACH = 8;

@@ -158,11 +158,11 @@ def test_loss_refuses_arguments():
 
 
 def test_workspaces_stay_bounded():
-    # pieces of the vocabulary of 256 MB, whatever its size; the sums for dh and the packed states beside them
+    # pieces of the vocabulary of 512 MB, whatever its size; the sums for dh and the packed states beside them
     for kind, size in ((1, 2), (0, 4)):
         for tokens, width, vocab in ((8192, 1280, 50257), (8192, 1280, 1 << 20), (65536, 1024, 50257)):
             n = mst.mst_vocab_loss_workspace_bytes(_loss(tokens=tokens, width=width, vocab=vocab, type=kind), True)
-            assert n < (1 << 28) + 64 * tokens * width + 8 * tokens * vocab / 128 + (1 << 24), (kind, tokens, n)
+            assert n < (1 << 29) + 64 * tokens * width + 8 * tokens * vocab / 128 + (1 << 24), (kind, tokens, n)
     # the forward of bfloat16 keeps 8 bytes a token and 128 columns
     n = mst.mst_vocab_loss_workspace_bytes(_loss(tokens=8192, width=1280, vocab=50257), False)
     assert n < 8192 * (50257 / 128 + 1) * 8 + 8192 * 1280 * 2 + (1 << 20)
