@@ -18,9 +18,6 @@ typedef __attribute__((address_space(3))) shortx4* lds_shortx4;
 
 constexpr float LOG2E = 1.44269504f;
 
-// parts of a term, the small ones first
-__device__ __constant__ const int8_t PART_A[6] = {0, 2, 1, 0, 1, 0}, PART_B[6] = {2, 0, 1, 1, 0, 0};
-
 // LDS position of unit u (eight k) of row m of an operand along: the sixteen rows of a read cover all banks
 __device__ __forceinline__ uint32_t along_unit(int m, int u) {
     const int rho = (m & ~15) | ((m & 3) << 2) | ((m >> 2) & 3);
@@ -28,9 +25,6 @@ __device__ __forceinline__ uint32_t along_unit(int m, int u) {
 }
 // The 32-byte units (16 columns) of row k of an operand across are kept at unit ^ swizzle(k): so do the eight rows of half a wavefront
 __device__ __forceinline__ int across_swizzle(int k) { return (k & 3) | ((k >> 1) & 4); }
-
-// ---- 128 x 128 tiles, four wavefronts of 64 x 64
-constexpr int SM = 128, S_OP = SM * 64;
 
 enum Epilogue { STATS, LOGIT_GRAD, LOGIT_GRAD_PARTS, SUMS, OUT_F32, OUT_BF16 };
 template <Epilogue E> struct EpilogueArgs;
@@ -46,11 +40,9 @@ template <> struct EpilogueArgs<OUT_BF16> { using type = VocabOutOf<bf16>; };
 // Results: acc[i][j][v] is row m0 + 16 i + lane % 16, column n0 + 16 j + 4 (lane / 16) + v of C; a wavefront's 16 I rows and 16 J columns.
 // Results go straight to memory: a store writes 32 or 64 bytes of sixteen rows, and those that fill a line follow one another.  (Through LDS, in whole lines, they
 // waited longer than they saved.)
-// Result v of a 16 x 16 product.  The large tiles' lie in accumulation registers and are read out where they are used (left to the compiler, most of them are read at
-// once, and other registers spill).
-template <bool LARGE>
+// Result v of a 16 x 16 product: it lies in accumulation registers and is read out where it is used (left to the compiler, most of them are read at once, and other
+// registers spill).
 __device__ __forceinline__ float result(const floatx4& acc, int v) {
-    if constexpr (!LARGE) return acc[v];
     float x;
     asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[v]));
     return x;
@@ -72,7 +64,7 @@ __device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProdu
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         auto z = [&](int j, int v) __attribute__((always_inline)) {
-            const float x = result<I == 8>(acc[i][j], v);
+            const float x = result(acc[i][j], v);
             return !ENDS || 16 * j + v < last ? x : -INFINITY;
         };
         if constexpr (MAXIMUM) {
@@ -126,7 +118,7 @@ __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabP
                 float x[4];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    x[v] = d[i] * exp2_fast(fmaf(result<I == 8>(acc[i][j], v), LOG2E, -base[i]));
+                    x[v] = d[i] * exp2_fast(fmaf(result(acc[i][j], v), LOG2E, -base[i]));
                     if (ENDS) x[v] = 16 * j + v < last ? x[v] : 0.f;
                     if (decltype(labels)::value && 16 * j + 4 * g + v == label[i]) x[v] = at_label[i];
                 }
@@ -187,7 +179,7 @@ __device__ __forceinline__ void finish(const VocabOutOf<T>& e, const VocabProduc
 #pragma unroll
             for (int j = 0; j < J; ++j)
                 if (!decltype(ends)::value || (m + 16 * i < m_rows && n + 16 * j < p.n))       // (p.n a multiple of eight)
-                    store4(row + 16 * j, u * result<I == 8>(acc[i][j], 0), u * result<I == 8>(acc[i][j], 1), u * result<I == 8>(acc[i][j], 2), u * result<I == 8>(acc[i][j], 3));
+                    store4(row + 16 * j, u * result(acc[i][j], 0), u * result(acc[i][j], 1), u * result(acc[i][j], 2), u * result(acc[i][j], 3));
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -197,75 +189,6 @@ __device__ __forceinline__ void finish(const VocabOutOf<T>& e, const VocabProduc
 
 // Of the stores of a unit's results, so many are issued whatever the unit holds (dz: 64 or more, as many as the counter of outstanding accesses can tell apart)
 constexpr int stores_behind(Epilogue E) { return E == LOGIT_GRAD || E == LOGIT_GRAD_PARTS ? 52 : 0; }
-
-template <bool A_ALONG, bool B_ALONG, Epilogue E>
-__global__ __launch_bounds__(256) void k_vocab_small(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
-    __shared__ __attribute__((aligned(16))) char lds[2 * S_OP];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m_rows = p.m_count ? *p.m_count : p.m, k_all = ((p.k_count ? *p.k_count : p.k) + VK - 1) / VK;
-    const int gm = (int)((m_rows + SM - 1) / SM), gn = (p.n + SM - 1) / SM, ntiles = gm * gn;
-    const int split = blockIdx.x % p.splits, tile = blockIdx.x / p.splits;
-    if (tile >= ntiles) return;
-    const int m0 = tile % gm * SM, n0 = tile / gm * SM;
-    const int per = (k_all + p.splits - 1) / p.splits, kb = min(split * per, k_all), ke = min(kb + per, k_all);
-    const uint32_t lds0 = lds_address(lds);
-    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-
-    auto load = [&](const VocabOperand& o, auto along, int part, int t, int first, uint32_t to) __attribute__((always_inline)) {
-        const uint16_t* const from = o.p + part * o.plane;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int piece = 2 * wave + j;                         // 1 KB
-            const uint16_t* at;
-            if constexpr (decltype(along)::value) {
-                const int rho = lane >> 2, row = first + 16 * piece + (((rho & 3) << 2) | (rho >> 2)), u = ((lane & 3) ^ (rho >> 2)) & 3;
-                at = from + (int64_t)min(row, o.rows - 1) * o.ld + t * VK + 8 * u;
-            } else {
-                const int k = 4 * piece + (lane >> 4), col = 16 * (((lane & 15) >> 1) ^ across_swizzle(k)) + 8 * (lane & 1);
-                at = from + (int64_t)min(t * VK + k, o.rows - 1) * o.ld + min((int64_t)first + col, o.ld - 8);
-            }
-            gather_to_lds(at, to + 1024u * piece);
-        }
-    };
-    auto read = [&](auto along, uint32_t op, int first) __attribute__((always_inline)) {
-        if constexpr (decltype(along)::value) {
-            return *reinterpret_cast<const bf16x8*>(lds + op + along_unit(first + (lane & 15), lane >> 4));
-        } else {
-            const int g = lane >> 4, x = (lane >> 2) & 3, k = 8 * g + x;
-            const uint32_t at = lds0 + op + (uint32_t)(k * SM * 2 + (((first >> 4) ^ across_swizzle(k)) << 5) + (lane & 3) * 8);
-            // (four rows further on: the same swizzle)
-            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)at);
-            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)(at + 4 * SM * 2));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-    };
-
-    floatx4 acc[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    begin(e, acc, m0 + wm, n0 + wn, split, lane);
-    for (int term = p.planes == 1 ? 5 : 0; term < 6; ++term)
-        for (int t = kb; t < ke; ++t) {
-            __syncthreads();
-            load(p.a, std::bool_constant<A_ALONG>{}, PART_A[term], t, m0, lds0);
-            load(p.b, std::bool_constant<B_ALONG>{}, PART_B[term], t, n0, lds0 + S_OP);
-            wait_loads<0>();
-            __syncthreads();
-            bf16x8 a[4], b[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = read(std::bool_constant<A_ALONG>{}, 0, wm + 16 * i);
-                b[i] = read(std::bool_constant<B_ALONG>{}, S_OP, wn + 16 * i);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
-        }
-    finish(e, p, acc, m0 + wm, n0 + wn, split, lane, m_rows);
-}
 
 // ---- 256 x 256 tiles, four wavefronts of 128 x 128, the sums in the accumulation half of the registers
 // A stage of LDS is 64 contraction indices of one operand, 32 KB, so that rows of memory are read in whole lines of 128 bytes; five of them, A and B in turn.
@@ -738,73 +661,64 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
 }
 
-// ---- few tokens: the embedding is read once, straight into registers, and that bounds it
-// A wavefront takes sixteen rows of the embedding and 16 TT tokens; both operands come as the product wants them, eight consecutive numbers of a row to a lane (the
-// tokens' out of the first cache).  fp32 numbers are split on the way.
-template <typename T> struct Parts;                                 // of eight numbers, as operands
-template <> struct Parts<bf16> {
-    bf16x8 v[1];
-    __device__ __forceinline__ Parts(const bf16* p, bool there) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (there) w = *reinterpret_cast<const uint4*>(p);
-        v[0] = __builtin_bit_cast(bf16x8, w);
+// ---- few tokens: the embedding is read once by each product, straight into registers, and that bounds them
+// Operands come as the products want them, 16 bytes of a row to a lane; which four (or eight) contraction indices a lane has is free as long as both operands agree.  Logits of bfloat16 numbers
+// on the bfloat16 instructions, everything else in fp32 on its own (16 x 16 x 4): dz is not rounded, and nothing is split into parts.
+// A lane has row (column) l % 16 and the indices of l / 16.
+__device__ __forceinline__ void four(const bf16* p, bool there, float (&x)[4]) {
+    uint2 w = make_uint2(0, 0);
+    if (there) w = *reinterpret_cast<const uint2*>(p);
+    x[0] = __uint_as_float(w.x << 16), x[1] = __uint_as_float(w.x & 0xFFFF0000u), x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void four(const float* p, bool there, float (&x)[4]) {
+    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (there) w = *reinterpret_cast<const float4*>(p);
+    x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
+}
+template <typename T>
+__device__ __forceinline__ floatx4 few_terms(uint4 a, uint4 b, floatx4 c) {
+    if constexpr (sizeof(T) == 2) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    } else {
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
     }
-};
-template <> struct Parts<float> {
-    bf16x8 v[PLANES_MAX];
-    __device__ __forceinline__ Parts(const float* p, bool there) {
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (there) load8(p, x);
-#pragma unroll
-        for (int part = 0; part < PLANES_MAX; ++part) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[e] = pack2(x[2 * e], x[2 * e + 1]);
-                x[2 * e] -= __uint_as_float(w[e] << 16);
-                x[2 * e + 1] -= __uint_as_float(w[e] & 0xFFFF0000u);
-            }
-            v[part] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-    }
-};
-__device__ __forceinline__ void terms(const Parts<bf16>& a, const Parts<bf16>& b, floatx4& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[0], b.v[0], c, 0, 0, 0); }
-__device__ __forceinline__ void terms(const Parts<float>& a, const Parts<float>& b, floatx4& c) {
-    constexpr int A[6] = {0, 2, 1, 0, 1, 0}, B[6] = {2, 0, 1, 1, 0, 0};
-#pragma unroll
-    for (int t = 0; t < 6; ++t) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[A[t]], b.v[B[t]], c, 0, 0, 0);
 }
 
-template <typename T, int TT>
-__global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, const T* __restrict__ E, const int* __restrict__ labels, int tokens, int W, int V,
-                                                   float2* __restrict__ stats, float* __restrict__ at_label) {
+// Logits: a wavefront takes sixteen rows of the embedding and all tokens, 16 TT at most.  GRAD: dz from them, else their statistics and each label's logit.
+struct FewArgs {
+    const int* labels;
+    float2* stats;                       // [VOCAB_FEW_COLUMNS columns][tokens]
+    float* at_label;
+    const float *lse, *dloss;
+    float* dz;                           // [tokens][few_pitch(vocab)]
+};
+template <typename T, int TT, bool GRAD>
+__global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, const T* __restrict__ E, int tokens, int W, int V, const FewArgs args) {
     __shared__ float2 part[4][16 * TT];
+    constexpr int WORD = 16 / sizeof(T), STEP = 4 * WORD, U = 8;    // numbers of a lane and of a step; steps whose loads are on the way while as many are worked on
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
-    const int v0 = blockIdx.x * VOCAB_FEW_COLUMNS + 16 * wave, t0 = blockIdx.y * 16 * TT;
-    const T* const e = E + (int64_t)min(v0 + r, V - 1) * W + 8 * g;
+    const int v0 = blockIdx.x * VOCAB_FEW_COLUMNS + 16 * wave;
+    const T* const e = E + (int64_t)min(v0 + r, V - 1) * W + WORD * g;
     const T* x[TT];
 #pragma unroll
-    for (int i = 0; i < TT; ++i) x[i] = h + (int64_t)min(t0 + 16 * i + r, tokens - 1) * W + 8 * g;
+    for (int i = 0; i < TT; ++i) x[i] = h + (int64_t)min(16 * i + r, tokens - 1) * W + WORD * g;
     floatx4 acc[TT];
 #pragma unroll
     for (int i = 0; i < TT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    // U steps' loads of the embedding are on the way while U others are worked on
-    constexpr int U = sizeof(T) == 2 ? 8 : 4, WORDS = sizeof(T) / 2;
-    uint4 raw[2][U][WORDS];
-    const int batches = W / (32 * U);
-    auto load = [&](uint4 (&to)[U][WORDS], int batch) __attribute__((always_inline)) {
+    uint4 raw[2][U];
+    const int batches = W / (STEP * U);
+    auto load = [&](uint4 (&to)[U], int batch) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) to[u] = *reinterpret_cast<const uint4*>(e + STEP * (batch * U + u));
+    };
+    auto work = [&](const uint4 (&from)[U], int batch) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int q = 0; q < WORDS; ++q) to[u][q] = reinterpret_cast<const uint4*>(e + 32 * (batch * U + u))[q];
-    };
-    auto work = [&](const uint4 (&from)[U][WORDS], int batch) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const Parts<T> b(reinterpret_cast<const T*>(from[u]), true);
-#pragma unroll
-            for (int i = 0; i < TT; ++i) terms(b, Parts<T>(x[i] + 32 * (batch * U + u), true), acc[i]);
-        }
+            for (int i = 0; i < TT; ++i) acc[i] = few_terms<T>(from[u], *reinterpret_cast<const uint4*>(x[i] + STEP * (batch * U + u)), acc[i]);
     };
     if (batches > 0) load(raw[0], 0);
     int batch = 0;
@@ -815,84 +729,200 @@ __global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, cons
         work(raw[1], batch + 1);
     }
     if (batch < batches) work(raw[0], batch);
-    int k = 32 * U * batches;
-    for (; k < W; k += 32) {                                        // (a last step may be short: W is a multiple of eight)
-        const bool there = k + 8 * g < W;
-        const Parts<T> b(e + k, there);
+    for (int k = STEP * U * batches; k < W; k += STEP) {            // (a last step may be short: W is a multiple of eight)
+        const bool there = k + WORD * g < W;
+        const uint4 none = make_uint4(0, 0, 0, 0), b = there ? *reinterpret_cast<const uint4*>(e + k) : none;
 #pragma unroll
-        for (int i = 0; i < TT; ++i) terms(b, Parts<T>(x[i] + k, there), acc[i]);
+        for (int i = 0; i < TT; ++i) acc[i] = few_terms<T>(b, there ? *reinterpret_cast<const uint4*>(x[i] + k) : none, acc[i]);
     }
-    // acc[i][v]: column v0 + 4 g + v, token t0 + 16 i + r
-    auto larger = [](float a, float b) { return fmaxf(a, b); };
-    auto plus = [](float a, float b) { return a + b; };
+    // acc[i][v]: column v0 + 4 g + v, token 16 i + r
+    if constexpr (GRAD) {
 #pragma unroll
-    for (int i = 0; i < TT; ++i) {
-        const int token = t0 + 16 * i + r, label = token < tokens ? labels[token] : -1;
-        float top = -INFINITY, sum = 0.f;
+        for (int i = 0; i < TT; ++i) {
+            const int token = 16 * i + r;
+            if (token >= tokens) continue;
+            const int label = args.labels[token];
+            const bool has = label >= 0 && label < V;
+            const float lse = args.lse[token], d = args.dloss[token];
+            float z[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int col = v0 + 4 * g + v;
-            if (col == label && col < V) at_label[token] = acc[i][v];
-            if (col >= V) acc[i][v] = -INFINITY;
-            top = fmaxf(top, acc[i][v]);
+            for (int v = 0; v < 4; ++v) {
+                const int col = v0 + 4 * g + v;
+                const float y = acc[i][v] - lse;
+                z[v] = has && col < V ? d * (col == label ? expm1f(y) : exp2_fast(y * LOG2E)) : 0.f;
+            }
+            *reinterpret_cast<float4*>(args.dz + (int64_t)token * few_pitch(V) + v0 + 4 * g) = make_float4(z[0], z[1], z[2], z[3]);
         }
-        top = apart<32>(apart<16>(top, larger), larger);
-        const float base = top == -INFINITY ? 0.f : top * LOG2E;
+    } else {
+        auto larger = [](float a, float b) { return fmaxf(a, b); };
+        auto plus = [](float a, float b) { return a + b; };
 #pragma unroll
-        for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(acc[i][v], LOG2E, -base));
-        sum = apart<32>(apart<16>(sum, plus), plus);
-        if (g == 0) part[wave][16 * i + r] = make_float2(top == -INFINITY ? -INFINITY : base, sum);
-    }
-    __syncthreads();
-    const int mine = threadIdx.x;
-    if (mine >= 16 * TT || t0 + mine >= tokens) return;
-    float2 all = part[0][mine];
+        for (int i = 0; i < TT; ++i) {
+            const int token = 16 * i + r, label = token < tokens ? args.labels[token] : -1;
+            float top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) {
-        const float2 o = part[w][mine];
-        const float m = fmaxf(all.x, o.x), from = m == -INFINITY ? 0.f : m;
-        all = make_float2(m, all.y * exp2_fast(all.x - from) + o.y * exp2_fast(o.x - from));
+            for (int v = 0; v < 4; ++v) {
+                const int col = v0 + 4 * g + v;
+                if (col == label && col < V) args.at_label[token] = acc[i][v];
+                if (col >= V) acc[i][v] = -INFINITY;
+                top = fmaxf(top, acc[i][v]);
+            }
+            top = apart<32>(apart<16>(top, larger), larger);
+            const float base = top == -INFINITY ? 0.f : top * LOG2E;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(acc[i][v], LOG2E, -base));
+            sum = apart<32>(apart<16>(sum, plus), plus);
+            if (g == 0) part[wave][16 * i + r] = make_float2(top == -INFINITY ? -INFINITY : base, sum);
+        }
+        __syncthreads();
+        const int mine = threadIdx.x;
+        if (mine >= 16 * TT || mine >= tokens) return;
+        float2 all = part[0][mine];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            const float2 o = part[w][mine];
+            const float m = fmaxf(all.x, o.x), from = m == -INFINITY ? 0.f : m;
+            all = make_float2(m, all.y * exp2_fast(all.x - from) + o.y * exp2_fast(o.x - from));
+        }
+        args.stats[(int64_t)blockIdx.x * tokens + mine] = all;
     }
-    stats[(int64_t)blockIdx.x * tokens + t0 + mine] = all;
 }
 
-bool small(int m) { return m <= 128; }
+// dh = dz E: a wavefront takes 64 columns and a range of the vocabulary, sixteen rows of it at a time.  Of a lane's four columns 4 (l % 16) + c each is a product of its
+// own, and so is each row 4 (l / 16) + d of the sixteen.
+template <typename T, int TT>
+__global__ __launch_bounds__(256) void k_vocab_few_dh(const float* __restrict__ dz, const T* __restrict__ E, int tokens, int W, int V, int rows_a_range, float* __restrict__ sums) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+    const int c0 = blockIdx.y * 256 + 64 * wave + 4 * r;
+    const int begin = blockIdx.x * rows_a_range, end = min(begin + rows_a_range, V);
+    if ((int)blockIdx.y * 256 + 64 * wave >= W) return;
+    const bool there = c0 < W;                                      // (W a multiple of eight)
+    const T* const e = E + (there ? c0 : 0);
+    const float* z[TT];
+#pragma unroll
+    for (int i = 0; i < TT; ++i) z[i] = dz + (int64_t)min(16 * i + r, tokens - 1) * few_pitch(V) + 4 * g;
+    floatx4 acc[TT][4];
+#pragma unroll
+    for (int i = 0; i < TT; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[i][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+    for (int v = begin; v < end; v += 16) {                         // (dz is 0 behind the vocabulary: its last row stands in for what is missing)
+        float y[4][4], x[TT][4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) four(e + (int64_t)min(v + 4 * g + d, V - 1) * W, there, y[d]);
+#pragma unroll
+        for (int i = 0; i < TT; ++i) four(z[i] + v, true, x[i]);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < TT; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][d], y[d][c], acc[i][c], 0, 0, 0);
+    }
+    if (!there) return;
+#pragma unroll
+    for (int i = 0; i < TT; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int token = 16 * i + 4 * g + q;
+            if (token < tokens) store4(sums + ((int64_t)blockIdx.x * tokens + token) * W + c0, acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]);
+        }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_vocab_few_sums(const float* __restrict__ sums, const int* __restrict__ labels, int tokens, int W, int V, int ranges, T* __restrict__ dh) {
+    const int64_t numbers = (int64_t)tokens * W, at = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+    if (at >= numbers) return;
+    const int label = labels[at / W];
+    if (label < 0 || label >= V) return store4(dh + at, 0.f, 0.f, 0.f, 0.f);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int i = 0; i < ranges; ++i) {
+        const float4 y = *reinterpret_cast<const float4*>(sums + i * numbers + at);
+        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+    }
+    store4(dh + at, x.x, x.y, x.z, x.w);
+}
+
+// dE = dz^T h: a wavefront takes 64 rows of the vocabulary and 64 columns, sixteen tokens at a time.  Hidden states without a label are not read.
+template <typename T>
+__global__ __launch_bounds__(256) void k_vocab_few_dE(const float* __restrict__ dz, const T* __restrict__ h, const int* __restrict__ labels, int tokens, int W, int V, T* __restrict__ dE) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+    const int c0 = blockIdx.y * 256 + 64 * wave + 4 * r, v0 = blockIdx.x * 64;
+    if ((int)blockIdx.y * 256 + 64 * wave >= W) return;
+    const bool there = c0 < W;
+    floatx4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[i][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < tokens; t += 16) {
+        float y[4][4], x[4][4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            const int token = t + 4 * g + d, label = token < tokens ? labels[token] : -1;
+            four(h + (int64_t)min(token, tokens - 1) * W + (there ? c0 : 0), there && label >= 0 && label < V, y[d]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i][d] = token < tokens ? dz[(int64_t)token * few_pitch(V) + v0 + 16 * i + r] : 0.f;
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i][d], y[d][c], acc[i][c], 0, 0, 0);
+    }
+    if (!there) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int v = v0 + 16 * i + 4 * g + q;
+            if (v < V) store4(dE + (int64_t)v * W + c0, acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]);
+        }
+}
+
+// f(a number of the type, tiles of sixteen tokens)
+template <typename F>
+void with_few(const mst_vocab_loss_shape& s, F&& f) {
+    auto sized = [&](auto type) {
+        if (s.tokens <= 16) f(type, std::integral_constant<int, 1>{});
+        else f(type, std::integral_constant<int, 2>{});
+    };
+    if (s.type == MST_BF16) sized(bf16{});
+    else if (s.tokens <= 32) sized(float{});
+    else f(float{}, std::integral_constant<int, 4>{});
+}
+static_assert(VOCAB_FEW_BF16 <= 32 && VOCAB_FEW_F32 <= 64);
 
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipStream_t s) {
-    if (small(E == OUT_F32 || E == OUT_BF16 ? p.k : p.m)) {
-        const int64_t blocks = cdiv(p.m, SM) * cdiv(p.n, SM) * p.splits;
-        k_vocab_small<A_ALONG, B_ALONG, E><<<(unsigned)blocks, 256, 0, s>>>(p, e);
-    } else {
-        // (one to a CU)
-        const unsigned grid = (unsigned)std::min<int64_t>(256, 8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8));
-        auto run = [&](auto kernel, unsigned bytes, uint64_t& done) {
-            if (int rc = allow_lds(reinterpret_cast<const void*>(kernel), (int)bytes, done)) return rc;
-            kernel<<<grid, 256, bytes, s>>>(p, e);
-            return (int)MST_OK;
-        };
-        static uint64_t done[2] = {0, 0};
-        int rc = MST_ERR_ARG;
-        if constexpr (E != LOGIT_GRAD && E != OUT_BF16) {
-            if (p.planes > 1) rc = run(k_vocab_large_parts<A_ALONG, B_ALONG, E>, Q_LDS, done[1]);
-        }
-        if constexpr (E != LOGIT_GRAD_PARTS && E != OUT_F32) {
-            if (p.planes == 1) rc = run(k_vocab_large<A_ALONG, B_ALONG, E>, L_LDS, done[0]);
-        }
-        if (rc) return rc;
+    // (one to a CU)
+    const unsigned grid = (unsigned)std::min<int64_t>(256, 8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8));
+    auto run = [&](auto kernel, unsigned bytes, uint64_t& done) {
+        if (int rc = allow_lds(reinterpret_cast<const void*>(kernel), (int)bytes, done)) return rc;
+        kernel<<<grid, 256, bytes, s>>>(p, e);
+        return (int)MST_OK;
+    };
+    static uint64_t done[2] = {0, 0};
+    int rc = MST_ERR_ARG;
+    if constexpr (E != LOGIT_GRAD && E != OUT_BF16) {
+        if (p.planes > 1) rc = run(k_vocab_large_parts<A_ALONG, B_ALONG, E>, Q_LDS, done[1]);
     }
+    if constexpr (E != LOGIT_GRAD_PARTS && E != OUT_F32) {
+        if (p.planes == 1) rc = run(k_vocab_large<A_ALONG, B_ALONG, E>, L_LDS, done[0]);
+    }
+    if (rc) return rc;
     MST_LAUNCH_CHECK();
     return MST_OK;
 }
 
 }  // namespace
 
-int vocab_stat_columns(int m) { return small(m) ? SM / 2 : VT / 2; }
-
 // As many ranges as let the products end first: rounds of 256 workgroups, each as long as its range and what begins and ends it (the time of some eight
 // pairs of steps, the sums of the pieces before and behind among it).
 int vocab_splits(int m, int n, int k) {
-    const int64_t side = small(m) ? SM : VT, tiles = cdiv(m, side) * cdiv(n, side), pairs = cdiv(k, L_PAIR);
+    const int64_t tiles = cdiv(m, VT) * cdiv(n, VT), pairs = cdiv(k, L_PAIR);
     int best = 1;
     int64_t least = INT64_MAX;
     for (int s = 1; s <= 64 && s <= pairs; ++s) {
@@ -903,19 +933,37 @@ int vocab_splits(int m, int n, int k) {
 }
 
 int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream) {
-    auto launch = [&](auto type, auto tt) {
+    with_few(s, [&](auto type, auto tt) {
         using T = decltype(type);
         constexpr int TT = decltype(tt)::value;
-        k_vocab_few<T, TT><<<dim3((unsigned)cdiv(s.vocab, VOCAB_FEW_COLUMNS), (unsigned)cdiv(s.tokens, 16 * TT)), 256, 0, stream>>>(
-            static_cast<const T*>(h), static_cast<const T*>(E), labels, s.tokens, s.width, s.vocab, stats, at_label);
-    };
-    auto typed = [&](auto type) {
-        if (s.tokens <= 16) launch(type, std::integral_constant<int, 1>{});
-        else if (s.tokens <= 32) launch(type, std::integral_constant<int, 2>{});
-        else launch(type, std::integral_constant<int, 4>{});
-    };
-    if (s.type == MST_F32) typed(float{});
-    else typed(bf16{});
+        k_vocab_few<T, TT, false><<<(unsigned)cdiv(s.vocab, VOCAB_FEW_COLUMNS), 256, 0, stream>>>(
+            static_cast<const T*>(h), static_cast<const T*>(E), s.tokens, s.width, s.vocab, {labels, stats, at_label, nullptr, nullptr, nullptr});
+    });
+    MST_LAUNCH_CHECK();
+    return MST_OK;
+}
+// Ranges of the vocabulary for dh: some thousand workgroups, of 64 rows at least.
+int vocab_few_ranges(const mst_vocab_loss_shape& s) {
+    return (int)std::min(cdiv(1024, cdiv(s.width, 256)), cdiv(s.vocab, 64));
+}
+int vocab_few_bwd(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, const float* lse, const float* dloss, float* dz, float* sums, void* dh, void* dE,
+                  hipStream_t stream) {
+    const int ranges = vocab_few_ranges(s), rows = (int)align_up(cdiv(s.vocab, ranges), 16);
+    const unsigned columns = (unsigned)cdiv(s.width, 256);
+    with_few(s, [&](auto type, auto tt) {
+        using T = decltype(type);
+        constexpr int TT = decltype(tt)::value;
+        k_vocab_few<T, TT, true><<<(unsigned)cdiv(s.vocab, VOCAB_FEW_COLUMNS), 256, 0, stream>>>(
+            static_cast<const T*>(h), static_cast<const T*>(E), s.tokens, s.width, s.vocab, {labels, nullptr, nullptr, lse, dloss, dz});
+        if (dh) {
+            const int used = (int)cdiv(s.vocab, rows);
+            const int64_t numbers = (int64_t)s.tokens * s.width;
+            k_vocab_few_dh<T, TT><<<dim3((unsigned)used, columns), 256, 0, stream>>>(dz, static_cast<const T*>(E), s.tokens, s.width, s.vocab, rows, sums);
+            k_vocab_few_sums<T><<<(unsigned)cdiv(numbers, 1024), 256, 0, stream>>>(sums, labels, s.tokens, s.width, s.vocab, used, static_cast<T*>(dh));
+        }
+        if (dE)
+            k_vocab_few_dE<T><<<dim3((unsigned)cdiv(s.vocab, 64), columns), 256, 0, stream>>>(dz, static_cast<const T*>(h), labels, s.tokens, s.width, s.vocab, static_cast<T*>(dE));
+    });
     MST_LAUNCH_CHECK();
     return MST_OK;
 }

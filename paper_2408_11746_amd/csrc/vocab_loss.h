@@ -10,6 +10,7 @@ constexpr int VT = 256;                  // rows and columns of the largest outp
 constexpr int VK = 32;                   // contraction indices of a step
 constexpr int VPAD = 64;                 // operands are padded to so many
 constexpr int PLANES_MAX = 3;
+constexpr int VOCAB_STAT_COLUMNS = VT / 2;      // (a wavefront's)
 
 // A matrix of bfloat16 numbers, or of numbers that are the sum of three (plane p a stride further on).  Along: a row's numbers are
 // contraction indices; across: a row is one contraction index.  Rows past `rows` read as the last one.
@@ -30,9 +31,9 @@ struct VocabProduct {
 };
 
 // ---- what becomes of C
-// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and vocab_stat_columns columns
+// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and VOCAB_STAT_COLUMNS columns
 struct VocabStats {
-    float2* stats;                       // [vocab_stat_columns columns][row_stride]
+    float2* stats;                       // [VOCAB_STAT_COLUMNS columns][row_stride]
     int64_t row_stride;
     int first;                           // number of the first of them
     const float* at_label;               // logit of a row's label, padded to VT
@@ -62,11 +63,17 @@ struct VocabOut {                        // rows of the result times the unit, i
     const float* unit;
 };
 
-int vocab_stat_columns(int m);
 int vocab_splits(int m, int n, int k);   // ranges of the contraction for vocab_sums
-// The forward for few tokens, from the hidden states as they are: statistics per VOCAB_FEW_COLUMNS columns, [columns][tokens], and each label's logit
-constexpr int VOCAB_FEW = 128, VOCAB_FEW_COLUMNS = 64;
+// Few tokens, from the hidden states as they are: statistics per VOCAB_FEW_COLUMNS columns, [columns][tokens], and each label's logit; dz in fp32, [tokens][few_pitch(vocab)],
+// and both gradients from it (either may be null), dh by way of sums [vocab_few_ranges][tokens][width]
+constexpr int VOCAB_FEW_COLUMNS = 64;
+__host__ __device__ constexpr int64_t few_pitch(int vocab) { return ((int64_t)vocab + VOCAB_FEW_COLUMNS - 1) / VOCAB_FEW_COLUMNS * VOCAB_FEW_COLUMNS; }
+constexpr int VOCAB_FEW_BF16 = 32, VOCAB_FEW_F32 = 64;
+inline bool vocab_is_few(const mst_vocab_loss_shape& s) { return s.tokens <= (s.type == MST_F32 ? VOCAB_FEW_F32 : VOCAB_FEW_BF16); }
 int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream);
+int vocab_few_ranges(const mst_vocab_loss_shape& s);
+int vocab_few_bwd(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, const float* lse, const float* dloss, float* dz, float* sums, void* dh, void* dE,
+                  hipStream_t stream);
 int vocab_stats(const VocabProduct& p, const VocabStats& e, hipStream_t s);            // a, b along
 int vocab_logit_grad(const VocabProduct& p, const VocabLogitGrad& e, hipStream_t s);   // a, b along
 int vocab_sums(const VocabProduct& p, const VocabSums& e, hipStream_t s);              // a along, b across

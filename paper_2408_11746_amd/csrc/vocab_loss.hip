@@ -249,13 +249,20 @@ struct Plan {
         pieces = (int)cdiv(s.vocab, most);
         piece = (int)align_up(cdiv(s.vocab, pieces), VT);
         pieces = (int)cdiv(s.vocab, piece);
-        few = !backward && s.tokens <= VOCAB_FEW;
-        stat_columns = few ? VOCAB_FEW_COLUMNS : vocab_stat_columns(s.tokens);
+        few = vocab_is_few(s);
+        stat_columns = few ? VOCAB_FEW_COLUMNS : VOCAB_STAT_COLUMNS;
         stats = (int)cdiv(s.vocab, stat_columns);
         sum_blocks = (int)align_up(s.width, VT) / 16;
         splits = vocab_splits(s.tokens, s.width, std::min(piece, s.vocab));
         bytes = 0;
         auto part = [&](size_t n) { const size_t at = bytes; bytes += align_up(n); return at; };
+        if (few) {
+            at_label = part(backward ? 0 : 4 * (size_t)s.tokens);
+            stat = part(backward ? 0 : 8 * (size_t)s.tokens * stats);
+            ds = part(backward ? 4 * (size_t)s.tokens * few_pitch(s.vocab) : 0);
+            sums = part(backward ? 4 * (size_t)vocab_few_ranges(s) * s.tokens * s.width : 0);
+            return;
+        }
         count = part(4);
         unit = part(4);
         place = part(4 * (size_t)rows);
@@ -264,8 +271,8 @@ struct Plan {
         at_label = part(4 * (size_t)rows);
         lse = part(backward ? 4 * (size_t)rows : 0);
         d = part(backward ? 4 * (size_t)rows : 0);
-        h = part(few ? 0 : 2 * planes * (size_t)rows * wide);
-        E = part(split_E && !few ? 2 * planes * (size_t)piece * wide : 0);
+        h = part(2 * planes * (size_t)rows * wide);
+        E = part(split_E ? 2 * planes * (size_t)piece * wide : 0);
         stat = part(backward ? 0 : 8 * (size_t)rows * stats);
         ds = part(backward ? 2 * planes * (size_t)rows * piece : 0);
         sums = part(backward ? 4 * (size_t)splits * sum_stride() : 0);
@@ -333,6 +340,7 @@ struct Run {
     }
 
     int backward(const int* labels, const float* lse, const float* dloss, T* dh, T* dE) const {
+        if (plan.few) return vocab_few_bwd(s, h, E, labels, lse, dloss, at<float>(plan.ds), at<float>(plan.sums), dh, dE, stream);
         if (int e = rows(labels, nullptr, nullptr, lse, dloss)) return e;
         const int64_t plane = plan.rows * plan.piece;
         const VocabOperand ds_rows = {at<uint16_t>(plan.ds), plane, plan.piece, (int)plan.rows};
