@@ -829,18 +829,24 @@ __global__ __launch_bounds__(256) void k_vocab_few_dh(const float* __restrict__ 
             if (token < tokens) store4(sums + ((int64_t)blockIdx.x * tokens + token) * W + c0, acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]);
         }
 }
+// (sixteen shares of the ranges to four numbers: with one, a token's sums are too few to hide behind one another, 17 us for eight tokens)
 template <typename T>
 __global__ __launch_bounds__(256) void k_vocab_few_sums(const float* __restrict__ sums, const int* __restrict__ labels, int tokens, int W, int V, int ranges, T* __restrict__ dh) {
-    const int64_t numbers = (int64_t)tokens * W, at = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
-    if (at >= numbers) return;
-    const int label = labels[at / W];
-    if (label < 0 || label >= V) return store4(dh + at, 0.f, 0.f, 0.f, 0.f);
+    __shared__ float4 part[16][16];
+    const int q = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int64_t numbers = (int64_t)tokens * W, at = 4 * ((int64_t)blockIdx.x * 16 + q);
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float4 y) __attribute__((always_inline)) { x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w); };
+    if (at < numbers)
 #pragma unroll 8
-    for (int i = 0; i < ranges; ++i) {
-        const float4 y = *reinterpret_cast<const float4*>(sums + i * numbers + at);
-        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-    }
+        for (int i = share; i < ranges; i += 16) add(*reinterpret_cast<const float4*>(sums + i * numbers + at));
+    part[share][q] = x;
+    __syncthreads();
+    if (share || at >= numbers) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) add(part[i][q]);
+    const int label = labels[at / W];
+    if (label < 0 || label >= V) x = make_float4(0.f, 0.f, 0.f, 0.f);
     store4(dh + at, x.x, x.y, x.z, x.w);
 }
 
@@ -959,7 +965,7 @@ int vocab_few_bwd(const mst_vocab_loss_shape& s, const void* h, const void* E, c
             const int used = (int)cdiv(s.vocab, rows);
             const int64_t numbers = (int64_t)s.tokens * s.width;
             k_vocab_few_dh<T, TT><<<dim3((unsigned)used, columns), 256, 0, stream>>>(dz, static_cast<const T*>(E), s.tokens, s.width, s.vocab, rows, sums);
-            k_vocab_few_sums<T><<<(unsigned)cdiv(numbers, 1024), 256, 0, stream>>>(sums, labels, s.tokens, s.width, s.vocab, used, static_cast<T*>(dh));
+            k_vocab_few_sums<T><<<(unsigned)cdiv(numbers, 64), 256, 0, stream>>>(sums, labels, s.tokens, s.width, s.vocab, used, static_cast<T*>(dh));
         }
         if (dE)
             k_vocab_few_dE<T><<<dim3((unsigned)cdiv(s.vocab, 64), columns), 256, 0, stream>>>(dz, static_cast<const T*>(h), labels, s.tokens, s.width, s.vocab, static_cast<T*>(dE));

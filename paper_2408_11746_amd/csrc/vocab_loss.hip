@@ -192,25 +192,27 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_vocab_join(const float2* __res
     if (loss) loss[token] = has ? l - at_label[row] : 0.f;
 }
 
-// gradients of the hidden states: sums of the splits, back to the tokens' places; a wavefront takes blocks of 16 rows and 16 columns
-template <typename T>
+// gradients of the hidden states: sums of the splits, back to the tokens' places; a wavefront takes blocks of 16 rows and 16 columns, or a workgroup's four share one
+template <typename T, bool SHARE>
 __global__ __launch_bounds__(256) void k_vocab_dh(const float* __restrict__ sums, int64_t stride, int wide, int splits, const int* __restrict__ count, const int* __restrict__ list,
                                                   const float* __restrict__ unit, int W, T* __restrict__ dh) {
-    const int rows = *count, lane = threadIdx.x & 63, row = blockIdx.x * 16 + (lane & 15);
-    if ((int)blockIdx.x * 16 >= rows) return;
-    const float u = *unit;
-    const int64_t token = row < rows ? list[row] : 0;
-    for (int c = 16 * (blockIdx.y * 4 + (threadIdx.x >> 6)); c < W; c += 64 * gridDim.y) {
-        const float* const from = sums + 4 * (sum_place(row, c, wide) + lane);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    __shared__ float4 part[4][64];
+    const int rows = *count, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * 16 + (lane & 15), c = 16 * (SHARE ? blockIdx.y : blockIdx.y * 4 + wave);
+    if ((int)blockIdx.x * 16 >= rows || c >= W) return;             // (SHARE: all of them or none)
+    const float* const from = sums + 4 * (sum_place(row, c, wide) + lane);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float4 y) __attribute__((always_inline)) { x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w); };
 #pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float4 y = *reinterpret_cast<const float4*>(from + s * stride);
-            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-        }
-        const int col = c + 4 * (lane >> 4);
-        if (row < rows && col < W) store4(dh + token * W + col, u * x.x, u * x.y, u * x.z, u * x.w);
+    for (int s = SHARE ? wave : 0; s < splits; s += SHARE ? 4 : 1) add(*reinterpret_cast<const float4*>(from + s * stride));
+    if constexpr (SHARE) {
+        part[wave][lane] = x;
+        __syncthreads();
+        if (wave) return;
+        for (int w = 1; w < 4; ++w) add(part[w][lane]);
     }
+    const int col = c + 4 * (lane >> 4);
+    const float u = *unit;
+    if (row < rows && col < W) store4(dh + (int64_t)list[row] * W + col, u * x.x, u * x.y, u * x.z, u * x.w);
 }
 // ... and those of the tokens without a label: 0; a wavefront a token
 template <typename T>
@@ -361,7 +363,9 @@ struct Run {
             }
         }
         if (dh) {
-            k_vocab_dh<T><<<dim3((unsigned)cdiv(s.tokens, 16), (unsigned)cdiv(s.width, 256)), 256, 0, stream>>>(
+            const bool share = plan.splits > 8;
+            const auto kernel = share ? k_vocab_dh<T, true> : k_vocab_dh<T, false>;
+            kernel<<<dim3((unsigned)cdiv(s.tokens, 16), (unsigned)cdiv(s.width, share ? 16 : 64)), 256, 0, stream>>>(
                 at<float>(plan.sums), plan.sum_stride(), plan.sum_blocks, plan.splits, at<int>(plan.count), at<int>(plan.list), at<float>(plan.unit), s.width, dh);
             MST_LAUNCH_CHECK();
             k_vocab_dh_others<T><<<(unsigned)cdiv(s.tokens, 4), 256, 0, stream>>>(at<int>(plan.place), s.tokens, s.width, dh);
