@@ -710,8 +710,8 @@ def _kept(kept, rows, width, device):
     if kept is None:
         return None
     f32, int8, _ = _small_types()
-    _dense(kept.codes, int8, rows * width, device)
-    _dense(kept.units, f32, rows * -(-width // 128) if width > 0 else 0, device)
+    kept._c.codes_dev = _dense(kept.codes, int8, rows * width, device)          # (as they are now: a tensor may have been given other memory)
+    kept._c.units_dev = _dense(kept.units, f32, rows * -(-width // 128) if width > 0 else 0, device)
     return kept._ref
 
 

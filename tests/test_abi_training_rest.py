@@ -190,3 +190,11 @@ def test_tensors_are_on_the_gpu_that_the_call_runs_on():
     for call in (lambda: _norm_fwd(_norm(), x=T), lambda: mst.mst_gelu_fwd(_gelu(), T, FAKE, None, 0), lambda: _loss_fwd(_loss(type=0), h=T), lambda: mst.mst_checkpoint_write(4, 64, T, 0, KEPT, 0)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_a_checkpoint_is_passed_as_it_is_now():
+    kept = mst.Checkpoint8(FAKE, FAKE)
+    kept.units = 0                                                  # (once without memory: refused)
+    assert _code(lambda: mst.mst_checkpoint_write(1, 8, FAKE, 0, kept, stream=0)) == -1
+    kept.codes, kept.units = FAKE + 8, FAKE
+    assert _code(lambda: mst.mst_checkpoint_read(1, 8, kept, 0, FAKE, stream=0)) == -1
