@@ -19,7 +19,7 @@ constexpr int64_t PIECE_BYTES = int64_t(1) << 29;
 // ---- which tokens have a label
 constexpr int ROWS_THREADS = 1024, ROWS_EACH = 8;
 // One workgroup: place[token] = its row or -1, list[row] = token, label[row], count.  In order.  Rows behind the last, up to a whole tile: label -1.
-// Outputs of tokens without one: 0.  unit: the largest size of the rows' dloss (1 if all are 0).
+// Outputs of tokens without one: 0.  unit: the largest finite size of the rows' dloss (1 if all are 0): an infinite one is its own row's alone.
 __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restrict__ labels, int T, int V, int* __restrict__ count, int* __restrict__ place,
                                                              int* __restrict__ list, int* __restrict__ label, float* __restrict__ loss, float* __restrict__ lse,
                                                              const float* __restrict__ dloss, float* __restrict__ unit) {
@@ -72,7 +72,8 @@ __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restri
                 const bool has = mine[e] >= 0;
                 place[first + e] = has ? row : -1;
                 if (has) list[row] = first + e, label[row] = mine[e], ++row;
-                if (has && dloss) top = max(top, __float_as_int(d[e]) & 0x7FFFFFFF);
+                const int size = __float_as_int(d[e]) & 0x7FFFFFFF;
+                if (has && dloss && size < 0x7F800000) top = max(top, size);
                 if (!has && loss) loss[first + e] = 0.f;
                 if (!has && lse) lse[first + e] = 0.f;
             }

@@ -171,6 +171,24 @@ def test_what_tokens_without_a_label_hold_counts_for_nothing(tokens, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [20, 150, 600])
+def test_an_infinite_gradient_is_its_own_token_s_alone(tokens, dtype):
+    a, b = (Case(16, tokens, 136, 450, dtype, unlabelled=0.2) for _ in range(2))
+    at = [int(t) for t in torch.nonzero((a.labels >= 0) & (a.labels < a.V))[:3, 0]]
+    a.dloss[at] = 0.0
+    b.dloss[at] = torch.tensor([float("inf"), -float("inf"), float("nan")], device=DEV)
+    for c in (a, b):
+        c.forward()
+        c.backward()
+    torch.cuda.synchronize()
+    others = torch.ones(tokens, dtype=torch.bool, device=DEV)
+    others[at] = False
+    assert torch.equal(a.dh.t[others], b.dh.t[others])
+    assert not b.dh.t[at].isfinite().any() and b.dE.t.isnan().all()
+    a.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_one_label_for_all(dtype):
     _all(7, 300, 64, 900, dtype, labels=np.full(300, 431))
     _all(8, 40, 64, 900, dtype, labels=np.full(40, 899))
