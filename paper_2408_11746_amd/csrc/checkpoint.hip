@@ -16,6 +16,9 @@ struct Groups {
     int64_t numbers;             // rows x width
     int width, per_row;          // per_row 0: one sequence
 };
+// (A launch has less than 2^32 threads along x: the rest along y.)
+constexpr int BLOCKS_ALONG = 1 << 22;
+__device__ inline int64_t group_of_thread() { return ((int64_t)blockIdx.y * BLOCKS_ALONG + blockIdx.x) * GROUPS_A_BLOCK + (threadIdx.x >> 5); }
 struct Place {
     int64_t at;                  // first number of the lane
     int n;                       // how many of its four are there (may be below 0)
@@ -62,7 +65,7 @@ __device__ inline void gelu(float x, float& y, float& slope) {
 template <typename T>
 __global__ __launch_bounds__(THREADS) void k_checkpoint_write(Groups g, const T* __restrict__ x, int8_t* __restrict__ codes, float* __restrict__ units) {
     const int lane = threadIdx.x & 31;
-    const int64_t group = (int64_t)blockIdx.x * GROUPS_A_BLOCK + (threadIdx.x >> 5);
+    const int64_t group = group_of_thread();
     if (group >= g.count) return;
     const Place p = place_of(g, group, lane);
     float v[4];
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(THREADS) void k_checkpoint_write(Groups g, const T*
 
 template <typename T>
 __global__ __launch_bounds__(THREADS) void k_checkpoint_read(Groups g, const int8_t* __restrict__ codes, const float* __restrict__ units, T* __restrict__ x) {
-    const int64_t group = (int64_t)blockIdx.x * GROUPS_A_BLOCK + (threadIdx.x >> 5);
+    const int64_t group = group_of_thread();
     if (group >= g.count) return;
     const Place p = place_of(g, group, threadIdx.x & 31);
     float v[4];
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(THREADS) void k_checkpoint_read(Groups g, const int
 template <typename TX, typename TY, bool ERF, bool KEPT>
 __global__ __launch_bounds__(THREADS) void k_gelu(Groups g, const TX* __restrict__ x, TY* __restrict__ y, int8_t* __restrict__ codes, float* __restrict__ units) {
     const int lane = threadIdx.x & 31;
-    const int64_t group = (int64_t)blockIdx.x * GROUPS_A_BLOCK + (threadIdx.x >> 5);
+    const int64_t group = group_of_thread();
     if (group >= g.count) return;
     const Place p = place_of(g, group, lane);
     float v[4], a[4], slope;
@@ -103,7 +106,7 @@ __global__ __launch_bounds__(THREADS) void k_gelu(Groups g, const TX* __restrict
 // TX int8_t: from what was kept.  (dx may be dy: a lane has read its numbers before it writes them.)
 template <typename TX, typename TG, typename TD, typename TY, bool ERF>
 __global__ __launch_bounds__(THREADS) void k_gelu_bwd(Groups g, const TX* __restrict__ x, const float* __restrict__ units, const TG* dy, TD* dx, TY* __restrict__ y) {
-    const int64_t group = (int64_t)blockIdx.x * GROUPS_A_BLOCK + (threadIdx.x >> 5);
+    const int64_t group = group_of_thread();
     if (group >= g.count) return;
     const Place p = place_of(g, group, threadIdx.x & 31);
     float v[4], d[4], a[4];
@@ -129,7 +132,10 @@ int check_gelu(const mst_gelu_shape* s) {
     return check_rows(s->rows, s->width);
 }
 bool given(const void* p) { return p && aligned16(p); }
-unsigned blocks_of(const Groups& g) { return (unsigned)cdiv(g.count, GROUPS_A_BLOCK); }
+dim3 blocks_of(const Groups& g) {
+    const int64_t blocks = cdiv(g.count, GROUPS_A_BLOCK);
+    return dim3((unsigned)std::min<int64_t>(blocks, BLOCKS_ALONG), (unsigned)cdiv(blocks, BLOCKS_ALONG));
+}
 
 // f(a number of the type)
 template <typename F>

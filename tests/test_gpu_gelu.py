@@ -152,3 +152,32 @@ def test_more_than_2_31_numbers():
     at = rest.kept(c, u).astype(np.float64)
     _within(x[-2:], wide(last) * rest.gelu(at, 0)[1], np.abs(wide(last)) * (_bounds(at, 0)[1] + U), "bf16")
     assert (x[:3] == 0).all()
+
+
+def test_more_than_2_34_numbers():
+    rows, width = 2 ** 22 + 5, 4096                                 # more groups than a launch has half wavefronts
+    x = torch.zeros(rows, width, dtype=torch.bfloat16, device=DEV)
+    x[-3:] = torch.randn(3, width, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).bfloat16()
+    codes, units = torch.empty(rows, width, dtype=torch.int8, device=DEV), torch.empty(rows, 32, device=DEV)
+    kept = mst.Checkpoint8(codes, units)
+    mst.mst_checkpoint_write(rows, width, x, mst.MST_BF16, kept)
+    torch.cuda.synchronize()
+    c, u = rest.keep(x[-3:].float().cpu().numpy())
+    np.testing.assert_array_equal(codes[-3:].cpu().numpy(), c)
+    np.testing.assert_array_equal(units[-3:].cpu().numpy(), u)
+    assert not codes[:-3].any()
+    last = x[-3:].clone()
+    mst.mst_checkpoint_read(rows, width, kept, mst.MST_BF16, x)
+    torch.cuda.synchronize()
+    assert torch.equal(x[-3:], torch.from_numpy(rest.kept(c, u)).bfloat16().to(DEV))
+    x[-3:] = last
+    mst.mst_gelu_bwd(mst.GeluShape(rows, width, 0, 1, 1, 1, 1), None, kept, x, x, None)
+    torch.cuda.synchronize()
+    at = rest.kept(c, u).astype(np.float64)
+    _within(x[-3:], wide(last) * rest.gelu(at, 0)[1], np.abs(wide(last)) * (_bounds(at, 0)[1] + U), "bf16")
+    y = codes = units = kept = None
+    y = torch.empty_like(x)
+    x[-3:] = last
+    mst.mst_gelu_fwd(mst.GeluShape(rows, width, 0, 1, 1, 1, 1), x, y)
+    torch.cuda.synchronize()
+    _within(y[-3:], rest.gelu(wide(last), 0)[0], _bounds(wide(last), 0)[0], "bf16")
