@@ -196,6 +196,11 @@ constexpr int stores_behind(Epilogue E) { return E == LOGIT_GRAD || E == LOGIT_G
 // after that, stand one by one between its 64 matrix instructions.  Steps come in pairs, of which the second waits for the pair behind it:
 //   first   products of its first half, reads of its second half, loads of the next pair but one: A
 //   second  waits; products of its second half, reads of the next pair's first half, loads of the next pair but one: B
+// 8192 tokens, width 1280, vocabulary 50257 (1054 GFLOP a product): statistics 879 us, 1200 TFLOP/s; dz 1052 (two pieces), 1002; dh 898, 1174; dE 876, 1203; the library's 8192^3 product
+// reaches 1191.  Matrix instructions are busy in 70 % of the clocks (dz, whose 64 stores and exponentials of a tile hide behind nothing: 56), at some 1.8 GHz.  Of 768 tokens of width 768
+// 591 tiles take three rounds of the 256 CUs: statistics 68 us, 870 TFLOP/s; dz 86, dh 68, dE 85.
+// What bounds the loop is the way of the loads into LDS, 64 KB a pair of steps and CU: 128 x 128 tiles (twice the loads a product) took 7.4 ms for the whole of the above, not 3.6;
+// results that leave for memory and loads that begin only then 4.46, workgroups that stay and load ahead 4.25.
 constexpr int L_PAIR = 2 * VK, L_STAGE = VT * L_PAIR * 2, L_STAGES = 5;
 constexpr unsigned L_LDS = L_STAGES * L_STAGE;
 
@@ -438,7 +443,8 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
 
 // ---- the same tiles for numbers of three parts: six products of each step of 32 indices
 // The parts of a step are in LDS once, 16 KB each, and a part stays in registers for the products that follow one another with it: seven reads of operands instead of
-// twelve, and half of the bytes from memory that six separate products would take, which bound them (1378 tokens, width 648, vocabulary 32003: statistics 317 us).
+// twelve, and half of the bytes from memory that six separate products would take, which bound them (1378 tokens, width 648, vocabulary 32003, forward and gradients: 1.64 ms, this way 1.35).
+// Now, of 343 GFLOP each: statistics 291 us, dz 372, dh 310, dE 363; matrix instructions are busy in 83 % of the clocks (dz 63).
 //   product   a2 b0   a1 b0   a0 b0   a0 b2   a0 b1   a1 b1        register set of a, of b:  0 Q   1 Q   0 Q   0 1-Q   0 Q   1 Q
 //   reads     a1      a0      b2      b1      a1      b0, a2 of the next step
 //   loads     b0      a2      a1      a0      b2      b1  of the next step
@@ -665,6 +671,9 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
 // Operands come as the products want them, 16 bytes of a row to a lane; which four (or eight) contraction indices a lane has is free as long as both operands agree.  Logits of bfloat16 numbers
 // on the bfloat16 instructions, everything else in fp32 on its own (16 x 16 x 4): dz is not rounded, and nothing is split into parts.
 // A lane has row (column) l % 16 and the indices of l / 16.
+// Vocabulary 50257, width 768: of 8 bfloat16 tokens logits take 21 us (77 MB, 3.7 TB/s), of 8 in fp32 39 (154 MB, 4.0 TB/s), dh 26 (5.9 TB/s), dE 32 (4.8); of 40 in fp32 104, 74 and 72: there the
+// hidden states (and dz) come from the caches four times as often as the embedding, and bound it.  Handing them round in LDS was slower (160), and so were loads of the next tokens
+// under the present products of dE (96: half the wavefronts).
 __device__ __forceinline__ void four(const bf16* p, bool there, float (&x)[4]) {
     uint2 w = make_uint2(0, 0);
     if (there) w = *reinterpret_cast<const uint2*>(p);

@@ -68,7 +68,9 @@ int vocab_splits(int m, int n, int k);   // ranges of the contraction for vocab_
 // and both gradients from it (either may be null), dh by way of sums [vocab_few_ranges][tokens][width]
 constexpr int VOCAB_FEW_COLUMNS = 64;
 __host__ __device__ constexpr int64_t few_pitch(int vocab) { return ((int64_t)vocab + VOCAB_FEW_COLUMNS - 1) / VOCAB_FEW_COLUMNS * VOCAB_FEW_COLUMNS; }
-constexpr int VOCAB_FEW_BF16 = 32, VOCAB_FEW_F32 = 64;
+// Width 768, vocabulary 50257, forward / forward and gradients in us, this way and by the tiles of 256 x 256:
+//   bf16, 16 tokens: 29 / 105 and 37 / 149; 24: 36 / 147 and 37 / 149.      fp32, 40: 104 / 356 and 166 / 550; 64: 115 / 402 and 167 / 554; 128: 195 / 695 and 166 / 558.
+constexpr int VOCAB_FEW_BF16 = 24, VOCAB_FEW_F32 = 64;
 inline bool vocab_is_few(const mst_vocab_loss_shape& s) { return s.tokens <= (s.type == MST_F32 ? VOCAB_FEW_F32 : VOCAB_FEW_BF16); }
 int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream);
 int vocab_few_ranges(const mst_vocab_loss_shape& s);

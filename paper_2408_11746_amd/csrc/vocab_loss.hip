@@ -8,12 +8,17 @@
 // pads their rows to whole steps of the products.  fp32 numbers are split into three bfloat16 parts on the way, those of the embedding
 // a piece at a time.
 // The logit of a token's own label is a dot product of its own in fp32, and so is what it adds to dz: exp(z - lse) - 1 without cancellation.
+// The products bound it (vocab_gemm.hip).  What is here takes, of 8192 bfloat16 tokens of width 1280 and a vocabulary of 50257 (3560 us with the gradients): rows 16, packing 13 (both
+// in either direction), join 8, dh 32; of 1024 tokens of width 768 (338 us): 5, 6, 7 and 10.
+// Few tokens (vocab_is_few) go neither through the packing nor through pieces.
 #include "rows.h"
 #include "vocab_loss.h"
 
 namespace mst {
 namespace {
 
+// Of dz and of the embedding's parts.  Every piece costs its launches and a last round of tiles that is not full, and takes up the sums for dh again: with 512 MB 8192 tokens of width 1280,
+// vocabulary 50257, have two pieces and take 3.56 ms, with 256 MB four and 3.68; fp32, 1531 tokens of width 648, vocabulary 32003, one and 1.29, two and 1.40.
 constexpr int64_t PIECE_BYTES = int64_t(1) << 29;
 
 // ---- which tokens have a label
@@ -143,7 +148,7 @@ __global__ __launch_bounds__(256) void k_vocab_pack(const T* __restrict__ h, con
     }
 }
 
-// rows of a piece of the embedding in parts, padded with zeros to `ld` columns and to whole steps of rows
+// rows of a piece of the embedding in parts, padded with zeros to `ld` columns and to whole steps of rows.  Bound by memory: 50257 x 768 fp32 numbers in 62 us (386 MB, 6.2 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void k_vocab_parts(const T* __restrict__ E, int rows, int padded, int W, uint16_t* __restrict__ to, int64_t plane, int ld, int planes) {
     const int64_t quads = (int64_t)padded * (ld / 4);
@@ -194,6 +199,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_vocab_join(const float2* __res
 }
 
 // gradients of the hidden states: sums of the splits, back to the tokens' places; a wavefront takes blocks of 16 rows and 16 columns, or a workgroup's four share one
+// (128 tokens of width 768, 64 splits: 33 us with a wavefront to a block, 7 with four)
 template <typename T, bool SHARE>
 __global__ __launch_bounds__(256) void k_vocab_dh(const float* __restrict__ sums, int64_t stride, int wide, int splits, const int* __restrict__ count, const int* __restrict__ list,
                                                   const float* __restrict__ unit, int W, T* __restrict__ dh) {
