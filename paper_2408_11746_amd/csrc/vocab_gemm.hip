@@ -187,8 +187,12 @@ __device__ __forceinline__ void finish(const VocabOutOf<T>& e, const VocabProduc
     else put(std::true_type{});
 }
 
-// Of the stores of a unit's results, so many are issued whatever the unit holds (dz: 64 or more, as many as the counter of outstanding accesses can tell apart)
-constexpr int stores_behind(Epilogue E) { return E == LOGIT_GRAD || E == LOGIT_GRAD_PARTS ? 52 : 0; }
+// Of the stores of a unit's results, so many are issued whatever the unit holds (dz: one a product of 16 x 16 and part; 52: as many as the counter of outstanding accesses can
+// tell apart beside the loads)
+constexpr int stores_behind(Epilogue E, int products) {
+    const int stores = E == LOGIT_GRAD ? products : E == LOGIT_GRAD_PARTS ? PLANES_MAX * products : 0;
+    return stores < 52 ? stores : 52;
+}
 
 // ---- 256 x 256 tiles, four wavefronts of 128 x 128, the sums in the accumulation half of the registers
 // A stage of LDS is 64 contraction indices of one operand, 32 KB, so that rows of memory are read in whole lines of 128 bytes; five of them, A and B in turn.
@@ -201,27 +205,29 @@ constexpr int stores_behind(Epilogue E) { return E == LOGIT_GRAD || E == LOGIT_G
 // 591 tiles take three rounds of the 256 CUs: statistics 68 us, 870 TFLOP/s; dz 86, dh 68, dE 85.
 // What bounds the loop is the way of the loads into LDS, 64 KB a pair of steps and CU: 128 x 128 tiles (twice the loads a product) took 7.4 ms for the whole of the above, not 3.6;
 // results that leave for memory and loads that begin only then 4.46, workgroups that stay and load ahead 4.25.
-constexpr int L_PAIR = 2 * VK, L_STAGE = VT * L_PAIR * 2, L_STAGES = 5;
-constexpr unsigned L_LDS = L_STAGES * L_STAGE;
+constexpr int L_PAIR = 2 * VK, L_STAGES = 5;
+constexpr int l_stage(int side) { return side * L_PAIR * 2; }
 
 // The 16-byte units (eight indices) of a row of an operand along are kept at unit ^ mix(row): sixteen rows of a read cover all banks
 __device__ __forceinline__ int pair_mix(int row) { return (row >> 1) & 7; }
 
-// One operand's share of a wavefront's loads: eight pieces of 1 KB a stage
-template <bool ALONG>
-struct LargeLoads {
-    uint32_t v[8];
+// One operand's share of a wavefront's loads
+template <bool ALONG, int SIDE>
+struct TileLoads {
+    static constexpr int PIECES = SIDE / 32;        // of 1 KB, a stage's
+    uint32_t v[PIECES];
     const char* base;                    // of the pair
     __device__ __forceinline__ void aim_rows(const VocabOperand& o, int first, int wave, int lane, int left, int turn) {
         const uint32_t row_bytes = 2u * (uint32_t)o.ld;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int piece = 8 * wave + (j ^ turn);
+        for (int j = 0; j < PIECES; ++j) {
+            const int piece = PIECES * wave + (j ^ turn);
             if constexpr (ALONG) {
                 const int row = 8 * piece + (lane >> 3), u = (lane & 7) ^ pair_mix(row);
                 v[j] = (uint32_t)min(row, o.rows - 1 - first) * row_bytes + 16u * u;
             } else {                     // left: contraction indices from this pair on
-                const int k = 2 * piece + (lane >> 5), col = 16 * (((lane & 31) >> 1) ^ across_swizzle(k)) + 8 * (lane & 1);
+                constexpr int WORDS = SIDE / 8;      // of 16 bytes, of a contraction index
+                const int k = 64 / WORDS * piece + lane / WORDS, col = 16 * ((lane % WORDS >> 1) ^ across_swizzle(k)) + 8 * (lane & 1);
                 v[j] = (uint32_t)min(k, left - 1) * row_bytes + 2u * (uint32_t)min((int64_t)col, o.ld - 8 - first);
             }
         }
@@ -229,14 +235,15 @@ struct LargeLoads {
     __device__ __forceinline__ void aim_pair(const VocabOperand& o, int first, int t) {
         base = reinterpret_cast<const char*>(ALONG ? o.p + (int64_t)first * o.ld + t * L_PAIR : o.p + (int64_t)t * L_PAIR * o.ld + first);
     }
-    // to: the wavefront's 8 KB of the stage (a multiple of that) ^ 1024 turn; the j-th load is of piece j ^ turn
+    // to: the wavefront's share of the stage (a multiple of its size) ^ 1024 turn; the j-th load is of piece j ^ turn
     __device__ __forceinline__ void piece(int j, uint32_t to) const { load_to_lds(base, v[j], to ^ 1024u * j); }
 };
-// ... and of its reads: eight operands of sixteen rows (or columns) a step, of half `step` of a stage
-template <bool ALONG>
-struct LargeReads {
-    uint32_t at[ALONG ? 2 : 8];
-    __device__ __forceinline__ LargeReads(int first, int lane) {
+// ... and of its reads: operands of sixteen rows (or columns) a step, of half `step` of a stage
+template <bool ALONG, int SIDE>
+struct TileReads {
+    static constexpr int TILES = SIDE / 32;
+    uint32_t at[ALONG ? 2 : TILES];
+    __device__ __forceinline__ TileReads(int first, int lane) {
         if constexpr (ALONG) {
             const int row = first + (lane & 15);
 #pragma unroll
@@ -244,7 +251,7 @@ struct LargeReads {
         } else {
             const int k = 8 * (lane >> 4) + ((lane >> 2) & 3);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) at[i] = (uint32_t)(k * 512 + (((first / 16 + i) ^ across_swizzle(k)) << 5) + (lane & 3) * 8);
+            for (int i = 0; i < TILES; ++i) at[i] = (uint32_t)(k * SIDE * 2 + (((first / 16 + i) ^ across_swizzle(k)) << 5) + (lane & 3) * 8);
         }
     }
     // half h of operand i; along, the first is all of it
@@ -253,7 +260,7 @@ struct LargeReads {
         if constexpr (ALONG) {
             if (h == 0) whole = *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)(stage + at[STEP] + 2048u * i));
         } else {
-            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)(stage + at[i] + 16384u * STEP + 2048u * h));
+            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)(stage + at[i] + 64u * SIDE * STEP + 8u * SIDE * h));
             if (h == 1) whole = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
@@ -262,13 +269,14 @@ struct LargeReads {
 // Units are (tile, range of the contraction), range by range.  XCD x takes a contiguous share of them, its workgroups in turn, so that what runs there at a time
 // reads the same operands.
 struct Unit { int m0, n0, split, kb, ke; };      // (range in pairs of steps)
+template <int SIDE>
 struct Units {
     int m_rows, gm, gn, ntiles, k_all, splits, next, end, each;
     __device__ __forceinline__ Units(const VocabProduct& p) {
         m_rows = p.m_count ? *p.m_count : p.m;
         k_all = ((p.k_count ? *p.k_count : p.k) + L_PAIR - 1) / L_PAIR;
-        gm = (m_rows + VT - 1) / VT;
-        gn = (p.n + VT - 1) / VT;
+        gm = (m_rows + SIDE - 1) / SIDE;
+        gn = (p.n + SIDE - 1) / SIDE;
         ntiles = gm * gn;
         splits = p.splits;
         const int units = ntiles * splits, Q = (units + 7) >> 3;
@@ -281,27 +289,29 @@ struct Units {
         int mi, ni;
         tile_coords(u - split * ntiles, gm, gn, mi, ni);
         auto uniform = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
-        return Unit{uniform(mi * VT), uniform(ni * VT), uniform(split), uniform((int)((int64_t)split * k_all / splits)), uniform((int)((int64_t)(split + 1) * k_all / splits))};
+        return Unit{uniform(mi * SIDE), uniform(ni * SIDE), uniform(split), uniform((int)((int64_t)split * k_all / splits)), uniform((int)((int64_t)(split + 1) * k_all / splits))};
     }
 };
 
-template <bool A_ALONG, bool B_ALONG, Epilogue E>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
+template <int SIDE, bool A_ALONG, bool B_ALONG, Epilogue E>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIDE == 256 ? 1 : 2, SIDE == 256 ? 1 : 2)))
+void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
-    const Units units(p);
+    constexpr int N = SIDE / 32, PIECES = N, STAGE = l_stage(SIDE);      // products a wavefront and side; pieces of its loads of a stage
+    constexpr int BEHIND = stores_behind(E, N * N);
+    const int wm = (wave >> 1) * (SIDE / 2), wn = (wave & 1) * (SIDE / 2);
+    const Units<SIDE> units(p);
     const int m_rows = units.m_rows, k_all = units.k_all, end = units.end, each = units.each;
     int unit = units.next;
     if (unit >= end) return;
     auto decode = [&](int u) __attribute__((always_inline)) { return units.decode(u); };
-    floatx4 acc[8][8];
+    floatx4 acc[N][N];
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < N; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     };
     if (k_all == 0) {                     // a batch without labels
         clear();
@@ -315,10 +325,10 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
 
     // Workgroups that share rows of an operand begin with different pieces of them, so that each meets what another has fetched already.  Loss and gradients of 8192 tokens,
     // width 1280, vocabulary 50257: 4.21 -> 3.9 ms; of 768 tokens, width 768, where three share what they read from memory: 366 -> 378 us.
-    auto turn = [&](int first) __attribute__((always_inline)) { return first / VT & 7; };
+    auto turn = [&](int first) __attribute__((always_inline)) { return first / SIDE & (PIECES - 1); };
     // The loads run two pairs ahead of the products, into the next unit where the present one ends, so that only the first has to wait for them
-    LargeLoads<A_ALONG> la;
-    LargeLoads<B_ALONG> lb;
+    TileLoads<A_ALONG, SIDE> la;
+    TileLoads<B_ALONG, SIDE> lb;
     // An operand that is read across ends inside its last pair only where it is the caller's own embedding: rows past its end are its last
     const int tail = B_ALONG ? L_PAIR : p.b.rows - (k_all - 1) * L_PAIR;
     Unit ahead;
@@ -342,27 +352,27 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
             enter = true;
         }                                 // (behind the last pair of all: that again, for nobody)
     };
-    const uint32_t mine = 8192u * wave;
-    auto next = [&](uint32_t stage) __attribute__((always_inline)) { return stage == (L_STAGES - 1) * L_STAGE ? 0u : stage + L_STAGE; };
-    const LargeReads<A_ALONG> ra(wm, lane);
-    const LargeReads<B_ALONG> rb(wn, lane);
-    bf16x8 a[2][8], b[2][8];
+    const uint32_t mine = 1024u * PIECES * wave;
+    auto next = [&](uint32_t stage) __attribute__((always_inline)) { return stage == (L_STAGES - 1) * STAGE ? 0u : stage + STAGE; };
+    const TileReads<A_ALONG, SIDE> ra(wm, lane);
+    const TileReads<B_ALONG, SIDE> rb(wn, lane);
+    bf16x8 a[2][N], b[2][N];
     // products from register set SET; half 1 - SET of the stages sa, sb goes to the other set, a stage's loads to `to`.  (The products by hand: the compiler would keep
     // some of the sums outside the accumulation registers and spill.)
     auto step = [&](auto set, auto fresh, uint32_t sa, uint32_t sb, uint32_t to) __attribute__((always_inline)) {
         constexpr int P = decltype(set)::value;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             shortx4 pa[2], pb[2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 if constexpr (decltype(fresh)::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b[P][j]), "v"(a[P][i]));
                 else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b[P][j]), "v"(a[P][i]));
                 if (j == 0) rb.template half<1 - P>(sb, i, 0, b[P ^ 1][i], pb);
                 if (j == 1) rb.template half<1 - P>(sb, i, 1, b[P ^ 1][i], pb);
-                if (j == 3) ra.template half<1 - P>(sa, i, 0, a[P ^ 1][i], pa);
-                if (j == 4) ra.template half<1 - P>(sa, i, 1, a[P ^ 1][i], pa);
-                if (j == 6) {
+                if (j == N / 2 - 1) ra.template half<1 - P>(sa, i, 0, a[P ^ 1][i], pa);
+                if (j == N / 2) ra.template half<1 - P>(sa, i, 1, a[P ^ 1][i], pa);
+                if (j == N - 2) {
                     if constexpr (P == 0) la.piece(i, to);
                     else lb.piece(i, to);
                 }
@@ -371,27 +381,27 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
         }
     };
 
-    uint32_t sa = lds0, sb = lds0 + L_STAGE, to = lds0 + mine;      // of the present pair; of the loads
+    uint32_t sa = lds0, sb = lds0 + STAGE, to = lds0 + mine;      // of the present pair; of the loads
     for (int d = 0; d < 2; ++d) {
         aim();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) la.piece(j, to ^ 1024 * turn(ahead.n0));
-        to += L_STAGE;
+        for (int j = 0; j < N; ++j) la.piece(j, to ^ 1024 * turn(ahead.n0));
+        to += STAGE;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) lb.piece(j, to ^ 1024 * turn(ahead.m0));
-        to += L_STAGE;
+        for (int j = 0; j < N; ++j) lb.piece(j, to ^ 1024 * turn(ahead.m0));
+        to += STAGE;
     }
-    wait_loads<16>();
+    wait_loads<2 * PIECES>();
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
         shortx4 pa[2], pb[2];
         rb.template half<0>(sb, i, 0, b[0][i], pb);
         rb.template half<0>(sb, i, 1, b[0][i], pb);
         ra.template half<0>(sa, i, 0, a[0][i], pa);
         ra.template half<0>(sa, i, 1, a[0][i], pa);
     }
-    uint32_t at = 4 * L_STAGE, na = 2 * L_STAGE, nb = 3 * L_STAGE;  // stage that is loaded next, and those of the next pair
+    uint32_t at = 4 * STAGE, na = 2 * STAGE, nb = 3 * STAGE;  // stage that is loaded next, and those of the next pair
     auto first = [&](auto fresh) __attribute__((always_inline)) {
         aim();
         step(std::integral_constant<int, 0>{}, fresh, sa, sb, (lds0 + at + mine) ^ 1024 * turn(ahead.n0));
@@ -418,24 +428,24 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
         }
         // The next pair is in LDS, and everyone has read this one.  Behind its loads only the stage above may be on its way; behind a unit also the stores of
         // its results, which were issued after them.
-        if (stores_behind(E) > 0 && stored) wait_loads<8 + stores_behind(E)>();
-        else wait_loads<8>();
+        if (BEHIND > 0 && stored) wait_loads<PIECES + BEHIND>();
+        else wait_loads<PIECES>();
         stored = true;
         lds_barrier();
         second();
 #pragma unroll 1
         for (int d = 1; d < pairs; ++d) {
             first(std::false_type{});
-            wait_loads<8>();
+            wait_loads<PIECES>();
             lds_barrier();
             second();
         }
         // the last product is 18 wait states from its result
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+            for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));
         finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
@@ -449,23 +459,25 @@ void k_vocab_large(const VocabProduct p, const typename EpilogueArgs<E>::type e)
 //   reads     a1      a0      b2      b1      a1      b0, a2 of the next step
 //   loads     b0      a2      a1      a0      b2      b1  of the next step
 // Ten stages: a part is loaded six products before the one that has its number in this order, and waited for every other product.
-constexpr int Q_STAGE = VT * VK * 2, Q_STAGES = 10;
-constexpr unsigned Q_LDS = Q_STAGES * Q_STAGE;
+constexpr int Q_STAGES = 10;
+constexpr int q_stage(int side) { return side * VK * 2; }
 
-template <bool ALONG>
+template <bool ALONG, int SIDE>
 struct PartLoads {
-    uint32_t v[4];
+    static constexpr int PIECES = SIDE / 64;        // of 1 KB, a wavefront's of a stage
+    uint32_t v[PIECES];
     const char* base;                    // of part 0 of the step
     __device__ __forceinline__ void aim_rows(const VocabOperand& o, int first, int wave, int lane, int turn) {
         const uint32_t row_bytes = 2u * (uint32_t)o.ld;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int piece = 4 * wave + (j ^ turn);
+        for (int j = 0; j < PIECES; ++j) {
+            const int piece = PIECES * wave + (j ^ turn);
             if constexpr (ALONG) {
                 const int rho = lane >> 2, row = 16 * piece + (((rho & 3) << 2) | (rho >> 2)), u = ((lane & 3) ^ (rho >> 2)) & 3;
                 v[j] = (uint32_t)min(row, o.rows - 1 - first) * row_bytes + 16u * u;
             } else {
-                const int k = 2 * piece + (lane >> 5), col = 16 * (((lane & 31) >> 1) ^ across_swizzle(k)) + 8 * (lane & 1);
+                constexpr int WORDS = SIDE / 8;      // of 16 bytes, of a contraction index
+                const int k = 64 / WORDS * piece + lane / WORDS, col = 16 * ((lane % WORDS >> 1) ^ across_swizzle(k)) + 8 * (lane & 1);
                 v[j] = (uint32_t)k * row_bytes + 2u * (uint32_t)min((int64_t)col, o.ld - 8 - first);
             }
         }
@@ -473,46 +485,49 @@ struct PartLoads {
     __device__ __forceinline__ void aim_step(const VocabOperand& o, int first, int t) {
         base = reinterpret_cast<const char*>(ALONG ? o.p + (int64_t)first * o.ld + t * VK : o.p + (int64_t)t * VK * o.ld + first);
     }
-    // to: the wavefront's 4 KB of the stage ^ 1024 turn
+    // to: the wavefront's share of the stage ^ 1024 turn
     __device__ __forceinline__ void piece(int j, int64_t part_bytes, uint32_t to) const { load_to_lds(base + part_bytes, v[j], to ^ 1024u * j); }
 };
-template <bool ALONG>
+template <bool ALONG, int SIDE>
 struct PartReads {
-    uint32_t at[ALONG ? 1 : 8];
+    static constexpr int TILES = SIDE / 32;         // of sixteen rows (or columns), a wavefront's
+    uint32_t at[ALONG ? 1 : TILES];
     __device__ __forceinline__ PartReads(int first, int lane) {
         if constexpr (ALONG) {
             at[0] = along_unit(first + (lane & 15), lane >> 4);
         } else {
             const int k = 8 * (lane >> 4) + ((lane >> 2) & 3);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) at[i] = (uint32_t)(k * 512 + (((first / 16 + i) ^ across_swizzle(k)) << 5) + (lane & 3) * 8);
+            for (int i = 0; i < TILES; ++i) at[i] = (uint32_t)(k * SIDE * 2 + (((first / 16 + i) ^ across_swizzle(k)) << 5) + (lane & 3) * 8);
         }
     }
     __device__ __forceinline__ void half(uint32_t stage, int i, int h, bf16x8& whole, shortx4 (&part)[2]) const {
         if constexpr (ALONG) {
             if (h == 0) whole = *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)(stage + at[0] + 1024u * i));
         } else {
-            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)(stage + at[i] + 2048u * h));
+            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4)(uintptr_t)(stage + at[i] + 8u * SIDE * h));
             if (h == 1) whole = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
 };
 
-template <bool A_ALONG, bool B_ALONG, Epilogue E>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
+template <int SIDE, bool A_ALONG, bool B_ALONG, Epilogue E>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SIDE == 256 ? 1 : 2, SIDE == 256 ? 1 : 2)))
+void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
-    const Units units(p);
+    constexpr int N = SIDE / 32, PIECES = SIDE / 64, STAGE = q_stage(SIDE);         // products a wavefront and side; pieces of its loads of a part
+    constexpr int BEHIND = stores_behind(E, N * N);
+    const int wm = (wave >> 1) * (SIDE / 2), wn = (wave & 1) * (SIDE / 2);
+    const Units<SIDE> units(p);
     const int m_rows = units.m_rows, end = units.end, each = units.each;
     int unit = units.next;
     if (unit >= end) return;
-    floatx4 acc[8][8];
+    floatx4 acc[N][N];
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < N; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     };
     if (units.k_all == 0) {               // a batch without labels
         clear();
@@ -526,12 +541,12 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
     // The loads run a step ahead of the products, into the next unit where the present one ends.  (Every operand is in the workspace, padded to whole pairs of steps.)
-    PartLoads<A_ALONG> la;
-    PartLoads<B_ALONG> lb;
+    PartLoads<A_ALONG, SIDE> la;
+    PartLoads<B_ALONG, SIDE> lb;
     Unit ahead;
     int ahead_unit = unit, at_t;
     bool enter = true;
-    auto turn = [&](int first) __attribute__((always_inline)) { return first / VT & 3; };
+    auto turn = [&](int first) __attribute__((always_inline)) { return first / SIDE & (PIECES - 1); };
     auto aim = [&]() __attribute__((always_inline)) {
         if (enter) {
             ahead = units.decode(ahead_unit);
@@ -550,26 +565,26 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
         }                                 // (behind the last step of all: that again, for nobody)
     };
     const int64_t plane_a = 2 * p.a.plane, plane_b = 2 * p.b.plane;
-    const uint32_t mine = 4096u * wave;
+    const uint32_t mine = 1024u * PIECES * wave;
     int base = 0;                                                   // stage of the present step's first part
     auto stage = [&](int n) __attribute__((always_inline)) {        // of part n from there on
         const int x = base + n;
-        return lds0 + (uint32_t)(x >= Q_STAGES ? x - Q_STAGES : x) * Q_STAGE;
+        return lds0 + (uint32_t)(x >= Q_STAGES ? x - Q_STAGES : x) * STAGE;
     };
     // where the wavefront's loads of part n (of the next step: n + 6) go
     auto to_a = [&](int n) __attribute__((always_inline)) { return (stage(n) + mine) ^ 1024 * turn(ahead.n0); };
     auto to_b = [&](int n) __attribute__((always_inline)) { return (stage(n) + mine) ^ 1024 * turn(ahead.m0); };
-    const PartReads<A_ALONG> ra(wm, lane);
-    const PartReads<B_ALONG> rb(wn, lane);
-    bf16x8 a[2][8], b[2][8];
+    const PartReads<A_ALONG, SIDE> ra(wm, lane);
+    const PartReads<B_ALONG, SIDE> rb(wn, lane);
+    bf16x8 a[2][N], b[2][N];
     // products of sets AS and BS; what stage sa (sb) holds goes to set RA (RB; -1: nothing is read), part `part` of an operand to `to`
     auto product = [&](auto as, auto bs, auto fresh, auto ra_set, uint32_t sa, auto rb_set, uint32_t sb, auto of_a, int part, uint32_t to) __attribute__((always_inline)) {
         constexpr int AS = decltype(as)::value, BS = decltype(bs)::value, RA = decltype(ra_set)::value, RB = decltype(rb_set)::value;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             shortx4 pa[2], pb[2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 if constexpr (decltype(fresh)::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b[BS][j]), "v"(a[AS][i]));
                 else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b[BS][j]), "v"(a[AS][i]));
                 if constexpr (RB >= 0) {
@@ -577,10 +592,10 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
                     if (j == 1) rb.half(sb, i, 1, b[RB][i], pb);
                 }
                 if constexpr (RA >= 0) {
-                    if (j == 3) ra.half(sa, i, 0, a[RA][i], pa);
-                    if (j == 4) ra.half(sa, i, 1, a[RA][i], pa);
+                    if (j == N / 2 - 1) ra.half(sa, i, 0, a[RA][i], pa);
+                    if (j == N / 2) ra.half(sa, i, 1, a[RA][i], pa);
                 }
-                if (j == 6 && (i & 1)) {
+                if (j == N - 2 && (i & 1)) {
                     if constexpr (decltype(of_a)::value) la.piece(i >> 1, part * plane_a, to);
                     else lb.piece(i >> 1, part * plane_b, to);
                 }
@@ -594,8 +609,8 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
     constexpr std::true_type yes;
     constexpr std::false_type no;
     auto meet = [&](bool stored) __attribute__((always_inline)) {   // the parts of this product and the next are in LDS, and everyone is done with the last two
-        if (stores_behind(E) > 0 && stored) wait_loads<8 + stores_behind(E)>();
-        else wait_loads<8>();
+        if (BEHIND > 0 && stored) wait_loads<2 * PIECES + BEHIND>();
+        else wait_loads<2 * PIECES>();
         lds_barrier();
     };
     auto step = [&](auto q, auto fresh, bool stored) __attribute__((always_inline)) {
@@ -617,21 +632,21 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
 
     aim();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) lb.piece(j, 0, to_b(0));
+    for (int j = 0; j < PIECES; ++j) lb.piece(j, 0, to_b(0));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) la.piece(j, 2 * plane_a, to_a(1));
+    for (int j = 0; j < PIECES; ++j) la.piece(j, 2 * plane_a, to_a(1));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) la.piece(j, plane_a, to_a(2));
+    for (int j = 0; j < PIECES; ++j) la.piece(j, plane_a, to_a(2));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) la.piece(j, 0, to_a(3));
+    for (int j = 0; j < PIECES; ++j) la.piece(j, 0, to_a(3));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) lb.piece(j, 2 * plane_b, to_b(4));
+    for (int j = 0; j < PIECES; ++j) lb.piece(j, 2 * plane_b, to_b(4));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) lb.piece(j, plane_b, to_b(5));
-    wait_loads<16>();
+    for (int j = 0; j < PIECES; ++j) lb.piece(j, plane_b, to_b(5));
+    wait_loads<4 * PIECES>();
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
         shortx4 pa[2], pb[2];
         rb.half(stage(0), i, 0, b[0][i], pb);
         rb.half(stage(0), i, 1, b[0][i], pb);
@@ -659,9 +674,9 @@ void k_vocab_large_parts(const VocabProduct p, const typename EpilogueArgs<E>::t
         // the last product is 18 wait states from its result
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+            for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));
         finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
@@ -900,32 +915,31 @@ __global__ __launch_bounds__(256) void k_vocab_few_dE(const float* __restrict__ 
 // f(a number of the type, tiles of sixteen tokens)
 template <typename F>
 void with_few(const mst_vocab_loss_shape& s, F&& f) {
-    auto sized = [&](auto type) {
-        if (s.tokens <= 16) f(type, std::integral_constant<int, 1>{});
-        else f(type, std::integral_constant<int, 2>{});
-    };
-    if (s.type == MST_BF16) sized(bf16{});
-    else if (s.tokens <= 32) sized(float{});
+    if (s.type == MST_BF16) f(bf16{}, std::integral_constant<int, 1>{});
+    else if (s.tokens <= 16) f(float{}, std::integral_constant<int, 1>{});
+    else if (s.tokens <= 32) f(float{}, std::integral_constant<int, 2>{});
     else f(float{}, std::integral_constant<int, 4>{});
 }
-static_assert(VOCAB_FEW_BF16 <= 32 && VOCAB_FEW_F32 <= 64);
+static_assert(VOCAB_FEW_BF16 <= 16 && VOCAB_FEW_F32 <= 64);
 
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipStream_t s) {
-    // (one to a CU)
-    const unsigned grid = (unsigned)std::min<int64_t>(256, 8 * cdiv(cdiv(p.m, VT) * cdiv(p.n, VT) * p.splits, 8));
-    auto run = [&](auto kernel, unsigned bytes, uint64_t& done) {
+    // (as many as the CUs hold: one of 256 x 256, two of 128 x 128)
+    auto run = [&](auto kernel, int side, unsigned bytes, uint64_t& done) {
+        const unsigned grid = (unsigned)std::min<int64_t>(side == VT ? 256 : 512, 8 * cdiv(cdiv(p.m, side) * cdiv(p.n, side) * p.splits, 8));
         if (int rc = allow_lds(reinterpret_cast<const void*>(kernel), (int)bytes, done)) return rc;
         kernel<<<grid, 256, bytes, s>>>(p, e);
         return (int)MST_OK;
     };
-    static uint64_t done[2] = {0, 0};
+    static uint64_t done[4] = {0, 0, 0, 0};
     int rc = MST_ERR_ARG;
     if constexpr (E != LOGIT_GRAD && E != OUT_BF16) {
-        if (p.planes > 1) rc = run(k_vocab_large_parts<A_ALONG, B_ALONG, E>, Q_LDS, done[1]);
+        if (p.planes > 1 && p.side == VT) rc = run(k_vocab_parts_tile<VT, A_ALONG, B_ALONG, E>, VT, Q_STAGES * q_stage(VT), done[1]);
+        if (p.planes > 1 && p.side != VT) rc = run(k_vocab_parts_tile<VT / 2, A_ALONG, B_ALONG, E>, VT / 2, Q_STAGES * q_stage(VT / 2), done[2]);
     }
     if constexpr (E != LOGIT_GRAD_PARTS && E != OUT_F32) {
-        if (p.planes == 1) rc = run(k_vocab_large<A_ALONG, B_ALONG, E>, L_LDS, done[0]);
+        if (p.planes == 1 && p.side == VT) rc = run(k_vocab_tile<VT, A_ALONG, B_ALONG, E>, VT, L_STAGES * l_stage(VT), done[0]);
+        if (p.planes == 1 && p.side != VT) rc = run(k_vocab_tile<VT / 2, A_ALONG, B_ALONG, E>, VT / 2, L_STAGES * l_stage(VT / 2), done[3]);
     }
     if (rc) return rc;
     MST_LAUNCH_CHECK();
@@ -934,17 +948,27 @@ int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipSt
 
 }  // namespace
 
-// As many ranges as let the products end first: rounds of 256 workgroups, each as long as its range and what begins and ends it (the time of some eight
-// pairs of steps, the sums of the pieces before and behind among it).
-int vocab_splits(int m, int n, int k) {
-    const int64_t tiles = cdiv(m, VT) * cdiv(n, VT), pairs = cdiv(k, L_PAIR);
-    int best = 1;
-    int64_t least = INT64_MAX;
-    for (int s = 1; s <= 64 && s <= pairs; ++s) {
-        const int64_t time = cdiv(tiles * s, 256) * (cdiv(pairs, s) + 8);
-        if (time < least) least = time, best = s;
-    }
-    return best;
+// Rounds of so many tiles, in rounds of 256 x 256: of 128 x 128 a CU has two at a time, which take 0.62 of the time (twice the loads a product), and one alone 0.4.
+static double rounds(int64_t tiles, int side) {
+    if (side == VT) return (double)cdiv(tiles, 256);
+    const int64_t rest = tiles % 512;
+    return 0.62 * (double)(tiles / 512) + (rest == 0 ? 0. : rest <= 256 ? 0.4 : 0.62);
+}
+// Tiles of 256 x 256 where there are enough of them.  Forward and gradients in us, by the large and by the small ones: bf16 of width 768 and vocabulary 50257, 128 tokens 156 and 127, 600 tokens
+// 315 and 288, 1500 tokens 534 and 583; width 1000, vocabulary 1200, 600 tokens 140 and 86 (fp32: 361 and 163); fp32 of width 768 and vocabulary 50257, 128 tokens 560 and 481, 1500 tokens 2392 and 2463.
+int vocab_side(int64_t m, int64_t n) {
+    return rounds(cdiv(m, VT / 2) * cdiv(n, VT / 2), VT / 2) < rounds(cdiv(m, VT) * cdiv(n, VT), VT) ? VT / 2 : VT;
+}
+// Tiles, and as many ranges, as let the products end first: each takes as long as its range and what begins and ends it (the time of some eight pairs of steps, the sums of the
+// pieces before and behind among it).
+void vocab_splits(int m, int n, int k, int& side, int& splits) {
+    const int64_t pairs = cdiv(k, L_PAIR);
+    double least = 1e30;
+    for (int of : {VT, VT / 2})
+        for (int s = 1; s <= 64 && s <= pairs; ++s) {
+            const double time = rounds(cdiv(m, of) * cdiv(n, of) * s, of) * (double)(cdiv(pairs, s) + 8);
+            if (time < least) least = time, side = of, splits = s;
+        }
 }
 
 int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream) {

@@ -10,7 +10,6 @@ constexpr int VT = 256;                  // rows and columns of the largest outp
 constexpr int VK = 32;                   // contraction indices of a step
 constexpr int VPAD = 64;                 // operands are padded to so many
 constexpr int PLANES_MAX = 3;
-constexpr int VOCAB_STAT_COLUMNS = VT / 2;      // (a wavefront's)
 
 // A matrix of bfloat16 numbers, or of numbers that are the sum of three (plane p a stride further on).  Along: a row's numbers are
 // contraction indices; across: a row is one contraction index.  Rows past `rows` read as the last one.
@@ -28,12 +27,13 @@ struct VocabProduct {
     int m, n, k;                         // as the host knows them (the most there are)
     int planes;                          // of either operand: 1, or 3 and six products a term
     int splits;                          // of the contraction, each with its own C (sums)
+    int side;                            // of a tile
 };
 
 // ---- what becomes of C
-// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and VOCAB_STAT_COLUMNS columns
+// statistics of the rows' logits, (b, sum of exp2(z log2 e - b)) per row and half a tile's columns (a wavefront's)
 struct VocabStats {
-    float2* stats;                       // [VOCAB_STAT_COLUMNS columns][row_stride]
+    float2* stats;                       // [columns][row_stride]
     int64_t row_stride;
     int first;                           // number of the first of them
     const float* at_label;               // logit of a row's label, padded to VT
@@ -63,14 +63,15 @@ struct VocabOut {                        // rows of the result times the unit, i
     const float* unit;
 };
 
-int vocab_splits(int m, int n, int k);   // ranges of the contraction for vocab_sums
+int vocab_side(int64_t m, int64_t n);    // of the tiles of a product
+void vocab_splits(int m, int n, int k, int& side, int& splits);        // the same, and ranges of the contraction, for vocab_sums
 // Few tokens, from the hidden states as they are: statistics per VOCAB_FEW_COLUMNS columns, [columns][tokens], and each label's logit; dz in fp32, [tokens][few_pitch(vocab)],
 // and both gradients from it (either may be null), dh by way of sums [vocab_few_ranges][tokens][width]
 constexpr int VOCAB_FEW_COLUMNS = 64;
 __host__ __device__ constexpr int64_t few_pitch(int vocab) { return ((int64_t)vocab + VOCAB_FEW_COLUMNS - 1) / VOCAB_FEW_COLUMNS * VOCAB_FEW_COLUMNS; }
-// Width 768, vocabulary 50257, forward / forward and gradients in us, this way and by the tiles of 256 x 256:
-//   bf16, 16 tokens: 29 / 105 and 37 / 149; 24: 36 / 147 and 37 / 149.      fp32, 40: 104 / 356 and 166 / 550; 64: 115 / 402 and 167 / 554; 128: 195 / 695 and 166 / 558.
-constexpr int VOCAB_FEW_BF16 = 24, VOCAB_FEW_F32 = 64;
+// Width 768, vocabulary 50257, forward / forward and gradients in us, this way and by tiles:
+//   bf16, 16 tokens: 29 / 105 and 35 / 122; 20: 34 / 142 and 35 / 122.      fp32, 40: 104 / 356 and 164 / 481; 64: 115 / 402 and 164 / 481; 128: 195 / 695 and 164 / 481.
+constexpr int VOCAB_FEW_BF16 = 16, VOCAB_FEW_F32 = 64;
 inline bool vocab_is_few(const mst_vocab_loss_shape& s) { return s.tokens <= (s.type == MST_F32 ? VOCAB_FEW_F32 : VOCAB_FEW_BF16); }
 int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream);
 int vocab_few_ranges(const mst_vocab_loss_shape& s);

@@ -239,6 +239,7 @@ bool given(const void* p) { return p && aligned16(p); }
 // The workspace: where its parts begin, and how the work is cut
 struct Plan {
     int planes, wide;                    // parts of a number; columns of packed rows
+    int side, side_dh, side_dE;          // of the tiles of logits, and of those of the gradients
     int64_t rows;                        // of packed arrays
     bool split_E;                        // the products read the embedding from its parts
     int piece, pieces;                   // columns of the vocabulary, and how often
@@ -259,10 +260,12 @@ struct Plan {
         piece = (int)align_up(cdiv(s.vocab, pieces), VT);
         pieces = (int)cdiv(s.vocab, piece);
         few = vocab_is_few(s);
-        stat_columns = few ? VOCAB_FEW_COLUMNS : VOCAB_STAT_COLUMNS;
+        side = vocab_side(s.tokens, std::min(piece, s.vocab));
+        side_dE = vocab_side(std::min(piece, s.vocab), s.width);
+        stat_columns = few ? VOCAB_FEW_COLUMNS : side / 2;
         stats = (int)cdiv(s.vocab, stat_columns);
         sum_blocks = (int)align_up(s.width, VT) / 16;
-        splits = vocab_splits(s.tokens, s.width, std::min(piece, s.vocab));
+        vocab_splits(s.tokens, s.width, std::min(piece, s.vocab), side_dh, splits);
         bytes = 0;
         auto part = [&](size_t n) { const size_t at = bytes; bytes += align_up(n); return at; };
         if (few) {
@@ -335,7 +338,7 @@ struct Run {
         for (int i = 0; i < plan.pieces; ++i) {
             VocabOperand e;
             if (int rc = embedding(i, e)) return rc;
-            const VocabProduct p = {packed(), e, at<int>(plan.count), nullptr, s.tokens, columns(i), plan.wide, plan.planes, 1};
+            const VocabProduct p = {packed(), e, at<int>(plan.count), nullptr, s.tokens, columns(i), plan.wide, plan.planes, 1, plan.side};
             if (int rc = vocab_stats(p, {at<float2>(plan.stat), plan.rows, i * (plan.piece / plan.stat_columns), at<float>(plan.at_label)}, stream)) return rc;
         }
         return join(nullptr, plan.rows, loss, lse);
@@ -357,15 +360,15 @@ struct Run {
             const int n = columns(i);
             VocabOperand e;
             if (int rc = embedding(i, e)) return rc;
-            const VocabProduct z = {packed(), e, at<int>(plan.count), nullptr, s.tokens, n, plan.wide, plan.planes, 1};
+            const VocabProduct z = {packed(), e, at<int>(plan.count), nullptr, s.tokens, n, plan.wide, plan.planes, 1, plan.side};
             if (int rc = vocab_logit_grad(z, {at<uint16_t>(plan.ds), plane, plan.piece, at<float>(plan.lse), at<float>(plan.d), at<int>(plan.label), at<float>(plan.at_label),
                                              i * plan.piece}, stream)) return rc;
             if (dh) {
-                const VocabProduct p = {ds_rows, e, at<int>(plan.count), nullptr, s.tokens, s.width, n, plan.planes, (int)std::min<int64_t>(plan.splits, cdiv(n, VPAD))};      // (a last piece may be short)
+                const VocabProduct p = {ds_rows, e, at<int>(plan.count), nullptr, s.tokens, s.width, n, plan.planes, (int)std::min<int64_t>(plan.splits, cdiv(n, VPAD)), plan.side_dh};      // (a last piece may be short)
                 if (int rc = vocab_sums(p, {at<float>(plan.sums), plan.sum_stride(), plan.sum_blocks, i > 0}, stream)) return rc;
             }
             if (dE) {
-                const VocabProduct p = {ds_rows, packed(), nullptr, at<int>(plan.count), n, s.width, s.tokens, plan.planes, 1};
+                const VocabProduct p = {ds_rows, packed(), nullptr, at<int>(plan.count), n, s.width, s.tokens, plan.planes, 1, plan.side_dE};
                 if (int rc = vocab_out(p, {dE + (int64_t)i * plan.piece * s.width, s.width, s.type == MST_F32, at<float>(plan.unit)}, stream)) return rc;
             }
         }
