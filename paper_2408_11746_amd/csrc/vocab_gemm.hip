@@ -915,12 +915,15 @@ __global__ __launch_bounds__(256) void k_vocab_few_dE(const float* __restrict__ 
 // f(a number of the type, tiles of sixteen tokens)
 template <typename F>
 void with_few(const mst_vocab_loss_shape& s, F&& f) {
-    if (s.type == MST_BF16) f(bf16{}, std::integral_constant<int, 1>{});
-    else if (s.tokens <= 16) f(float{}, std::integral_constant<int, 1>{});
-    else if (s.tokens <= 32) f(float{}, std::integral_constant<int, 2>{});
+    auto sized = [&](auto type) {
+        if (s.tokens <= 16) f(type, std::integral_constant<int, 1>{});
+        else f(type, std::integral_constant<int, 2>{});
+    };
+    if (s.type == MST_BF16) sized(bf16{});
+    else if (s.tokens <= 32) sized(float{});
     else f(float{}, std::integral_constant<int, 4>{});
 }
-static_assert(VOCAB_FEW_BF16 <= 16 && VOCAB_FEW_F32 <= 64);
+static_assert(VOCAB_FEW_BF16 <= 32 && VOCAB_FEW_SMALL <= 32 && VOCAB_FEW_F32 <= 64);
 
 template <bool A_ALONG, bool B_ALONG, Epilogue E>
 int launch(const VocabProduct& p, const typename EpilogueArgs<E>::type& e, hipStream_t s) {

@@ -72,7 +72,13 @@ __host__ __device__ constexpr int64_t few_pitch(int vocab) { return ((int64_t)vo
 // Width 768, vocabulary 50257, forward / forward and gradients in us, this way and by tiles:
 //   bf16, 16 tokens: 29 / 105 and 35 / 122; 20: 34 / 142 and 35 / 122.      fp32, 40: 104 / 356 and 164 / 481; 64: 115 / 402 and 164 / 481; 128: 195 / 695 and 164 / 481.
 constexpr int VOCAB_FEW_BF16 = 16, VOCAB_FEW_F32 = 64;
-inline bool vocab_is_few(const mst_vocab_loss_shape& s) { return s.tokens <= (s.type == MST_F32 ? VOCAB_FEW_F32 : VOCAB_FEW_BF16); }
+// A small embedding is read in no time, and the launches before the tiles' count: as above, bf16, 17 tokens: width 1000, vocabulary 1200 14 / 40 and 26 / 70; width 256, vocabulary 50304 16 / 67 and 24 / 80.
+constexpr int VOCAB_FEW_SMALL = 32;
+constexpr int64_t VOCAB_SMALL = int64_t(1) << 24;
+inline bool vocab_is_few(const mst_vocab_loss_shape& s) {
+    const int few = s.type == MST_F32 ? VOCAB_FEW_F32 : (int64_t)s.vocab * s.width <= VOCAB_SMALL ? VOCAB_FEW_SMALL : VOCAB_FEW_BF16;
+    return s.tokens <= few;
+}
 int vocab_few(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, float2* stats, float* at_label, hipStream_t stream);
 int vocab_few_ranges(const mst_vocab_loss_shape& s);
 int vocab_few_bwd(const mst_vocab_loss_shape& s, const void* h, const void* E, const int* labels, const float* lse, const float* dloss, float* dz, float* sums, void* dh, void* dE,
