@@ -683,7 +683,7 @@ typedef struct {
     int32_t vocab;               /* 1 .. 2^24 */
     mst_dtype type;              /* of h, E and their gradients.  MST_BF16: products of the numbers as they are, fp32 sums; the gradient of z is rounded
                                     to bfloat16 for its products.  MST_F32: numbers as three bfloat16 parts each, six products (2^-24 of a term).
-                                    Few tokens (24 and 64 at most): the gradient of z stays fp32, and so do the products of MST_F32 */
+                                    Few tokens (16 to 64 at most, by type and size): the gradient of z stays fp32, and so do the products of MST_F32 */
 } mst_vocab_loss_shape;
 
 /* loss_dev, lse_dev fp32 [tokens] (loss_dev may be NULL).  Workspace: mst_vocab_loss_workspace_bytes(shape, 0). */

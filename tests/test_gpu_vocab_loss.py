@@ -117,6 +117,13 @@ def test_pieces_and_many_tiles(tokens, width, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,width,vocab", [(1500, 1280, 9003), (1531, 1288, 9001), (600, 264, 30011), (520, 72, 20000), (33, 2056, 9001)])
+def test_large_and_small_tiles(tokens, width, vocab, dtype):
+    # (all three products by tiles of 256 x 256, by those of 128 x 128 several to a workgroup, and by a mixture)
+    _all(17, tokens, width, vocab, dtype, unlabelled=0.1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("tokens", [9, 100, 400])
 def test_labels_far_from_likely(tokens, dtype):
     """logits some hundreds apart: exp(z - z_label) leaves fp32, and so do most probabilities below"""
