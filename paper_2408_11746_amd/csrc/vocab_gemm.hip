@@ -104,8 +104,11 @@ __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabP
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         const int m = m0 + 16 * i + (lane & 15);
-        base[i] = e.lse[m] * LOG2E;
-        d[i] = e.d[m];
+        const float lse = e.lse[m];
+        base[i] = lse * LOG2E;
+        // What the product's rounding loses (1e-6 of a row's dz where its lse is 20) is made up for in d: its own exact remainder.  (Rows of no token: infinite - infinite.)
+        const float left = fmaf(lse, LOG2E, -base[i]);
+        d[i] = e.d[m] * (lse < INFINITY ? exp2_fast(-left) : 1.f);
         at_label[i] = e.at_label[m];
         label[i] = e.label[m] - e.v0 - n0;
     }

@@ -191,11 +191,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_vocab_join(const float2* __res
         __syncthreads();
     }
     if (share || row >= rows) return;
-    const float l = (top + log2f(sum)) * 0.69314718f;
+    // 1 / (log2 e as the products of z and it have it), in two parts: lse is rounded once, and what top takes away of the loss goes away exactly
+    constexpr float HIGH = 0.6931472f, LOW = 7.3486931e-9f;
+    const float log_sum = log2f(sum) * HIGH, l = fmaf(top, HIGH, fmaf(top, LOW, log_sum));
     const int token = list ? list[row] : row;
     const bool has = !labels || (labels[token] >= 0 && labels[token] < vocab);
     lse[token] = has ? l : 0.f;
-    if (loss) loss[token] = has ? l - at_label[row] : 0.f;
+    if (loss) loss[token] = has ? fmaf(top, HIGH, -at_label[row]) + fmaf(top, LOW, log_sum) : 0.f;
 }
 
 // gradients of the hidden states: sums of the splits, back to the tokens' places; a wavefront takes blocks of 16 rows and 16 columns, or a workgroup's four share one
