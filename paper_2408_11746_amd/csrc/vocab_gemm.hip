@@ -48,11 +48,17 @@ __device__ __forceinline__ float result(const floatx4& acc, int v) {
     return x;
 }
 
+// ... or of two sums
+struct TwoSums { floatx4 main, low; };
+__device__ __forceinline__ float result(const TwoSums& acc, int v) { return result(acc.main, v) + result(acc.low, v); }
+__device__ __forceinline__ void clear_sum(floatx4& acc) { acc = floatx4{0.f, 0.f, 0.f, 0.f}; }
+__device__ __forceinline__ void clear_sum(TwoSums& acc) { acc.main = acc.low = floatx4{0.f, 0.f, 0.f, 0.f}; }
+
 // Sums of exp2(z log2 e - base) over a wavefront's columns, those below p.n.  Base is the logit of the row's own label: the sum over all columns is then 1 at least,
 // what is lost below fp32 does not count in it, and no maximum has to be found first (a fifth of the instructions).  A sum that leaves fp32 is formed again
 // from the row's maximum here.
-template <int I, int J, bool ENDS, bool MAXIMUM>
-__device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
+template <int I, int J, bool ENDS, bool MAXIMUM, typename X>
+__device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProduct& p, const X (&acc)[I][J], int m0, int n0, int lane) {
     const int last = p.n - n0 - 4 * (lane >> 4);
     auto larger = [](float a, float b) { return fmaxf(a, b); };
     auto plus = [](float a, float b) { return a + b; };
@@ -85,19 +91,19 @@ __device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProdu
     }
     return fits;
 }
-template <int I, int J, bool ENDS>
-__device__ __forceinline__ void statistics(const VocabStats& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
+template <int I, int J, bool ENDS, typename X>
+__device__ __forceinline__ void statistics(const VocabStats& e, const VocabProduct& p, const X (&acc)[I][J], int m0, int n0, int lane) {
     if (__any(!statistics<I, J, ENDS, false>(e, p, acc, m0, n0, lane))) statistics<I, J, ENDS, true>(e, p, acc, m0, n0, lane);
 }
-template <int I, int J>
-__device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int) {
+template <int I, int J, typename X>
+__device__ __forceinline__ void finish(const VocabStats& e, const VocabProduct& p, X (&acc)[I][J], int m0, int n0, int, int lane, int) {
     if (n0 + 16 * J <= p.n) statistics<I, J, false>(e, p, acc, m0, n0, lane);
     else if (n0 < p.n) statistics<I, J, true>(e, p, acc, m0, n0, lane);
 }
 
 // dz
-template <int I, int J, int PLANES, bool ENDS>
-__device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabProduct& p, const floatx4 (&acc)[I][J], int m0, int n0, int lane) {
+template <int I, int J, int PLANES, bool ENDS, typename X>
+__device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabProduct& p, const X (&acc)[I][J], int m0, int n0, int lane) {
     const int g = lane >> 4, last = p.n - n0 - 4 * g;
     float base[I], d[I], at_label[I];
     int label[I];
@@ -142,36 +148,39 @@ __device__ __forceinline__ void logit_grad(const VocabLogitGrad& e, const VocabP
         __builtin_amdgcn_sched_barrier(0);
     }
 }
-template <int I, int J, int PLANES>
-__device__ __forceinline__ void finish(const VocabLogitGradOf<PLANES>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int) {
+template <int I, int J, int PLANES, typename X>
+__device__ __forceinline__ void finish(const VocabLogitGradOf<PLANES>& e, const VocabProduct& p, X (&acc)[I][J], int m0, int n0, int, int lane, int) {
     if (n0 + 16 * J <= p.n) logit_grad<I, J, PLANES, false>(e, p, acc, m0, n0, lane);
     else logit_grad<I, J, PLANES, true>(e, p, acc, m0, n0, lane);
 }
 
 // Sums lie as the wavefronts hold them, a wavefront's 16 x 16 results in 1 KB after another (sum_place): the next piece begins with them.
-template <int I, int J>
+__device__ __forceinline__ floatx4& main_sum(floatx4& acc) { return acc; }
+__device__ __forceinline__ floatx4& main_sum(TwoSums& acc) { return acc.main; }
+__device__ __forceinline__ floatx4 whole_sum(const floatx4& acc) { return acc; }
+__device__ __forceinline__ floatx4 whole_sum(const TwoSums& acc) { return acc.main + acc.low; }
 __device__ __forceinline__ float4* sums_of(const VocabSums& e, int m0, int n0, int split, int lane) {
     return reinterpret_cast<float4*>(e.sums + split * e.stride) + sum_place(m0, n0, e.wide) + lane;
 }
-template <int I, int J>
-__device__ __forceinline__ void begin(const VocabSums& e, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane) {
+template <int I, int J, typename X>
+__device__ __forceinline__ void begin(const VocabSums& e, X (&acc)[I][J], int m0, int n0, int split, int lane) {
     if (!e.add) return;
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int j = 0; j < J; ++j) acc[i][j] = *reinterpret_cast<const floatx4*>(sums_of<I, J>(e, m0 + 16 * i, n0 + 16 * j, split, lane));
+        for (int j = 0; j < J; ++j) main_sum(acc[i][j]) = *reinterpret_cast<const floatx4*>(sums_of(e, m0 + 16 * i, n0 + 16 * j, split, lane));
 }
-template <int I, int J, typename Args>
-__device__ __forceinline__ void begin(const Args&, floatx4 (&)[I][J], int, int, int, int) {}
-template <int I, int J>
-__device__ __forceinline__ void finish(const VocabSums& e, const VocabProduct&, floatx4 (&acc)[I][J], int m0, int n0, int split, int lane, int) {
+template <int I, int J, typename Args, typename X>
+__device__ __forceinline__ void begin(const Args&, X (&)[I][J], int, int, int, int) {}
+template <int I, int J, typename X>
+__device__ __forceinline__ void finish(const VocabSums& e, const VocabProduct&, X (&acc)[I][J], int m0, int n0, int split, int lane, int) {
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int j = 0; j < J; ++j) *reinterpret_cast<floatx4*>(sums_of<I, J>(e, m0 + 16 * i, n0 + 16 * j, split, lane)) = acc[i][j];
+        for (int j = 0; j < J; ++j) *reinterpret_cast<floatx4*>(sums_of(e, m0 + 16 * i, n0 + 16 * j, split, lane)) = whole_sum(acc[i][j]);
 }
-template <int I, int J, typename T>
-__device__ __forceinline__ void finish(const VocabOutOf<T>& e, const VocabProduct& p, floatx4 (&acc)[I][J], int m0, int n0, int, int lane, int m_rows) {
+template <int I, int J, typename T, typename X>
+__device__ __forceinline__ void finish(const VocabOutOf<T>& e, const VocabProduct& p, X (&acc)[I][J], int m0, int n0, int, int lane, int m_rows) {
     const float u = *e.unit;
     const int m = m0 + (lane & 15), n = n0 + 4 * (lane >> 4);
     T* const first = static_cast<T*>(e.out) + (int64_t)m * e.ld + n;
@@ -525,12 +534,14 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
     const int m_rows = units.m_rows, end = units.end, each = units.each;
     int unit = units.next;
     if (unit >= end) return;
-    floatx4 acc[N][N];
+    // Small tiles have room to sum the five products of smaller parts for themselves: every one added to the sum of a0 b0 rounds it once more.
+    constexpr bool APART = SIDE != VT;
+    std::conditional_t<APART, TwoSums, floatx4> acc[N][N];
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < N; ++j) clear_sum(acc[i][j]);
     };
     if (units.k_all == 0) {               // a batch without labels
         clear();
@@ -581,15 +592,19 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
     const PartReads<B_ALONG, SIDE> rb(wn, lane);
     bf16x8 a[2][N], b[2][N];
     // products of sets AS and BS; what stage sa (sb) holds goes to set RA (RB; -1: nothing is read), part `part` of an operand to `to`
-    auto product = [&](auto as, auto bs, auto fresh, auto ra_set, uint32_t sa, auto rb_set, uint32_t sb, auto of_a, int part, uint32_t to) __attribute__((always_inline)) {
+    auto product = [&](auto main, auto as, auto bs, auto fresh, auto ra_set, uint32_t sa, auto rb_set, uint32_t sb, auto of_a, int part, uint32_t to) __attribute__((always_inline)) {
         constexpr int AS = decltype(as)::value, BS = decltype(bs)::value, RA = decltype(ra_set)::value, RB = decltype(rb_set)::value;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             shortx4 pa[2], pb[2];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                if constexpr (decltype(fresh)::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b[BS][j]), "v"(a[AS][i]));
-                else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b[BS][j]), "v"(a[AS][i]));
+                floatx4* sum;
+                if constexpr (!APART) sum = &acc[i][j];
+                else if constexpr (decltype(main)::value) sum = &acc[i][j].main;
+                else sum = &acc[i][j].low;
+                if constexpr (decltype(fresh)::value) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(*sum) : "v"(b[BS][j]), "v"(a[AS][i]));
+                else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(*sum) : "v"(b[BS][j]), "v"(a[AS][i]));
                 if constexpr (RB >= 0) {
                     if (j == 0) rb.half(sb, i, 0, b[RB][i], pb);
                     if (j == 1) rb.half(sb, i, 1, b[RB][i], pb);
@@ -616,21 +631,24 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
         else wait_loads<2 * PIECES>();
         lds_barrier();
     };
-    auto step = [&](auto q, auto fresh, bool stored) __attribute__((always_inline)) {
+    // first: of a unit; fresh: and its sums begin at 0
+    auto step = [&](auto q, auto first, auto fresh, bool stored) __attribute__((always_inline)) {
         constexpr std::integral_constant<int, decltype(q)::value> Q;
         constexpr std::integral_constant<int, 1 - decltype(q)::value> R;
         meet(stored);
         aim();
-        product(zero, Q, fresh, one, stage(2), none, 0, no, 0, to_b(6));
-        product(one, Q, no, zero, stage(3), none, 0, yes, 2, to_a(7));
+        constexpr std::bool_constant<APART ? decltype(first)::value : decltype(fresh)::value> fresh_first;
+        constexpr std::bool_constant<APART && decltype(fresh)::value> fresh_main;
+        product(no, zero, Q, fresh_first, one, stage(2), none, 0, no, 0, to_b(6));
+        product(no, one, Q, no, zero, stage(3), none, 0, yes, 2, to_a(7));
         meet(false);
-        product(zero, Q, no, none, 0, R, stage(4), yes, 1, to_a(8));
-        product(zero, R, no, none, 0, Q, stage(5), yes, 0, to_a(9));
+        product(yes, zero, Q, fresh_main, none, 0, R, stage(4), yes, 1, to_a(8));
+        product(no, zero, R, no, none, 0, Q, stage(5), yes, 0, to_a(9));
         meet(false);
-        product(zero, Q, no, one, stage(2), none, 0, no, 2, to_b(10));
+        product(no, zero, Q, no, one, stage(2), none, 0, no, 2, to_b(10));
         const uint32_t load = to_b(11);
         base = base + 6 >= Q_STAGES ? base + 6 - Q_STAGES : base + 6;
-        product(one, Q, no, zero, stage(1), R, stage(0), no, 1, load);
+        product(no, one, Q, no, zero, stage(1), R, stage(0), no, 1, load);
     };
 
     aim();
@@ -663,23 +681,26 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
         if constexpr (E == SUMS) {
             clear();
             begin(e, acc, x.m0 + wm, x.n0 + wn, x.split, lane);
-            step(zero, no, stored);
+            step(zero, yes, no, stored);
         } else {
-            step(zero, yes, stored);
+            step(zero, yes, yes, stored);
         }
         stored = true;
-        step(one, no, false);
+        step(one, no, no, false);
 #pragma unroll 1
         for (int d = 1; d < pairs; ++d) {
-            step(zero, no, false);
-            step(one, no, false);
+            step(zero, no, no, false);
+            step(one, no, no, false);
         }
         // the last product is 18 wait states from its result
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));
+            for (int j = 0; j < N; ++j) {
+                if constexpr (APART) asm volatile("" : "+a"(acc[i][j].main), "+a"(acc[i][j].low));
+                else asm volatile("" : "+a"(acc[i][j]));
+            }
         finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more

@@ -262,7 +262,9 @@ struct Plan {
         piece = (int)align_up(cdiv(s.vocab, pieces), VT);
         pieces = (int)cdiv(s.vocab, piece);
         few = vocab_is_few(s);
-        side = vocab_side(s.tokens, std::min(piece, s.vocab));
+        // Logits of fp32 numbers are rounded less by small tiles, which sum small parts for themselves.  It shows in dh where few logits share a row: vocabulary 572, width 768, 2.0e-6 by large
+        // tiles, 0.9e-6 by small ones (products of fp32 numbers as they are: 1.2e-6); vocabulary 32003, width 648, 0.9e-6 by large ones (3.8e-6).
+        side = planes > 1 && s.vocab <= 2048 ? VT / 2 : vocab_side(s.tokens, std::min(piece, s.vocab));
         side_dE = vocab_side(std::min(piece, s.vocab), s.width);
         stat_columns = few ? VOCAB_FEW_COLUMNS : side / 2;
         stats = (int)cdiv(s.vocab, stat_columns);
