@@ -269,7 +269,8 @@ struct Plan {
         stat_columns = few ? VOCAB_FEW_COLUMNS : side / 2;
         stats = (int)cdiv(s.vocab, stat_columns);
         sum_blocks = (int)align_up(s.width, VT) / 16;
-        vocab_splits(s.tokens, s.width, std::min(piece, s.vocab), side_dh, splits);
+        side_dh = VT, splits = 1;
+        if (backward && !few) vocab_splits(s.tokens, s.width, std::min(piece, s.vocab), side_dh, splits);
         bytes = 0;
         auto part = [&](size_t n) { const size_t at = bytes; bytes += align_up(n); return at; };
         if (few) {
