@@ -212,9 +212,9 @@ constexpr int stores_behind(Epilogue E, int products) {
 // after that, stand one by one between its 64 matrix instructions (16).  Steps come in pairs, of which the second waits for the pair behind it:
 //   first   products of its first half, reads of its second half, loads of the next pair but one: A
 //   second  waits; products of its second half, reads of the next pair's first half, loads of the next pair but one: B
-// 8192 tokens, width 1280, vocabulary 50257 (1054 GFLOP a product): statistics 879 us, 1200 TFLOP/s; dz 1052 (two pieces), 1002; dh 898, 1174; dE 876, 1203; the library's 8192^3 product
+// 8192 tokens, width 1280, vocabulary 50257 (1054 GFLOP a product): statistics 863 us, 1222 TFLOP/s; dz 1042 (two pieces), 1012; dh 894, 1180; dE 862, 1223; the library's 8192^3 product
 // reaches 1191.  Matrix instructions are busy in 70 % of the clocks (dz, whose 64 stores and exponentials of a tile hide behind nothing: 56), at some 1.8 GHz.  Of 768 tokens of width 768
-// 591 tiles take three rounds of the 256 CUs: statistics 68 us, 870 TFLOP/s; dz 86, dh 68, dE 85.
+// 591 tiles take three rounds of the 256 CUs: statistics 69 us, 860 TFLOP/s; dz 87, dh 69, dE 84.
 // What bounds the loop is the way of the loads into LDS, 64 KB a pair of steps and CU; small tiles load twice as much a product (which of them: vocab_side).  Of the whole of the above, 3.5 ms now,
 // results that leave for memory and loads that begin only then took 4.46, workgroups that stay and load ahead 4.25.
 constexpr int L_PAIR = 2 * VK, L_STAGES = 5;
@@ -466,7 +466,7 @@ void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) 
 // ---- the same tiles for numbers of three parts: six products of each step of 32 indices
 // The parts of a step are in LDS once, 16 KB each (8), and a part stays in registers for the products that follow one another with it: seven reads of operands instead of
 // twelve, and half of the bytes from memory that six separate products would take, which bound them (1378 tokens, width 648, vocabulary 32003, forward and gradients: 1.64 ms, this way 1.35).
-// Now, of 343 GFLOP each: statistics 291 us, dz 372, dh 310, dE 363; matrix instructions are busy in 83 % of the clocks (dz 63).
+// Now, of 343 GFLOP each: statistics 304 us, dz 390, dh 322, dE (by small tiles) 349; matrix instructions are busy in 83 % of the clocks (dz 63).
 //   product   a2 b0   a1 b0   a0 b0   a0 b2   a0 b1   a1 b1        register set of a, of b:  0 Q   1 Q   0 Q   0 1-Q   0 Q   1 Q
 //   reads     a1      a0      b2      b1      a1      b0, a2 of the next step
 //   loads     b0      a2      a1      a0      b2      b1  of the next step

@@ -8,7 +8,7 @@
 // pads their rows to whole steps of the products.  fp32 numbers are split into three bfloat16 parts on the way, those of the embedding
 // a piece at a time.
 // The logit of a token's own label is a dot product of its own in fp32, and so is what it adds to dz: exp(z - lse) - 1 without cancellation.
-// The products bound it (vocab_gemm.hip).  What is here takes, of 8192 bfloat16 tokens of width 1280 and a vocabulary of 50257 (3560 us with the gradients): rows 16, packing 13 (both
+// The products bound it (vocab_gemm.hip).  What is here takes, of 8192 bfloat16 tokens of width 1280 and a vocabulary of 50257 (3520 us with the gradients): rows 16, packing 13 (both
 // in either direction), join 8, dh 32; of 1024 tokens of width 768 (338 us): 5, 6, 7 and 10.
 // Few tokens (vocab_is_few) go neither through the packing nor through pieces.
 #include "rows.h"
