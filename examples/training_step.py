@@ -3,7 +3,7 @@ products around the activation, and the loss over the vocabulary.  What the norm
 
     python examples/training_step.py            # a few steps on random tokens, with activations kept in 8 bits
 
-The topology updates of the sparse products are the driver's business and are left out here.
+The topology updates of the sparse products are left out here (`paper_2408_11746_amd/driver.py` makes them).
 """
 import math
 import os

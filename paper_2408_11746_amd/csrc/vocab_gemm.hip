@@ -945,6 +945,7 @@ void with_few(const mst_vocab_loss_shape& s, F&& f) {
     };
     if (s.type == MST_BF16) sized(bf16{});
     else if (s.tokens <= 32) sized(float{});
+    else if (s.tokens <= 48) f(float{}, std::integral_constant<int, 3>{});
     else f(float{}, std::integral_constant<int, 4>{});
 }
 static_assert(VOCAB_FEW_BF16 <= 32 && VOCAB_FEW_SMALL <= 32 && VOCAB_FEW_F32 <= 64);

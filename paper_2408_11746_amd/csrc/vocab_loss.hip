@@ -31,7 +31,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restri
     __shared__ int sums[ROWS_THREADS / 64];
     int top = 0;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int before = 0;                                                 // rows of the tokens before this round's
+    int before = 0;                                                 // rows of the tokens before these
     for (int t0 = 0; t0 < T; t0 += ROWS_THREADS * ROWS_EACH) {
         int mine[ROWS_EACH], n = 0;
         float d[ROWS_EACH];
