@@ -710,9 +710,9 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
 // Operands come as the products want them, 16 bytes of a row to a lane; which four (or eight) contraction indices a lane has is free as long as both operands agree.  Logits of bfloat16 numbers
 // on the bfloat16 instructions, everything else in fp32 on its own (16 x 16 x 4): dz is not rounded, and nothing is split into parts.
 // A lane has row (column) l % 16 and the indices of l / 16.
-// Vocabulary 50257, width 768: of 8 bfloat16 tokens logits take 21 us (77 MB, 3.7 TB/s), of 8 in fp32 39 (154 MB, 4.0 TB/s), dh 26 (5.9 TB/s), dE 32 (4.8); of 40 in fp32 104, 74 and 72: there the
-// hidden states (and dz) come from the caches four times as often as the embedding, and bound it.  Handing them round in LDS was slower (160), and so were loads of the next tokens
-// under the present products of dE (96: half the wavefronts).
+// Vocabulary 50257, width 768: of 8 bfloat16 tokens logits take 21 us (77 MB, 3.7 TB/s), of 8 in fp32 39 (154 MB, 4.0 TB/s), dh 26 (5.9 TB/s), dE 32 (4.8); of 40 in fp32 87, 57 and 71: there the
+// hidden states (and dz) come from the caches three times as often as the embedding, and bound it.  Handing them round in LDS was slower (four tiles: 155 where these take 104), and so were loads of the
+// next tokens under the present products of dE (96 where these take 72: half the wavefronts).
 __device__ __forceinline__ void four(const bf16* p, bool there, float (&x)[4]) {
     uint2 w = make_uint2(0, 0);
     if (there) w = *reinterpret_cast<const uint2*>(p);
@@ -746,7 +746,8 @@ struct FewArgs {
 template <typename T, int TT, bool GRAD>
 __global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, const T* __restrict__ E, int tokens, int W, int V, const FewArgs args) {
     __shared__ float2 part[4][16 * TT];
-    constexpr int WORD = 16 / sizeof(T), STEP = 4 * WORD, U = 8;    // numbers of a lane and of a step; steps whose loads are on the way while as many are worked on
+    constexpr int WORD = 16 / sizeof(T), STEP = 4 * WORD, U = 2;    // numbers of a lane and of a step; steps whose loads are on the way while as many are worked on (eight: 295, not 280 us
+    // for 33 fp32 tokens of width 768, vocabulary 50257, with gradients; 63, not 51, for 24 of width 1000, vocabulary 1200: fewer wavefronts a SIMD, and hidden states that leave the first cache)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
     const int v0 = blockIdx.x * VOCAB_FEW_COLUMNS + 16 * wave;
     const T* const e = E + (int64_t)min(v0 + r, V - 1) * W + WORD * g;

@@ -70,9 +70,10 @@ void vocab_splits(int m, int n, int k, int& side, int& splits);        // the sa
 constexpr int VOCAB_FEW_COLUMNS = 64;
 __host__ __device__ constexpr int64_t few_pitch(int vocab) { return ((int64_t)vocab + VOCAB_FEW_COLUMNS - 1) / VOCAB_FEW_COLUMNS * VOCAB_FEW_COLUMNS; }
 // Width 768, vocabulary 50257, forward / forward and gradients in us, this way and by tiles:
-//   bf16, 16 tokens: 29 / 105 and 35 / 122; 20: 34 / 142 and 35 / 122.      fp32, 40: 104 / 356 and 164 / 481; 64: 115 / 402 and 164 / 481; 128: 195 / 695 and 164 / 481.
+//   bf16, 16 tokens: 28 / 103 and 34 / 124; 24: - / 143 and 34 / 124.      fp32, 40: 86 / 301 and 160 / 480; 64: 117 / 405 and 160 / 480; 128: 195 / 695 and 160 / 485.
 constexpr int VOCAB_FEW_BF16 = 16, VOCAB_FEW_F32 = 64;
-// A small embedding is read in no time, and the launches before the tiles' count: as above, bf16, 17 tokens: width 1000, vocabulary 1200 14 / 40 and 26 / 70; width 256, vocabulary 50304 16 / 67 and 24 / 80.
+// A small embedding is read in no time, and the launches before the tiles' count: as above, bf16, 17 tokens: width 1000, vocabulary 1200 12 / 35 and 26 / 70; width 256, vocabulary 50304 17 / 67
+// and 24 / 80.
 constexpr int VOCAB_FEW_SMALL = 32;
 constexpr int64_t VOCAB_SMALL = int64_t(1) << 24;
 inline bool vocab_is_few(const mst_vocab_loss_shape& s) {
