@@ -370,7 +370,8 @@ void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) 
     const TileReads<B_ALONG, SIDE> rb(wn, lane);
     bf16x8 a[2][N], b[2][N];
     // products from register set SET; half 1 - SET of the stages sa, sb goes to the other set, a stage's loads to `to`.  (The products by hand: the compiler would keep
-    // some of the sums outside the accumulation registers and spill.)
+    // some of the sums outside the accumulation registers and spill.  It does not know them for what they are, and would not keep a vector instruction that writes an operand or a sum two wait
+    // states away: operands come from LDS, sums that are not fresh from memory or from the products before, so that there is none.  The epilogues leave the sums as they are for the same reason.)
     auto step = [&](auto set, auto fresh, uint32_t sa, uint32_t sb, uint32_t to) __attribute__((always_inline)) {
         constexpr int P = decltype(set)::value;
 #pragma unroll
