@@ -55,8 +55,10 @@ __device__ __forceinline__ void clear_sum(floatx4& acc) { acc = floatx4{0.f, 0.f
 __device__ __forceinline__ void clear_sum(TwoSums& acc) { acc.main = acc.low = floatx4{0.f, 0.f, 0.f, 0.f}; }
 
 // Sums of exp2(z log2 e - base) over a wavefront's columns, those below p.n.  Base is the logit of the row's own label: the sum over all columns is then 1 at least,
-// what is lost below fp32 does not count in it, and no maximum has to be found first (a fifth of the instructions).  A sum that leaves fp32 is formed again
-// from the row's maximum here.
+// what is lost below fp32 does not count in it, and no maximum has to be found first (a fifth of the instructions).  A sum that passes 2^64 (or is no number) is formed
+// again from the row's maximum here.  A row's sums, 2^18 at most, are added elsewhere: those with the label's base stay below 2^82 together, and what falls below fp32 of them beside a sum
+// with another base, 1 at least in its own, is less than 2^(64 - 126 + 18) of that.
+constexpr float SUM_MOST = 0x1p64f;
 template <int I, int J, bool ENDS, bool MAXIMUM, typename X>
 __device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProduct& p, const X (&acc)[I][J], int m0, int n0, int lane) {
     const int last = p.n - n0 - 4 * (lane >> 4);
@@ -85,7 +87,7 @@ __device__ __forceinline__ bool statistics(const VocabStats& e, const VocabProdu
 #pragma unroll
             for (int v = 0; v < 4; ++v) sum += exp2_fast(fmaf(z(j, v), LOG2E, -base[i]));
         sum = apart<32>(apart<16>(sum, plus), plus);
-        fits &= sum < INFINITY;
+        fits &= sum < SUM_MOST;
         if (lane < 16) to[16 * i] = make_float2(base[i], sum);
         __builtin_amdgcn_sched_barrier(0);                          // (with the results of several rows out of the accumulation registers it spills)
     }
