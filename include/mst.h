@@ -691,7 +691,8 @@ int mst_vocab_loss_fwd(const mst_vocab_loss_shape* shape, const void* h_dev, con
                        float* loss_dev, float* lse_dev, void* ws_dev, size_t ws_bytes, mst_stream_t stream);
 
 /* Gradients of sum_t dloss_t loss_t: dh [tokens x width], dE [vocab x width] (either may be NULL: not wanted) from lse of the forward call and
- * dloss_dev fp32 [tokens].  z is formed again, in pieces of the vocabulary.  Workspace: mst_vocab_loss_workspace_bytes(shape, 1). */
+ * dloss_dev fp32 [tokens].  z is formed again, in pieces of the vocabulary; what of its gradient is below 2^-126 (of the batch's largest finite |dloss|, where that is below 1)
+ * may count as 0.  Workspace: mst_vocab_loss_workspace_bytes(shape, 1). */
 int mst_vocab_loss_bwd(const mst_vocab_loss_shape* shape, const void* h_dev, const void* E_dev, const int32_t* labels_dev,
                        const float* lse_dev, const float* dloss_dev, void* dh_dev, void* dE_dev, void* ws_dev, size_t ws_bytes,
                        mst_stream_t stream);

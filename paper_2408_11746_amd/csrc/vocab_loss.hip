@@ -24,7 +24,8 @@ constexpr int64_t PIECE_BYTES = int64_t(1) << 29;
 // ---- which tokens have a label
 constexpr int ROWS_THREADS = 1024, ROWS_EACH = 8;
 // One workgroup: place[token] = its row or -1, list[row] = token, label[row], count.  In order.  Rows behind the last, up to a whole tile: label -1.
-// Outputs of tokens without one: 0.  unit: the largest finite size of the rows' dloss (1 if all are 0): an infinite one is its own row's alone.
+// Outputs of tokens without one: 0.  unit: the largest finite size of the rows' dloss (1 if all are 0; an infinite one is its own row's alone), or, where that is above 1, its
+// significant digits, 1 to 2: in units of a large number itself rows of a small dloss would fall below fp32.
 __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restrict__ labels, int T, int V, int* __restrict__ count, int* __restrict__ place,
                                                              int* __restrict__ list, int* __restrict__ label, float* __restrict__ loss, float* __restrict__ lse,
                                                              const float* __restrict__ dloss, float* __restrict__ unit) {
@@ -90,7 +91,8 @@ __global__ __launch_bounds__(ROWS_THREADS) void k_vocab_rows(const int* __restri
         if (lane == 0) sums[wave] = top;
         __syncthreads();
         for (int w = 0; w < ROWS_THREADS / 64; ++w) top = max(top, sums[w]);
-        if (tid == 0) *unit = top == 0 ? 1.f : __int_as_float(top);
+        constexpr int ONE = 0x3F800000;
+        if (tid == 0) *unit = __int_as_float(top == 0 ? ONE : top < ONE ? top : ONE | (top & 0x007FFFFF));
     }
     const int end = (before + VT - 1) / VT * VT;
     for (int r = before + tid; r < end; r += ROWS_THREADS) label[r] = -1;
@@ -109,7 +111,7 @@ __device__ inline void put_parts(uint16_t* to, int64_t plane, int planes, float 
 }
 
 // What the packing of the rows leaves beside them, per row (zeros and an infinite lse behind the last, up to a whole tile).
-// dz is held in units of the largest dloss: where the loss is a mean, all dloss are one number, and the label's dz, by far the largest of a
+// dz is held in units of the largest dloss, but for a power of two: where the loss is a mean, all dloss are one number, and the label's dz, by far the largest of a
 // row, would be rounded to bfloat16 the same way in every row (2.5e-3 of dh and dE, 2.0e-3 in these units).  Both results are multiplied by the unit in fp32.
 struct RowNumbers {
     float* at_label;                     // forward: the label's logit; backward: dz there
