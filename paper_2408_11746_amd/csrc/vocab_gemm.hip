@@ -795,13 +795,14 @@ __global__ __launch_bounds__(256) void k_vocab_few(const T* __restrict__ h, cons
             if (token >= tokens) continue;
             const int label = args.labels[token];
             const bool has = label >= 0 && label < V;
-            const float lse = args.lse[token], d = args.dloss[token];
+            const float lse = args.lse[token], d = args.dloss[token], base = lse * LOG2E;
+            // (what that product's rounding loses is made up for as in the tiles)
+            const float weight = d * (lse < INFINITY ? exp2_fast(-fmaf(lse, LOG2E, -base)) : 1.f);
             float z[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int col = v0 + 4 * g + v;
-                const float y = acc[i][v] - lse;
-                z[v] = has && col < V ? d * (col == label ? expm1f(y) : exp2_fast(y * LOG2E)) : 0.f;
+                z[v] = has && col < V ? col == label ? d * expm1f(acc[i][v] - lse) : weight * exp2_fast(fmaf(acc[i][v], LOG2E, -base)) : 0.f;
             }
             *reinterpret_cast<float4*>(args.dz + (int64_t)token * few_pitch(V) + v0 + 4 * g) = make_float4(z[0], z[1], z[2], z[3]);
         }
