@@ -53,6 +53,10 @@ struct TwoSums { floatx4 main, low; };
 __device__ __forceinline__ float result(const TwoSums& acc, int v) { return result(acc.main, v) + result(acc.low, v); }
 __device__ __forceinline__ void clear_sum(floatx4& acc) { acc = floatx4{0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ void clear_sum(TwoSums& acc) { acc.main = acc.low = floatx4{0.f, 0.f, 0.f, 0.f}; }
+// What a vector instruction has written into it is two wait states away from the matrix instructions behind, once all are held and settle() has followed.
+__device__ __forceinline__ void hold_sum(floatx4& acc) { asm volatile("" : "+a"(acc)); }
+__device__ __forceinline__ void hold_sum(TwoSums& acc) { asm volatile("" : "+a"(acc.main), "+a"(acc.low)); }
+__device__ __forceinline__ void settle() { asm volatile("s_nop 1"); }
 
 // Sums of exp2(z log2 e - base) over a wavefront's columns, those below p.n.  Base is the logit of the row's own label: the sum over all columns is then 1 at least,
 // what is lost below fp32 does not count in it, and no maximum has to be found first (a fifth of the instructions).  A sum that passes 2^64 (or is no number) is formed
@@ -325,7 +329,13 @@ void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) 
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < N; ++j) clear_sum(acc[i][j]);
+    };
+    auto hold = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) hold_sum(acc[i][j]);
     };
     if (k_all == 0) {                     // a batch without labels
         clear();
@@ -373,7 +383,7 @@ void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) 
     bf16x8 a[2][N], b[2][N];
     // products from register set SET; half 1 - SET of the stages sa, sb goes to the other set, a stage's loads to `to`.  (The products by hand: the compiler would keep
     // some of the sums outside the accumulation registers and spill.  It does not know them for what they are, and would not keep a vector instruction that writes an operand or a sum two wait
-    // states away: operands come from LDS, sums that are not fresh from memory or from the products before, so that there is none.  The epilogues leave the sums as they are for the same reason.)
+    // states away: operands come from LDS; sums that are not fresh come from memory, from the products before, or are zeros, which are held and settled.  The epilogues leave the sums as they are for the same reason.)
     auto step = [&](auto set, auto fresh, uint32_t sa, uint32_t sb, uint32_t to) __attribute__((always_inline)) {
         constexpr int P = decltype(set)::value;
 #pragma unroll
@@ -436,6 +446,8 @@ void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) 
         const int pairs = x.ke - x.kb;
         if constexpr (E == SUMS) {
             clear();
+            hold();
+            settle();
             begin(e, acc, x.m0 + wm, x.n0 + wn, x.split, lane);
             first(std::false_type{});
         } else {
@@ -457,10 +469,7 @@ void k_vocab_tile(const VocabProduct p, const typename EpilogueArgs<E>::type e) 
         }
         // the last product is 18 wait states from its result
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));
+        hold();
         finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
@@ -545,6 +554,12 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int j = 0; j < N; ++j) clear_sum(acc[i][j]);
+    };
+    auto hold = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) hold_sum(acc[i][j]);
     };
     if (units.k_all == 0) {               // a batch without labels
         clear();
@@ -683,6 +698,8 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
         const int pairs = x.ke - x.kb;
         if constexpr (E == SUMS) {
             clear();
+            hold();
+            settle();
             begin(e, acc, x.m0 + wm, x.n0 + wn, x.split, lane);
             step(zero, yes, no, stored);
         } else {
@@ -697,13 +714,7 @@ void k_vocab_parts_tile(const VocabProduct p, const typename EpilogueArgs<E>::ty
         }
         // the last product is 18 wait states from its result
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if constexpr (APART) asm volatile("" : "+a"(acc[i][j].main), "+a"(acc[i][j].low));
-                else asm volatile("" : "+a"(acc[i][j]));
-            }
+        hold();
         finish(e, p, acc, x.m0 + wm, x.n0 + wn, x.split, lane, m_rows);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // nothing may arrive in LDS that is not ours any more
