@@ -684,6 +684,16 @@ def _dense(t, dtype, numbers, device):
     return t.data_ptr()
 
 
+def _space(ws, device):
+    """Address and size of a workspace, one byte behind the other on the device that the call runs on; 0 for None"""
+    if ws is None:
+        return 0, 0
+    if getattr(ws, "get_device", None) is not None and (ws.get_device() != device or not ws.is_contiguous()):
+        raise ValueError("a workspace on %s%s where the call takes one of the current GPU, one byte behind the other"
+                         % (ws.device, "" if ws.is_contiguous() else " with strides %s" % (ws.stride(),)))
+    return ws.data_ptr(), ws.numel()
+
+
 _device_function = None
 
 
@@ -763,7 +773,7 @@ def mst_layer_norm_bwd(shape: LayerNormShape, sum, kept: Optional[Checkpoint8], 
     _check("mst_layer_norm_bwd",
            lib().mst_layer_norm_bwd(C.byref(shape), _dense(sum, tx, n, dev), _kept(kept, rows, width, dev), _dense(weight, f32, width, dev), _dense(bias, f32, width, dev),
                                     _dense(dy, tg, n, dev), _dense(ds, tx, n, dev), _dense(dx, tx, n, dev), _dense(dweight, f32, width, dev),
-                                    _dense(dbias, f32, width, dev), _dense(y, ty, n, dev), _ptr(ws), ws.numel(), _stream(stream)))
+                                    _dense(dbias, f32, width, dev), _dense(y, ty, n, dev), *_space(ws, dev), _stream(stream)))
 
 
 def mst_gelu_fwd(shape: GeluShape, x, y, kept: Optional[Checkpoint8] = None, stream=None):
@@ -789,7 +799,7 @@ def mst_vocab_loss_fwd(shape: VocabLossShape, h, E, labels, loss, lse, ws, strea
     dev = _device()
     _check("mst_vocab_loss_fwd",
            lib().mst_vocab_loss_fwd(C.byref(shape), _dense(h, t, nh, dev), _dense(E, t, nE, dev), _dense(labels, int32, T, dev), _dense(loss, f32, T, dev),
-                                    _dense(lse, f32, T, dev), _ptr(ws), ws.numel(), _stream(stream)))
+                                    _dense(lse, f32, T, dev), *_space(ws, dev), _stream(stream)))
 
 
 def mst_vocab_loss_bwd(shape: VocabLossShape, h, E, labels, lse, dloss, dh, dE, ws, stream=None):
@@ -797,4 +807,4 @@ def mst_vocab_loss_bwd(shape: VocabLossShape, h, E, labels, lse, dloss, dh, dE, 
     dev = _device()
     _check("mst_vocab_loss_bwd",
            lib().mst_vocab_loss_bwd(C.byref(shape), _dense(h, t, nh, dev), _dense(E, t, nE, dev), _dense(labels, int32, T, dev), _dense(lse, f32, T, dev),
-                                    _dense(dloss, f32, T, dev), _dense(dh, t, nh, dev), _dense(dE, t, nE, dev), _ptr(ws), ws.numel(), _stream(stream)))
+                                    _dense(dloss, f32, T, dev), _dense(dh, t, nh, dev), _dense(dE, t, nE, dev), *_space(ws, dev), _stream(stream)))
