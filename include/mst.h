@@ -648,7 +648,7 @@ int mst_layer_norm_fwd(const mst_norm_shape* shape, const void* x_dev, const voi
  * its values.  dx = the gradient of y through the norm, plus ds_dev, the gradient that reaches s along the residual stream (NULL: none);
  * it is the gradient of x and of the residual, and may be ds_dev or, of one type, dy_dev.  dweight_dev, dbias_dev fp32 [width] (NULL: not wanted).  y_dev takes y again
  * (NULL: not wanted; bias_dev is used for that alone).  Nothing else has to be kept from the forward call.
- * Workspace: mst_layer_norm_workspace_bytes, 0 on invalid arguments. */
+ * Workspace: mst_layer_norm_workspace_bytes (0 on invalid arguments); none (NULL, 0) where neither dweight nor dbias is wanted. */
 int mst_layer_norm_bwd(const mst_norm_shape* shape, const void* sum_dev, const mst_checkpoint8* kept, const float* weight_dev,
                        const float* bias_dev, const void* dy_dev, const void* ds_dev, void* dx_dev, float* dweight_dev, float* dbias_dev,
                        void* y_dev, void* ws_dev, size_t ws_bytes, mst_stream_t stream);

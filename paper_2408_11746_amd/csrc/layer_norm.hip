@@ -342,7 +342,8 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
                                   const void* ds, void* dx, float* dweight, float* dbias, void* y, void* ws, size_t ws_bytes, mst_stream_t stream) {
     using namespace mst;
     if (int e = check_shape(s)) return e;
-    if (!aligned16(dweight) || !aligned16(dbias) || !given(ws)) return MST_ERR_ARG;
+    const bool sums = dweight || dbias;
+    if (!aligned16(dweight) || !aligned16(dbias) || (sums && !given(ws))) return MST_ERR_ARG;
     if (s->rows > 0) {
         if ((sum != nullptr) == (kept != nullptr)) return MST_ERR_ARG;
         if (!given(dy) || !given(dx) || !aligned16(sum) || !aligned16(ds) || !aligned16(weight) || !aligned16(bias) || !aligned16(y)) return MST_ERR_ARG;
@@ -350,7 +351,7 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
             if (int e = check_kept(kept)) return e;
     }
     if (dx == dy && dy && s->grad_type != s->in_type) return MST_ERR_ARG;
-    if (ws_bytes < mst_layer_norm_workspace_bytes(s)) return MST_ERR_WORKSPACE;
+    if (sums && ws_bytes < mst_layer_norm_workspace_bytes(s)) return MST_ERR_WORKSPACE;
     const NormRows n = {s->rows, s->width, s->eps, 1.f / (float)s->width};
     const unsigned blocks = blocks_of(s, ROWS_A_BLOCK, BWD_BLOCKS);
     float* const partial = static_cast<float*>(ws);
@@ -364,7 +365,7 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
                 constexpr int WAVES = decltype(waves)::value;
                 k_layer_norm_bwd<decltype(ch)::value, WAVES, decltype(ends)::value, TS, TX, TG><<<blocks, 64 * (WAVES == 1 ? ROWS_A_BLOCK : WAVES), 0, st>>>(
                     n, from, units, weight, bias, static_cast<const TG*>(dy), static_cast<const TX*>(ds), static_cast<TX*>(dx), y, s->out_type == MST_F32,
-                    dweight || dbias ? partial : nullptr);
+                    sums ? partial : nullptr);
             });
         });
     };
@@ -379,7 +380,7 @@ extern "C" int mst_layer_norm_bwd(const mst_norm_shape* s, const void* sum, cons
         }
         MST_LAUNCH_CHECK();
     }
-    if (dweight || dbias) {               // (no rows: zeros)
+    if (sums) {                           // (no rows: zeros)
         k_layer_norm_sums<<<dim3((unsigned)cdiv(s->width, 16), 2), 512, 0, st>>>(partial, s->width, (int)blocks, dweight, dbias);
         MST_LAUNCH_CHECK();
     }
