@@ -1,6 +1,7 @@
 // Activations in 8 bits (mst_checkpoint_write, _read) and the activation between fc1 and fc2 with its gradient (mst_gelu_fwd, _bwd), which
 // writes and reads them beside its other operands: nothing but a pass over memory, and bound by that.  8192 x 5120 numbers, fp32 to bfloat16: 43 us (252 MB, 5.8 TB/s); the
 // gradient from fp32 to bfloat16 72 (420 MB, 5.8 TB/s).  16384 x 4096 with the 8-bit form: 83 us (471 MB, 5.7 TB/s); the gradient from it and y again 99 (604 MB, 6.1 TB/s).
+// The erf form is bound by the vector instructions of erfcf: 8192 x 5120 numbers to bfloat16 55 us from fp32 and 52 from bfloat16 (tanh, calls repeated in the same way: 38 and 29), the gradients 76 and 63 (73 and 42).
 // 4096 x 768 bfloat16 numbers into 8 bits or back: 4.2 us, a launch; 4099 x 1601 in fp32 8.3 and 8.0 (33 MB).
 //
 // 32 lanes take a group of 128 columns, four to a lane, so that a group's largest number is found within half a wavefront.  Where rows are whole groups, or no units are
